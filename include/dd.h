@@ -266,6 +266,87 @@ int dd_cache_insert_rows(void *Kc, void *Vc, const void *Krows, const void *Vrow
                          int B, int Hkv, int N, int d, dd_dtype qk_dtype, dd_dtype v_dtype, void *stream);
 
 /*
+ * Rows of a projection on their way into attention: the norm of every head of queries and keys, and the rotation by
+ * position, in one pass that also brings them into the [B, heads, n, d] order of the calls above.  For x = Q[b,h,i,:] and
+ * p = positions[b*n + i] (positions == NULL: p = i), with weight w = q_weight:
+ *     y = x / sqrt(mean(x^2) + eps) * w         (q_weight == NULL: y = x)
+ *     (u, v) -> (u cos a - v sin a, v cos a + u sin a),  a = p * inv_freq[k]       for k < rot_dim / 2, where (u, v) are the
+ *         elements k and k + rot_dim/2 of y (interleaved == 0) or 2k and 2k + 1 (interleaved != 0); elements from rot_dim on
+ *         stay as they are; rot_dim == 0 (inv_freq == NULL): no rotation
+ * and K likewise with k_weight.
+ *   Q  element (b,h,i,c) at q_batch*b + q_head*h + q_row*i + c (strides in elements, >= 0; an axis of one entry may have
+ *      any; otherwise a multiple of 16 bytes, the last element less than 2^40 elements from the first); dtype DD_F32 or DD_BF16.  So a view of a fused projection's output serves.
+ *   K  the same with Hkv heads and its own strides; K == NULL (then Ko == NULL): queries only
+ *   Qo [B,H,n,d], Ko [B,Hkv,n,d]  dense, dtype.  Qo may be Q (and Ko may be K) where that is dense itself; any other overlap of an
+ *      output with an input, or of the two outputs, is DD_ERR_SHAPE
+ *   q_weight, k_weight [d] dtype, 16-byte aligned; each may be NULL; with either, eps must be > 0 and finite
+ *   inv_freq [rot_dim/2] f32; rot_dim a multiple of 16, at most d        positions [B*n] i32, any value
+ * d in {64, 128}; B, H >= 1, Hkv >= 1 with K; n >= 0 (0: a no-op); B*n < 2^31, B*H*n*d and B*Hkv*n*d < 2^40.
+ * Arithmetic: fp32, angles reduced in fp64 (so that far positions turn by the right angle), results rounded once.
+ * Errors: DD_ERR_NULL, DD_ERR_SHAPE, DD_ERR_DTYPE, DD_ERR_ALIGN, DD_ERR_LAUNCH.
+ */
+int dd_qk_norm_rope(const void *Q, int64_t q_batch, int64_t q_head, int64_t q_row,
+                    const void *K, int64_t k_batch, int64_t k_head, int64_t k_row,
+                    const void *q_weight, const void *k_weight, float eps,
+                    const float *inv_freq, int rot_dim, int interleaved, const int32_t *positions,
+                    void *Qo, void *Ko, int B, int H, int Hkv, int n, int d, dd_dtype dtype, void *stream);
+
+/*
+ * A paged cache.  Pages of page_size positions (16, 32, 64 or 128) belong to one pool and sequences hold some of them:
+ *   Kc [num_pages,Hkv,page_size,d], Vc [num_pages,Hkv,d,page_size]     DD_BF16, or DD_FP8_E4M3 with
+ *   k_scale, v_scale [num_pages,Hkv] f32: real value = scale x decoded code; one scale per page and head
+ *   block_table [B,max_pages] i32: position p of sequence b is slot p % page_size of page block_table[b, p / page_size]
+ * (Values have the keys of one head dim side by side: the order in which the matrix instructions take them.)
+ * Entries of block_table, lengths and positions are device data and not validated; no access leaves the tensors for any value.
+ *
+ * dd_paged_cache_append brings rows of keys and values into the pages: row r < n_rows[b] of sequence b goes to position
+ * starts[b] + r; keys are normed and rotated on the way as in dd_qk_norm_rope, position starts[b] + r, with no rounding in
+ * between.  Rows at positions < 0 or >= max_pages*page_size, and rows whose page is not in [0, num_pages), are skipped.
+ *   K, V  [B,Hkv,n,d] by strides as in dd_qk_norm_rope, row_dtype DD_BF16 or DD_F32
+ *   starts [B] i32;  n_rows [B] i32 or NULL (n each; entries are clamped to [0, n])
+ *   kv_lens [B] i32: the positions that sequence b holds before the call, or NULL: starts[b] (rows are added at the end)
+ * With DD_BF16 pages a key is rounded once and nothing but the rows is written.  With DD_FP8_E4M3, for each page and head
+ * that gets rows, keys and values each for themselves: a = max |x| over those rows, s = 2^e with the least e >= -126 such that
+ * a <= 448 * 2^e; if the page holds other positions below kv_lens[b], s = max(s, its scale so far), and where that grows their
+ * codes become rne(code * old / s); rows become rne(x / s) (to nearest, ties to even).  Positions that are neither written
+ * nor below kv_lens[b] are left as they are.  A scale is positive and finite wherever the page holds positions.
+ * The pages that a call writes must be distinct over the sequences (else which rows and which scale win is unspecified);
+ * pages that are only read later (a shared prefix) may be shared.  K and V must not overlap the cache (not checked).  The
+ * caller owns kv_lens: the call does not write it.
+ * d in {64, 128}; B, Hkv, num_pages, max_pages >= 1; n >= 0 (0: a no-op); max_pages*page_size < 2^31, num_pages*Hkv*page_size*d < 2^40.
+ * Errors: DD_ERR_NULL (scales are required with DD_FP8_E4M3), DD_ERR_SHAPE, DD_ERR_DTYPE, DD_ERR_ALIGN, DD_ERR_LAUNCH.
+ */
+int dd_paged_cache_append(void *Kc, void *Vc, float *k_scale, float *v_scale,
+                          const void *K, int64_t k_batch, int64_t k_head, int64_t k_row,
+                          const void *V, int64_t v_batch, int64_t v_head, int64_t v_row,
+                          const int32_t *block_table, const int32_t *starts, const int32_t *kv_lens, const int32_t *n_rows,
+                          const void *k_weight, float eps, const float *inv_freq, int rot_dim, int interleaved,
+                          int n, int B, int Hkv, int d, int num_pages, int page_size, int max_pages,
+                          dd_dtype row_dtype, dd_dtype cache_dtype, void *stream);
+
+/*
+ * Drafter attention over a paged cache, from single tokens (n = 1) to blocks and prompts: the formula of
+ * dd_block_attention_cached (no causal mask) over the positions j < kv_lens[b] that sequence b holds,
+ *     O[b,h,i,:] = sum_j softmax_j( Q[b,h,i,:] . K_j / sqrt(d) ) V_j
+ * with K_j, V_j of kv head h*Hkv/H as the cache holds them; the block's own rows take part by being appended first.
+ * kv_lens[b] is clamped to [0, max_pages*page_size]; positions whose page is not in [0, num_pages) take no part; a sequence
+ * without a position that does gets zeros.  Slots that hold no position may hold anything, NaN included.
+ *   Q, O [B,H,n,d] DD_BF16, dense;  cache_dtype DD_BF16 or DD_FP8_E4M3 (then k_scale and v_scale are required, positive and finite
+ *   wherever a page holds positions)
+ * Arithmetic: matrix cores with fp32 accumulation, e4m3 codes decoded exactly to bf16, k_scale in the exponent's factor, fp32
+ * online softmax, weights (times v_scale) rounded to bf16 before the PV product.
+ * The key range is split over workgroups where those are few; the partial states live in `workspace`.  A capacity
+ * max_pages*page_size far above the lengths costs workspace, not time: a sequence's own keys are shared out.
+ * d in {64, 128}; H % Hkv == 0; B, H, Hkv, num_pages, max_pages >= 1; n >= 0 (0: a no-op); sizes as above, B*H*n < 2^31.
+ */
+int dd_paged_attention(const void *Q, const void *Kc, const void *Vc, const float *k_scale, const float *v_scale,
+                       const int32_t *block_table, const int32_t *kv_lens, void *O,
+                       int n, int B, int H, int Hkv, int d, int num_pages, int page_size, int max_pages,
+                       dd_dtype cache_dtype, void *workspace, size_t workspace_bytes, void *stream);
+size_t dd_paged_attention_workspace_bytes(int n, int B, int H, int Hkv, int d, int page_size, int max_pages,
+                                          dd_dtype cache_dtype);
+
+/*
  * Verification rule of Sec. 3.2 for P = B*G positions (G verified positions per sequence),
  * softmax at temperature 1 over the whole vocabulary, natural logarithm:
  *     c_V,i  = max_x p_V(x | i)                     (Eq. 7)      t_V,i = lowest x attaining it

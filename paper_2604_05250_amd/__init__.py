@@ -91,6 +91,16 @@ def lib():
     L.dd_verify_scores.argtypes = [vp, vp, vp, vp, vp, vp, vp, i, i, i, vp, sz, vp]
     L.dd_verify_scores_workspace_bytes.restype = sz
     L.dd_verify_scores_workspace_bytes.argtypes = [i, i, i]
+    i64, f = C.c_int64, C.c_float
+    L.dd_qk_norm_rope.restype = i
+    L.dd_qk_norm_rope.argtypes = [vp, i64, i64, i64, vp, i64, i64, i64, vp, vp, f, vp, i, i, vp, vp, vp, i, i, i, i, i, i, vp]
+    L.dd_paged_cache_append.restype = i
+    L.dd_paged_cache_append.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, vp, i64, i64, i64, vp, vp, vp, vp, vp, f, vp, i, i,
+                                        i, i, i, i, i, i, i, i, i, vp]
+    L.dd_paged_attention.restype = i
+    L.dd_paged_attention.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i, i, i, i, i, i, i, i, i, vp, sz, vp]
+    L.dd_paged_attention_workspace_bytes.restype = sz
+    L.dd_paged_attention_workspace_bytes.argtypes = [i, i, i, i, i, i, i, i]
     _lib = L
     return L
 
@@ -103,7 +113,8 @@ EXPORTS = ("dd_strerror", "dd_version", "dd_bidir_attention", "dd_bidir_attentio
            "dd_block_attention_window", "dd_block_attention_window_workspace_bytes", "dd_cache_insert_rows",
            "dd_block_attention_batched", "dd_block_attention_batched_workspace_bytes",
            "dd_bidir_attention_fp8v", "dd_block_attention_cached_fp8v", "dd_block_attention_cached_fp8v_workspace_bytes",
-           "dd_bidir_attention_mx")
+           "dd_bidir_attention_mx", "dd_qk_norm_rope", "dd_paged_cache_append", "dd_paged_attention",
+           "dd_paged_attention_workspace_bytes")
 
 
 # ---------------------------------------------------------------- marshalling (csrc/binding.cpp)
@@ -229,6 +240,36 @@ def dd_cache_insert_rows(Kc, Vc, Krows, Vrows, positions, qk_dtype: Optional[int
     """Kc/Vc [B,Hkv,N,d] <- rows of Krows/Vrows [B,Hkv,n,d] at positions [B,n] (i32, on the device; entries outside
     [0, N) skip their row).  In place; returns None."""
     native().cache_insert(Kc, Vc, Krows, Vrows, positions, qk_dtype, v_dtype)
+
+
+def dd_qk_norm_rope(Q, K=None, q_weight=None, k_weight=None, eps: float = 1e-6, inv_freq=None, positions=None,
+                    interleaved: bool = False, Qo=None, Ko=None, dtype: Optional[int] = None):
+    """Head norms and the rotation by position, from a projection's rows to dense queries and keys.  Q [B,H,n,d],
+    K [B,Hkv,n,d] (optional): any strides, the last dimension contiguous (q.view(B,n,H,d).transpose(1,2) of a fused
+    projection); weights [d] of the same type; inv_freq [rot_dim/2] f32; positions [B,n] i32 (default 0..n-1).
+    Returns (Qo, Ko), contiguous; Ko is None without K."""
+    return native().qk_norm_rope(Q, K, q_weight, k_weight, eps, inv_freq, positions, interleaved, Qo, Ko, dtype)
+
+
+def dd_paged_cache_append(Kc, Vc, K, V, block_table, starts, kv_lens=None, n_rows=None, k_scale=None, v_scale=None, k_weight=None,
+                          eps: float = 1e-6, inv_freq=None, interleaved: bool = False, row_dtype: Optional[int] = None,
+                          cache_dtype: Optional[int] = None):
+    """Rows K, V [B,Hkv,n,d] (any strides) into the pages Kc [pages,Hkv,page_size,d], Vc [pages,Hkv,d,page_size] of their
+    sequences: row r of sequence b to position starts[b] + r, keys normed (k_weight) and rotated (inv_freq) on the way.  bf16
+    pages, or e4m3 pages with k_scale, v_scale [pages,Hkv] f32.  block_table [B,max_pages], starts, kv_lens (lengths before the
+    call; default: starts), n_rows (default: n) [B]: i32, on the device.  In place; returns None."""
+    native().paged_append(Kc, Vc, K, V, block_table, starts, kv_lens, n_rows, k_scale, v_scale, k_weight, eps, inv_freq, interleaved,
+                          row_dtype, cache_dtype)
+
+
+def dd_paged_attention_workspace_bytes(n, B, H, Hkv, d, page_size, max_pages, cache_dtype) -> int:
+    return lib().dd_paged_attention_workspace_bytes(n, B, H, Hkv, d, page_size, max_pages, cache_dtype)
+
+
+def dd_paged_attention(Q, Kc, Vc, block_table, kv_lens, k_scale=None, v_scale=None, O=None, cache_dtype: Optional[int] = None):
+    """Attention of Q [B,H,n,d] (bf16) over the kv_lens[b] positions that each sequence holds in a paged cache (shapes as for
+    dd_paged_cache_append) -> O [B,H,n,d] bf16; a sequence that holds none gets zeros."""
+    return native().paged_attention(Q, Kc, Vc, block_table, kv_lens, k_scale, v_scale, O, cache_dtype)
 
 
 def dd_verify_remask_workspace_bytes(B, G, V, logit_dtype) -> int:

@@ -19,6 +19,7 @@
 #include <ATen/record_function.h>
 #include <c10/core/impl/LocalDispatchKeySet.h>
 #include <c10/hip/HIPGraphsC10Utils.h>
+#include <c10/hip/HIPGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -570,6 +571,182 @@ PyObject *verify_scores(PyObject *const *a, Py_ssize_t n)
     return t;
 }
 
+// ---- rows before attention and the paged cache.  These calls run on the current stream of the device that their tensors are on,
+// which need not be the current one; all of them have to be there.
+struct OneDevice {
+    const at::Tensor &on;
+    explicit OneDevice(const at::Tensor &t) : on(t) {}
+    void *operator()(const at::Tensor *t, const char *what, bool dense = true) const
+    {
+        if (t == nullptr) return nullptr;
+        if (!t->is_cuda()) value_error(what, "must live in GPU memory");
+        if (t->device() != on.device()) value_error(what, "must be on the device of the other tensors");
+        if (dense && !t->is_contiguous()) value_error(what, "must be contiguous");
+        return t->data_ptr();
+    }
+    void *operator()(const at::Tensor &t, const char *what, bool dense = true) const { return (*this)(&t, what, dense); }
+};
+// rows [B, heads, n, d] by strides: the last dimension dense
+void rows_of(const at::Tensor &t, const char *what)
+{
+    if (t.size(3) > 1 && t.stride(3) != 1) value_error(what, "the last dimension must be contiguous");
+}
+void ints_of(const at::Tensor *t, int64_t n, const char *what)
+{
+    if (t == nullptr || (t->scalar_type() == at::kInt && t->numel() == n)) return;
+    PyErr_Format(PyExc_ValueError, "%s: must be int32 with %lld entries", what, (long long)n);
+    throw Raised{};
+}
+void weight_of(const at::Tensor *t, int tag, int64_t d, const char *what)
+{
+    if (t == nullptr) return;
+    elements_of(t, tag, what);
+    if (t->numel() == d) return;
+    PyErr_Format(PyExc_ValueError, "%s: must have %lld elements", what, (long long)d);
+    throw Raised{};
+}
+int rotated_dims(const at::Tensor *inv_freq, int64_t d)
+{
+    if (inv_freq == nullptr) return 0;
+    if (inv_freq->scalar_type() != at::kFloat) {
+        PyErr_Format(PyExc_TypeError, "inv_freq: float32 expected, has %s", c10::toString(inv_freq->scalar_type()));
+        throw Raised{};
+    }
+    if (2 * inv_freq->numel() > d) value_error("inv_freq", "has more than d/2 entries");
+    return (int)(2 * inv_freq->numel());
+}
+int truth(PyObject *o)
+{
+    const int v = PyObject_IsTrue(o);
+    if (v < 0) throw Raised{};
+    return v;
+}
+// sizes as the library takes them
+void fits_int(std::initializer_list<int64_t> v)
+{
+    for (const int64_t x : v)
+        if (x > 0x7fffffff) value_error("", "a size is out of range");
+}
+
+// (Q, K, q_weight, k_weight, eps, inv_freq, positions, interleaved, Qo, Ko, dtype) -> (Qo, Ko | None)
+PyObject *qk_norm_rope(PyObject *const *a, Py_ssize_t n)
+{
+    want(n, 11);
+    const at::Tensor &Q = tensor(a[0], "Q");
+    const at::Tensor *K = opt_tensor(a[1], "K"), *qw = opt_tensor(a[2], "q_weight"), *kw = opt_tensor(a[3], "k_weight");
+    const float eps = (float)real(a[4]);
+    const at::Tensor *freq = opt_tensor(a[5], "inv_freq"), *pos = opt_tensor(a[6], "positions"), *Qo = opt_tensor(a[8], "Qo"), *Ko = opt_tensor(a[9], "Ko");
+    const int interleaved = truth(a[7]);
+    if (Q.dim() != 4 || (K && K->dim() != 4)) value_error("", "Q, K must have four dimensions");
+    const int64_t B = Q.size(0), H = Q.size(1), rows = Q.size(2), d = Q.size(3), Hkv = K ? K->size(1) : 0;
+    if (K && !has_shape(*K, {B, Hkv, rows, d})) value_error("", "K shape must be [B,Hkv,n,d] matching Q");
+    if (!K && (Ko || kw)) value_error("", "Ko and k_weight go with K");
+    fits_int({B, H, Hkv, rows, d});
+    const int tag = tag_or(a[10], Q, "Q");
+    elements_of(&Q, tag, "Q"); elements_of(K, tag, "K"); elements_of(Qo, tag, "Qo"); elements_of(Ko, tag, "Ko");
+    weight_of(qw, tag, d, "q_weight"); weight_of(kw, tag, d, "k_weight");
+    const int rot = rotated_dims(freq, d);
+    ints_of(pos, B * rows, "positions");
+    room_for(Qo, B * H * rows * d, tag_bytes(tag), "Qo"); room_for(Ko, B * Hkv * rows * d, tag_bytes(tag), "Ko");
+    rows_of(Q, "Q");
+    if (K) rows_of(*K, "K");
+    const OneDevice dev(Q);
+    void *const q = dev(Q, "Q", false), *const k = dev(K, "K", false), *const w = dev(qw, "q_weight"), *const v = dev(kw, "k_weight");
+    void *const f = dev(freq, "inv_freq"), *const p = dev(pos, "positions");
+    const c10::hip::HIPGuard guard(Q.device().index());
+    const at::Tensor qo = Qo ? *Qo : empty_like_type({B, H, rows, d}, Q.scalar_type(), Q);
+    const at::Tensor ko = Ko ? *Ko : K ? empty_like_type({B, Hkv, rows, d}, K->scalar_type(), Q) : at::Tensor();
+    void *const x = dev(qo, "Qo"), *const y = dev(ko.defined() ? &ko : nullptr, "Ko");
+    const hipStream_t stream = current_stream();
+    const int64_t ks[3] = {K ? K->stride(0) : 0, K ? K->stride(1) : 0, K ? K->stride(2) : 0};
+    check(unlocked([&] { return dd_qk_norm_rope(q, Q.stride(0), Q.stride(1), Q.stride(2), k, ks[0], ks[1], ks[2], w, v, eps, (const float *)f, rot,
+                                                interleaved, (const int32_t *)p, x, y, B, H, Hkv, rows, d, (dd_dtype)tag, stream); }),
+          "dd_qk_norm_rope");
+    PyObject *t = PyTuple_New(2);
+    if (t == nullptr) throw Raised{};
+    PyTuple_SET_ITEM(t, 0, THPVariable_Wrap(qo));
+    if (ko.defined()) {
+        PyTuple_SET_ITEM(t, 1, THPVariable_Wrap(ko));
+    } else {
+        Py_INCREF(Py_None); PyTuple_SET_ITEM(t, 1, Py_None);
+    }
+    return t;
+}
+
+struct Pages { int64_t num, Hkv, size, d, B, max; int tag; };
+Pages pages_of(const at::Tensor &Kc, const at::Tensor &Vc, const at::Tensor &table, const at::Tensor *ks, const at::Tensor *vs, PyObject *tag)
+{
+    if (Kc.dim() != 4) value_error("", "Kc, Vc must have four dimensions");
+    Pages p{Kc.size(0), Kc.size(1), Kc.size(2), Kc.size(3), 0, 0, 0};
+    if (!has_shape(Vc, {p.num, p.Hkv, p.d, p.size})) value_error("", "shapes must be Kc [pages,Hkv,page_size,d] and Vc [pages,Hkv,d,page_size]");
+    if (table.dim() != 2 || table.scalar_type() != at::kInt) value_error("", "block_table must be int32 with two dimensions");
+    p.B = table.size(0);
+    p.max = table.size(1);
+    fits_int({p.num, p.Hkv, p.size, p.d, p.B, p.max});
+    p.tag = tag_or(tag, Kc, "Kc");
+    elements_of(&Kc, p.tag, "Kc"); elements_of(&Vc, p.tag, "Vc");
+    scales_of(ks, p.num * p.Hkv, "k_scale"); scales_of(vs, p.num * p.Hkv, "v_scale");
+    return p;
+}
+
+// (Kc, Vc, K, V, block_table, starts, kv_lens, n_rows, k_scale, v_scale, k_weight, eps, inv_freq, interleaved, row_dtype, cache_dtype) -> None
+PyObject *paged_append(PyObject *const *a, Py_ssize_t n)
+{
+    want(n, 16);
+    const at::Tensor &Kc = tensor(a[0], "Kc"), &Vc = tensor(a[1], "Vc"), &K = tensor(a[2], "K"), &V = tensor(a[3], "V"), &table = tensor(a[4], "block_table");
+    const at::Tensor &starts = tensor(a[5], "starts");
+    const at::Tensor *lens = opt_tensor(a[6], "kv_lens"), *count = opt_tensor(a[7], "n_rows"), *ks = opt_tensor(a[8], "k_scale"), *vs = opt_tensor(a[9], "v_scale");
+    const at::Tensor *kw = opt_tensor(a[10], "k_weight"), *freq = opt_tensor(a[12], "inv_freq");
+    const float eps = (float)real(a[11]);
+    const int interleaved = truth(a[13]);
+    const Pages p = pages_of(Kc, Vc, table, ks, vs, a[15]);
+    if (K.dim() != 4 || !has_shape(K, {p.B, p.Hkv, K.size(2), p.d}) || V.sizes() != K.sizes()) value_error("", "K and V shapes must be [B,Hkv,n,d] matching the cache");
+    const int64_t rows = K.size(2);
+    fits_int({rows});
+    const int tag = tag_or(a[14], K, "K");
+    elements_of(&K, tag, "K"); elements_of(&V, tag, "V");
+    weight_of(kw, tag, p.d, "k_weight");
+    const int rot = rotated_dims(freq, p.d);
+    ints_of(&starts, p.B, "starts"); ints_of(lens, p.B, "kv_lens"); ints_of(count, p.B, "n_rows");
+    rows_of(K, "K"); rows_of(V, "V");
+    const OneDevice dev(Kc);
+    void *const kc = dev(Kc, "Kc"), *const vc = dev(Vc, "Vc"), *const k = dev(K, "K", false), *const v = dev(V, "V", false), *const t = dev(table, "block_table");
+    void *const st = dev(starts, "starts"), *const ln = dev(lens, "kv_lens"), *const ct = dev(count, "n_rows"), *const sk = dev(ks, "k_scale"), *const sv = dev(vs, "v_scale");
+    void *const w = dev(kw, "k_weight"), *const f = dev(freq, "inv_freq");
+    const c10::hip::HIPGuard guard(Kc.device().index());
+    const hipStream_t stream = current_stream();
+    check(unlocked([&] { return dd_paged_cache_append(kc, vc, (float *)sk, (float *)sv, k, K.stride(0), K.stride(1), K.stride(2), v, V.stride(0), V.stride(1),
+                                                      V.stride(2), (const int32_t *)t, (const int32_t *)st, (const int32_t *)ln, (const int32_t *)ct, w, eps,
+                                                      (const float *)f, rot, interleaved, rows, p.B, p.Hkv, p.d, p.num, p.size, p.max, (dd_dtype)tag,
+                                                      (dd_dtype)p.tag, stream); }), "dd_paged_cache_append");
+    Py_RETURN_NONE;
+}
+
+// (Q, Kc, Vc, block_table, kv_lens, k_scale, v_scale, O, cache_dtype) -> O
+PyObject *paged_attention(PyObject *const *a, Py_ssize_t n)
+{
+    want(n, 9);
+    const at::Tensor &Q = tensor(a[0], "Q"), &Kc = tensor(a[1], "Kc"), &Vc = tensor(a[2], "Vc"), &table = tensor(a[3], "block_table"), &lens = tensor(a[4], "kv_lens");
+    const at::Tensor *ks = opt_tensor(a[5], "k_scale"), *vs = opt_tensor(a[6], "v_scale"), *O = opt_tensor(a[7], "O");
+    const Pages p = pages_of(Kc, Vc, table, ks, vs, a[8]);
+    if (Q.dim() != 4 || Q.size(0) != p.B || Q.size(3) != p.d) value_error("", "Q shape must be [B,H,n,d] matching the cache and block_table");
+    const int64_t H = Q.size(1), rows = Q.size(2);
+    fits_int({H, rows});
+    elements_of(&Q, DD_BF16, "Q"); elements_of(O, DD_BF16, "O");
+    ints_of(&lens, p.B, "kv_lens");
+    room_for(O, p.B * H * rows * p.d, 2, "O");
+    const OneDevice dev(Q);
+    void *const q = dev(Q, "Q"), *const kc = dev(Kc, "Kc"), *const vc = dev(Vc, "Vc"), *const t = dev(table, "block_table"), *const ln = dev(lens, "kv_lens");
+    void *const sk = dev(ks, "k_scale"), *const sv = dev(vs, "v_scale");
+    const c10::hip::HIPGuard guard(Q.device().index());
+    const at::Tensor out = O ? *O : empty_like_type({p.B, H, rows, p.d}, Q.scalar_type(), Q);
+    void *const o = dev(out, "O");
+    const Call c(dd_paged_attention_workspace_bytes(rows, p.B, H, p.Hkv, p.d, p.size, p.max, (dd_dtype)p.tag), Q);
+    check(unlocked([&] { return dd_paged_attention(q, kc, vc, (const float *)sk, (const float *)sv, (const int32_t *)t, (const int32_t *)ln, o, rows, p.B, H, p.Hkv,
+                                                   p.d, p.num, p.size, p.max, (dd_dtype)p.tag, c.ptr(), c.bytes(), c.stream); }), "dd_paged_attention");
+    return THPVariable_Wrap(out);
+}
+
 // (DDError) -> None
 PyObject *set_error_class(PyObject *const *a, Py_ssize_t n)
 {
@@ -617,6 +794,7 @@ PyObject *entry(PyObject *, PyObject *const *a, Py_ssize_t n)
 #define DD_METHOD(name) {#name, (PyCFunction)(void (*)(void))entry<name>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {DD_METHOD(bidir), DD_METHOD(block), DD_METHOD(bidir_fp8v), DD_METHOD(bidir_mx), DD_METHOD(block_fp8v),
                          DD_METHOD(cache_insert), DD_METHOD(verify_remask), DD_METHOD(unmask), DD_METHOD(verify_scores),
+                         DD_METHOD(qk_norm_rope), DD_METHOD(paged_append), DD_METHOD(paged_attention),
                          DD_METHOD(set_error_class), DD_METHOD(set_fixed_workspace), DD_METHOD(reset_workspace_peak),
                          DD_METHOD(workspace_peak), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", "argument marshalling of paper_2604_05250_amd", -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -402,6 +402,170 @@ int dd_cache_insert_rows(void *Kc, void *Vc, const void *Krows, const void *Vrow
     return e == hipSuccess ? DD_OK : DD_ERR_LAUNCH;
 }
 
+// strides of rows (elements): non-negative, and a multiple of 16 bytes where an axis has more than one entry
+static int check_strides(const int64_t *st, const int *extent, int eb)
+{
+    double last = 0;
+    for (int i = 0; i < 3; ++i) {
+        if (extent[i] <= 1) continue;
+        if (st[i] < 0) return DD_ERR_SHAPE;
+        last += (double)st[i] * (extent[i] - 1);
+        if (last >= 1099511627776.0) return DD_ERR_SHAPE;
+        if (st[i] * eb % 16 != 0) return DD_ERR_ALIGN;
+    }
+    return DD_OK;
+}
+// bytes from the first element that rows by strides reach
+static uintptr_t reach(const int64_t *st, const int *extent, int d, int eb)
+{
+    uintptr_t last = (uintptr_t)d;
+    for (int i = 0; i < 3; ++i)
+        if (extent[i] > 1) last += (uintptr_t)st[i] * (uintptr_t)(extent[i] - 1);
+    return last * (uintptr_t)eb;
+}
+static bool overlap(const void *a, uintptr_t na, const void *b, uintptr_t nb)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x < y + nb && y < x + na;
+}
+static int check_rotation(const void *weight, float eps, const float *inv_freq, int rot_dim, int d)
+{
+    if (rot_dim < 0 || rot_dim > d || rot_dim % 16 != 0) return DD_ERR_SHAPE;
+    if (rot_dim > 0 && !inv_freq) return DD_ERR_NULL;
+    if (weight && !(eps > 0.0f && eps <= 3.0e38f)) return DD_ERR_SHAPE;
+    if (misaligned16(weight) || (reinterpret_cast<uintptr_t>(inv_freq) & 3u) != 0) return DD_ERR_ALIGN;
+    return DD_OK;
+}
+
+int dd_qk_norm_rope(const void *Q, int64_t q_batch, int64_t q_head, int64_t q_row,
+                    const void *K, int64_t k_batch, int64_t k_head, int64_t k_row,
+                    const void *q_weight, const void *k_weight, float eps,
+                    const float *inv_freq, int rot_dim, int interleaved, const int32_t *positions,
+                    void *Qo, void *Ko, int B, int H, int Hkv, int n, int d, dd_dtype dtype, void *stream)
+{
+    if (dtype != DD_F32 && dtype != DD_BF16) return DD_ERR_DTYPE;
+    if (n == 0 && B >= 1 && H >= 1 && Hkv >= 0 && (d == 64 || d == 128)) return DD_OK;
+    if (!Q || !Qo || (K == nullptr) != (Ko == nullptr)) return DD_ERR_NULL;
+    if (B < 1 || H < 1 || n < 0 || (K && Hkv < 1) || (d != 64 && d != 128)) return DD_ERR_SHAPE;
+    const int kv = K ? Hkv : 0, eb = dtype == DD_BF16 ? 2 : 4;
+    if ((double)B * n >= 2147483648.0 || (double)B * (H > kv ? H : kv) * n * d >= 1099511627776.0) return DD_ERR_SHAPE;
+    int rc = check_rotation(q_weight ? q_weight : K ? k_weight : nullptr, eps, inv_freq, rot_dim, d);
+    if (rc != DD_OK) return rc;
+    const int64_t qs[3] = {q_batch, q_head, q_row}, ks[3] = {k_batch, k_head, k_row};
+    const int qe[3] = {B, H, n}, ke[3] = {B, kv, n};
+    if ((rc = check_strides(qs, qe, eb)) != DD_OK || (K && (rc = check_strides(ks, ke, eb)) != DD_OK)) return rc;
+    if (misaligned16(Q) || misaligned16(K) || misaligned16(Qo) || misaligned16(Ko) || misaligned16(q_weight) || misaligned16(k_weight) ||
+        (reinterpret_cast<uintptr_t>(positions) & 3u) != 0)
+        return DD_ERR_ALIGN;
+    // an output may be its own dense input (a row is read whole by the lanes that write it) and shares memory with nothing else
+    const uintptr_t qb = (uintptr_t)B * H * n * d * eb, kb = (uintptr_t)B * kv * n * d * eb;
+    const uintptr_t qr = reach(qs, qe, d, eb), kr = K ? reach(ks, ke, d, eb) : 0;
+    auto dense = [&](const int64_t *st, int heads) {
+        return (B == 1 || st[0] == (int64_t)heads * n * d) && (heads == 1 || st[1] == (int64_t)n * d) && (n == 1 || st[2] == d);
+    };
+    const bool q_in_place = Qo == Q && dense(qs, H), k_in_place = K && Ko == K && dense(ks, kv);
+    if ((!q_in_place && overlap(Qo, qb, Q, qr)) || (K && overlap(Qo, qb, K, kr))) return DD_ERR_SHAPE;
+    if (K && ((!k_in_place && overlap(Ko, kb, K, kr)) || overlap(Ko, kb, Q, qr) || overlap(Ko, kb, Qo, qb))) return DD_ERR_SHAPE;
+    dd::NormRotateArgs a;
+    auto side = [](dd::NormRotateSide &s, const void *x, void *y, const void *w, int heads, const int64_t *st, const int *extent) {
+        s.x = x; s.y = y; s.weight = w; s.heads = heads;
+        s.batch = extent[0] > 1 ? st[0] : 0; s.head = extent[1] > 1 ? st[1] : 0; s.row = extent[2] > 1 ? st[2] : 0;
+    };
+    side(a.q, Q, Qo, q_weight, H, qs, qe);
+    if (K) side(a.k, K, Ko, k_weight, kv, ks, ke);
+    a.inv_freq = inv_freq; a.positions = positions;
+    a.tokens = (unsigned)((long)B * n); a.n = n; a.rot = rot_dim;
+    a.interleaved = interleaved != 0;
+    a.eps = eps;
+    const hipError_t e = dd::launch_norm_rotate(a, d, dtype == DD_BF16, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? DD_OK : DD_ERR_LAUNCH;
+}
+
+static int page_log2_of(int page_size) { return page_size == 16 ? 4 : page_size == 32 ? 5 : page_size == 64 ? 6 : page_size == 128 ? 7 : -1; }
+// what the calls on a paged cache have in common
+static int check_pages(const void *Kc, const void *Vc, const float *k_scale, const float *v_scale, const int32_t *table, const int32_t *lens,
+                       int n, int B, int Hkv, int d, int num_pages, int page_size, int max_pages, dd_dtype cache_dtype)
+{
+    if (!Kc || !Vc || !table || !lens) return DD_ERR_NULL;
+    if (cache_dtype != DD_BF16 && cache_dtype != DD_FP8_E4M3) return DD_ERR_DTYPE;
+    if (cache_dtype == DD_FP8_E4M3 && (!k_scale || !v_scale)) return DD_ERR_NULL;
+    if (n < 0 || B < 1 || Hkv < 1 || (d != 64 && d != 128) || num_pages < 1 || max_pages < 1 || page_log2_of(page_size) < 0) return DD_ERR_SHAPE;
+    if ((double)max_pages * page_size >= 2147483648.0 || (double)num_pages * Hkv * page_size * d >= 1099511627776.0) return DD_ERR_SHAPE;
+    if (misaligned16(Kc) || misaligned16(Vc)) return DD_ERR_ALIGN;
+    const uintptr_t words = reinterpret_cast<uintptr_t>(k_scale) | reinterpret_cast<uintptr_t>(v_scale) | reinterpret_cast<uintptr_t>(table) |
+                            reinterpret_cast<uintptr_t>(lens);
+    return (words & 3u) != 0 ? DD_ERR_ALIGN : DD_OK;
+}
+
+int dd_paged_cache_append(void *Kc, void *Vc, float *k_scale, float *v_scale,
+                          const void *K, int64_t k_batch, int64_t k_head, int64_t k_row,
+                          const void *V, int64_t v_batch, int64_t v_head, int64_t v_row,
+                          const int32_t *block_table, const int32_t *starts, const int32_t *kv_lens, const int32_t *n_rows,
+                          const void *k_weight, float eps, const float *inv_freq, int rot_dim, int interleaved,
+                          int n, int B, int Hkv, int d, int num_pages, int page_size, int max_pages,
+                          dd_dtype row_dtype, dd_dtype cache_dtype, void *stream)
+{
+    int rc = check_pages(Kc, Vc, k_scale, v_scale, block_table, starts, n, B, Hkv, d, num_pages, page_size, max_pages, cache_dtype);
+    if (rc != DD_OK || n == 0) return rc;
+    if (!K || !V) return DD_ERR_NULL;
+    if (row_dtype != DD_BF16 && row_dtype != DD_F32) return DD_ERR_DTYPE;
+    if ((double)B * Hkv * n * d >= 1099511627776.0) return DD_ERR_SHAPE;
+    if ((rc = check_rotation(k_weight, eps, inv_freq, rot_dim, d)) != DD_OK) return rc;
+    const int eb = row_dtype == DD_BF16 ? 2 : 4;
+    const int64_t ks[3] = {k_batch, k_head, k_row}, vs[3] = {v_batch, v_head, v_row};
+    const int extent[3] = {B, Hkv, n};
+    if ((rc = check_strides(ks, extent, eb)) != DD_OK || (rc = check_strides(vs, extent, eb)) != DD_OK) return rc;
+    if (misaligned16(K) || misaligned16(V) || ((reinterpret_cast<uintptr_t>(kv_lens) | reinterpret_cast<uintptr_t>(n_rows)) & 3u) != 0) return DD_ERR_ALIGN;
+    const int log2 = page_log2_of(page_size);
+    if (dd::page_append_wgs(n, B, Hkv, log2) >= (1L << 31)) return DD_ERR_SHAPE;
+    dd::PageAppendArgs a;
+    auto side = [&](dd::PageAppendSide &s, const void *x, void *cache, float *scale, const int64_t *st) {
+        s.x = x; s.cache = cache; s.scale = cache_dtype == DD_FP8_E4M3 ? scale : nullptr;
+        s.batch = B > 1 ? st[0] : 0; s.head = Hkv > 1 ? st[1] : 0; s.row = n > 1 ? st[2] : 0;
+    };
+    side(a.k, K, Kc, k_scale, ks);
+    side(a.v, V, Vc, v_scale, vs);
+    a.table = block_table; a.starts = starts; a.kv_lens = kv_lens; a.n_rows = n_rows;
+    a.weight = k_weight; a.inv_freq = inv_freq; a.eps = eps;
+    a.n = n; a.B = B; a.Hkv = Hkv; a.num_pages = num_pages; a.max_pages = max_pages; a.page_log2 = log2; a.rot = rot_dim;
+    a.interleaved = interleaved != 0;
+    const hipError_t e = dd::launch_page_append(a, d, row_dtype == DD_BF16, cache_dtype == DD_FP8_E4M3, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? DD_OK : DD_ERR_LAUNCH;
+}
+
+size_t dd_paged_attention_workspace_bytes(int n, int B, int H, int Hkv, int d, int page_size, int max_pages, dd_dtype cache_dtype)
+{
+    if (n < 1 || B < 1 || H < 1 || Hkv < 1 || H % Hkv != 0 || (d != 64 && d != 128) || max_pages < 1 || page_log2_of(page_size) < 0) return 0;
+    if (cache_dtype != DD_BF16 && cache_dtype != DD_FP8_E4M3) return 0;
+    if ((double)max_pages * page_size >= 2147483648.0 || (double)B * H * n >= 2147483648.0) return 0;
+    return dd::paged_attention_workspace_bytes(n, B, H, Hkv, d, (long)max_pages * page_size, cache_dtype == DD_FP8_E4M3);
+}
+
+int dd_paged_attention(const void *Q, const void *Kc, const void *Vc, const float *k_scale, const float *v_scale,
+                       const int32_t *block_table, const int32_t *kv_lens, void *O,
+                       int n, int B, int H, int Hkv, int d, int num_pages, int page_size, int max_pages,
+                       dd_dtype cache_dtype, void *workspace, size_t workspace_bytes, void *stream)
+{
+    int rc = check_pages(Kc, Vc, k_scale, v_scale, block_table, kv_lens, n, B, Hkv, d, num_pages, page_size, max_pages, cache_dtype);
+    if (rc != DD_OK) return rc;
+    if (H < 1 || H % Hkv != 0) return DD_ERR_SHAPE;
+    if (n == 0) return DD_OK;
+    if (!Q || !O) return DD_ERR_NULL;
+    if ((double)B * H * n >= 2147483648.0) return DD_ERR_SHAPE;
+    if (misaligned16(Q) || misaligned16(O)) return DD_ERR_ALIGN;
+    const bool fp8 = cache_dtype == DD_FP8_E4M3;
+    rc = check_workspace(workspace, workspace_bytes, dd::paged_attention_workspace_bytes(n, B, H, Hkv, d, (long)max_pages * page_size, fp8));
+    if (rc != DD_OK) return rc;
+    dd::PagedAttnArgs a;
+    a.Q = Q; a.Kc = Kc; a.Vc = Vc; a.O = O;
+    a.k_scale = fp8 ? k_scale : nullptr; a.v_scale = fp8 ? v_scale : nullptr;
+    a.table = block_table; a.kv_lens = kv_lens;
+    a.n = n; a.B = B; a.H = H; a.Hkv = Hkv; a.d = d; a.num_pages = num_pages; a.max_pages = max_pages; a.page_log2 = page_log2_of(page_size);
+    a.workspace = workspace;
+    const hipError_t e = dd::launch_attention_paged(a, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? DD_OK : DD_ERR_LAUNCH;
+}
+
 size_t dd_verify_remask_workspace_bytes(int B, int G, int V, dd_dtype logit_dtype)
 {
     if (B < 0 || G < 0 || V < 1 || (logit_dtype != DD_F32 && logit_dtype != DD_BF16)) return 0;

@@ -145,6 +145,60 @@ hipError_t launch_attention_solo(const AttnArgs &a, int form, hipStream_t stream
 hipError_t launch_cache_insert_rows(const void *Krows, const void *Vrows, void *Kc, void *Vc, const int32_t *pos,
                                     int n, int B, int Hkv, int N, int d, int k_elem_bytes, int v_elem_bytes,
                                     hipStream_t stream);
+// ---- rows before attention (rows.hip) --------------------------------------------
+// One side, queries or keys, of the norm and rotation of dense rows: x[b, h, i, :] at b * batch + h * head + i * row (elements),
+// y dense [B, heads, n, d].
+struct NormRotateSide {
+    const void *x = nullptr;
+    void *y = nullptr;
+    const void *weight = nullptr;        // [d], the rows' type; nullptr: no norm
+    int heads = 0;
+    long batch = 0, head = 0, row = 0;
+};
+struct NormRotateArgs {
+    NormRotateSide q, k;                 // k.heads == 0: queries only
+    const float *inv_freq = nullptr;     // [rot / 2]
+    const int32_t *positions = nullptr;  // [B, n]; nullptr: 0 .. n - 1
+    unsigned tokens = 0;                 // B * n
+    int n = 0, rot = 0;                  // rot == 0: no rotation
+    bool interleaved = false;
+    float eps = 0;
+    int per_wg = 0, q_groups = 0;        // set by the launcher: heads per workgroup, workgroups (y) that have queries
+};
+hipError_t launch_norm_rotate(NormRotateArgs a, int d, bool bf16, hipStream_t stream);
+
+// Rows [B, Hkv, n, d] (strides as above) into the pages of their sequences: row r of sequence b to position starts[b] + r.
+struct PageAppendSide {
+    const void *x = nullptr;
+    void *cache = nullptr;
+    float *scale = nullptr;              // [pages, Hkv]; e4m3 pages only
+    long batch = 0, head = 0, row = 0;
+};
+struct PageAppendArgs {
+    PageAppendSide k, v;
+    const int32_t *table = nullptr, *starts = nullptr, *kv_lens = nullptr, *n_rows = nullptr;    // the last two may be nullptr
+    const void *weight = nullptr;        // [d] or nullptr: no norm of the keys
+    const float *inv_freq = nullptr;
+    int n = 0, B = 0, Hkv = 0, num_pages = 0, max_pages = 0, page_log2 = 0, rot = 0;
+    bool interleaved = false;
+    float eps = 0;
+    int pages_per_seq = 0, per_wg = 0, head_groups = 0;      // set by the launcher
+};
+long page_append_wgs(int n, int B, int Hkv, int page_log2);  // the most workgroups that a call can take
+hipError_t launch_page_append(PageAppendArgs a, int d, bool rows_bf16, bool fp8, hipStream_t stream);
+
+// ---- attention over a paged cache (attention_paged.hip) ----------------------------
+struct PagedAttnArgs {
+    const void *Q = nullptr, *Kc = nullptr, *Vc = nullptr;
+    const float *k_scale = nullptr, *v_scale = nullptr;      // [pages, Hkv]: e4m3 pages; nullptr: bf16 pages
+    const int32_t *table = nullptr, *kv_lens = nullptr;
+    void *O = nullptr;
+    int n = 0, B = 0, H = 0, Hkv = 0, d = 0, num_pages = 0, max_pages = 0, page_log2 = 0;
+    void *workspace = nullptr;
+};
+size_t paged_attention_workspace_bytes(int n, int B, int H, int Hkv, int d, long capacity, bool fp8);     // capacity: keys of a table row
+hipError_t launch_attention_paged(const PagedAttnArgs &a, hipStream_t stream);
+
 // merge of the partial states (a.splits > 1), carrying the cache refresh on extra workgroups when one is asked for
 hipError_t launch_attention_combine(const AttnArgs &a, hipStream_t stream);
 // what every attention launcher ends with: the merge if the key range was split (`splits_used` > 1),
