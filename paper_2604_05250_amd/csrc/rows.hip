@@ -9,7 +9,9 @@
 // are chosen so that the two members of every pair are in one lane - chunk c and chunk c + rot/2 where halves are paired, neighbours
 // otherwise - so a rotation needs no exchange, and lane c needs the angles 8c .. 8c + 7 in both pairings.
 // Angles: position * inv_freq in revolutions, in fp64, and its fraction to fp32 (a product in fp32 is off by 2^-24 of the angle:
-// a hundredth of a radian at position 130000).  bf16 and e4m3 results take the hardware's sine (off by some 2^-20), fp32 results sinpi.
+// a hundredth of a radian at position 130000).  The hardware's sine and cosine take revolutions and are off by 2^-23 (measured over
+// [0, 1] against fp64).
+#include "attention_common.h"
 #include "dd_internal.h"
 
 #include <type_traits>
@@ -19,12 +21,16 @@ namespace {
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float floatx2 __attribute__((ext_vector_type(2)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ unsigned pack_bf16(float lo, float hi)
 {
     floatx2 f = {lo, hi};
     return __builtin_bit_cast(unsigned, __builtin_convertvector(f, bf16x2));
 }
+// (by value: a bit cast of a vector's element in place takes element 0)
+__device__ __forceinline__ float as_float(unsigned w) { return __builtin_bit_cast(float, w); }
 __device__ __forceinline__ float bf16_lo(unsigned w) { return __builtin_bit_cast(float, w << 16); }
 __device__ __forceinline__ float bf16_hi(unsigned w) { return __builtin_bit_cast(float, w & 0xffff0000u); }
 
@@ -32,43 +38,35 @@ struct Bf16 { static constexpr int bytes = 2; };
 struct F32 { static constexpr int bytes = 4; };
 
 // eight consecutive elements as they are in memory
-template <typename T> struct Chunk { uint4 w[T::bytes / 2]; };
+template <typename T> struct Chunk { u32x4 w[T::bytes / 2]; };
 template <typename T> __device__ __forceinline__ Chunk<T> load_chunk(const uint8_t *row, int element)
 {
     Chunk<T> c;
-    const uint4 *p = reinterpret_cast<const uint4 *>(row + element * T::bytes);
+    const u32x4 *p = reinterpret_cast<const u32x4 *>(row + element * T::bytes);
 #pragma unroll
     for (int i = 0; i < T::bytes / 2; ++i) c.w[i] = p[i];
     return c;
 }
 __device__ __forceinline__ void unpack(const Chunk<Bf16> &c, float *x)
 {
-    const unsigned w[4] = {c.w[0].x, c.w[0].y, c.w[0].z, c.w[0].w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { x[2 * i] = bf16_lo(w[i]); x[2 * i + 1] = bf16_hi(w[i]); }
+    for (int i = 0; i < 4; ++i) { x[2 * i] = bf16_lo(c.w[0][i]); x[2 * i + 1] = bf16_hi(c.w[0][i]); }
 }
 __device__ __forceinline__ void unpack(const Chunk<F32> &c, float *x)
 {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        x[4 * i] = __builtin_bit_cast(float, c.w[i].x); x[4 * i + 1] = __builtin_bit_cast(float, c.w[i].y);
-        x[4 * i + 2] = __builtin_bit_cast(float, c.w[i].z); x[4 * i + 3] = __builtin_bit_cast(float, c.w[i].w);
-    }
+    for (int i = 0; i < 8; ++i) x[i] = as_float(c.w[i / 4][i % 4]);
 }
-__device__ __forceinline__ uint4 pack8_bf16(const float *x)
+template <typename T, bool STREAM> __device__ __forceinline__ void store_chunk(uint8_t *row, int element, const float *x)
 {
-    return make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
-}
-template <typename T> __device__ __forceinline__ void store_chunk(uint8_t *row, int element, const float *x)
-{
-    uint4 *p = reinterpret_cast<uint4 *>(row + element * T::bytes);
-    if constexpr (std::is_same<T, Bf16>::value) {
-        p[0] = pack8_bf16(x);
-    } else {
+    u32x4 *p = reinterpret_cast<u32x4 *>(row + element * T::bytes);
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-            p[i] = make_uint4(__builtin_bit_cast(unsigned, x[4 * i]), __builtin_bit_cast(unsigned, x[4 * i + 1]),
-                              __builtin_bit_cast(unsigned, x[4 * i + 2]), __builtin_bit_cast(unsigned, x[4 * i + 3]));
+    for (int i = 0; i < T::bytes / 2; ++i) {
+        u32x4 v;
+        if constexpr (std::is_same<T, Bf16>::value) v = u32x4{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])};
+        else v = __builtin_bit_cast(u32x4, floatx4{x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]});
+        if constexpr (STREAM) __builtin_nontemporal_store(v, p + i);
+        else p[i] = v;
     }
 }
 
@@ -100,51 +98,47 @@ __device__ __forceinline__ Pairing pairing(int lane, int rot, bool interleaved)
     return p;
 }
 
-// cos and sin of the eight angles of a lane
-template <bool EXACT> __device__ __forceinline__ void turn_of(const double *turns_per_step, long position, float *c, float *s)
+enum { kNoTurn = 0, kHalves = 1, kNeighbours = 2 };
+
+// cos and sin of the eight angles of a lane at a position; a lane whose elements stay as they are gets 1 and 0
+__device__ __forceinline__ void turn_of(const float *inv_freq, int lane, bool turns, double position, float *c, float *s)
+{
+    const double p = position * 0.15915494309189533577;      // 1 / 2 pi
+    const float *const f = inv_freq + (turns ? 8 * lane : 0);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float r = (float)__builtin_amdgcn_fract((double)f[i] * p);             // revolutions
+        c[i] = turns ? __builtin_amdgcn_cosf(r) : 1.0f;
+        s[i] = turns ? __builtin_amdgcn_sinf(r) : 0.0f;
+    }
+}
+template <int PAIR> __device__ __forceinline__ void rotate(float *x, const float *c, const float *s)     // x: both chunks, 16 values
 {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const double r = (double)position * turns_per_step[i];
-        const float f = (float)(r - __builtin_floor(r));     // revolutions, in [0, 1]
-        if constexpr (EXACT) {
-            s[i] = sinpif(2.0f * f);
-            c[i] = cospif(2.0f * f);
-        } else {
-            s[i] = __builtin_amdgcn_sinf(f);
-            c[i] = __builtin_amdgcn_cosf(f);
-        }
+        float &u = PAIR == kHalves ? x[i] : x[2 * i], &v = PAIR == kHalves ? x[8 + i] : x[2 * i + 1];
+        const float u0 = u, v0 = v;
+        u = u0 * c[i] - v0 * s[i];
+        v = v0 * c[i] + u0 * s[i];
     }
 }
-__device__ __forceinline__ void turns_per_step(const float *inv_freq, int lane, double *t)
+// weights of a lane's elements, 1 where there are none; norm() of a row without weights leaves it as it is
+template <typename T> __device__ __forceinline__ void weights_of(const void *weight, const Pairing &p, float *w)
 {
+    if (weight == nullptr) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) t[i] = (double)inv_freq[8 * lane + i] * 0.15915494309189533577;      // 1 / 2 pi
-}
-__device__ __forceinline__ void rotate(float *x, const Pairing &p, const float *c, const float *s)     // x: both chunks, 16 values
-{
-    if (p.halves) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float u = x[i], v = x[8 + i];
-            x[i] = u * c[i] - v * s[i];
-            x[8 + i] = v * c[i] + u * s[i];
-        }
-    } else if (p.turns) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float u = x[2 * i], v = x[2 * i + 1];
-            x[2 * i] = u * c[i] - v * s[i];
-            x[2 * i + 1] = v * c[i] + u * s[i];
-        }
+        for (int i = 0; i < 16; ++i) w[i] = 1.0f;
+        return;
     }
+    unpack(load_chunk<T>(static_cast<const uint8_t *>(weight), p.a), w);
+    unpack(load_chunk<T>(static_cast<const uint8_t *>(weight), p.b), w + 8);
 }
-template <int D> __device__ __forceinline__ void norm(float *x, const float *w, float eps)
+template <int D> __device__ __forceinline__ void norm(float *x, const float *w, float eps, bool normed)
 {
     float q = 0;
 #pragma unroll
     for (int i = 0; i < 16; ++i) q += x[i] * x[i];
-    const float r = 1.0f / sqrtf(row_sum<D / 16>(q) * (1.0f / D) + eps);
+    const float root = __builtin_amdgcn_rsqf(row_sum<D / 16>(q) * (1.0f / D) + eps), r = normed ? root : 1.0f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) x[i] = x[i] * r * w[i];
 }
@@ -152,56 +146,52 @@ template <int D> __device__ __forceinline__ void norm(float *x, const float *w, 
 // ---------------------------------------------------------------- queries and keys for dense attention
 // A lane keeps its place in the row and its token, and goes through `per_wg` heads: the angles and the weights are made once for all
 // of them.  Reads and writes every row once: bound by memory where tokens are many.
-template <typename T, int D>
+// Every load and store of the loop is unconditional (the last heads' prefetch reads the last row again), so that a wave waits for one
+// row's loads and not for all that are on their way.  Stores are non-temporal: 16 x 2048 rows of 40 heads 141 -> 137 us (4.9 TB/s read and
+// written, what a copy reaches), 16 x 64 rows 7.0 -> 6.0; with dd_bidir_attention after it 1 x 1024 rows of 32 + 8 heads 31.3 -> 29.3, 1 x 4096
+// of 32 + 32 224.5 -> 223.7, but 8 x 1024 of 32 + 32 168.5 -> 174.5, where all that is written would have stayed in the last cache.
+template <typename T, int D, bool NORM, int PAIR>
 __global__ __launch_bounds__(256) void norm_rotate_kernel(NormRotateArgs a)
 {
     constexpr int LANES = D / 16, TOKENS = 256 / LANES;
+    constexpr int U = 4 / (T::bytes / 2);                    // heads on their way
     const int lane = threadIdx.x % LANES;
     const unsigned token = blockIdx.x * TOKENS + threadIdx.x / LANES;
-    const bool live = token < a.tokens;
-    const unsigned at = live ? token : a.tokens - 1;
-    const long b = at / (unsigned)a.n, i = at - (unsigned)b * (unsigned)a.n;
+    if (token >= a.tokens) return;                           // (whole rows: the lanes of a row stay together)
+    const unsigned b = token / (unsigned)a.n, i = token - b * (unsigned)a.n;
     const bool is_q = (int)blockIdx.y < a.q_groups;
     const NormRotateSide &side = is_q ? a.q : a.k;
-    const int first = ((int)blockIdx.y - (is_q ? 0 : a.q_groups)) * a.per_wg, last = min(first + a.per_wg, side.heads);
-    const Pairing p = pairing(lane, a.rot, a.interleaved);
+    const int first = ((int)blockIdx.y - (is_q ? 0 : a.q_groups)) * a.per_wg, count = min(a.per_wg, side.heads - first);
+    const Pairing p = pairing(lane, a.rot, PAIR == kNeighbours);
 
-    const uint8_t *src = static_cast<const uint8_t *>(side.x) + (b * side.batch + i * side.row) * T::bytes;
-    uint8_t *dst = static_cast<uint8_t *>(side.y) + ((b * side.heads) * a.n + i) * D * T::bytes;
-    constexpr int U = 2;                                     // heads on their way
+    const uint8_t *src = static_cast<const uint8_t *>(side.x) + ((long)b * side.batch + first * side.head + (long)i * side.row) * T::bytes;
+    uint8_t *dst = static_cast<uint8_t *>(side.y) + (((long)b * side.heads + first) * a.n + i) * D * T::bytes;
     Chunk<T> in[U][2];
     auto fetch = [&](int h, int u) __attribute__((always_inline)) {
-        const uint8_t *row = src + (long)min(h, last - 1) * side.head * T::bytes;
+        const uint8_t *row = src + (long)min(h, count - 1) * side.head * T::bytes;
         in[u][0] = load_chunk<T>(row, p.a);
         in[u][1] = load_chunk<T>(row, p.b);
     };
 #pragma unroll
-    for (int u = 0; u < U; ++u) fetch(first + u, u);
+    for (int u = 0; u < U; ++u) fetch(u, u);
 
     float w[16], c[8], s[8];
-    if (side.weight != nullptr) {
-        unpack(load_chunk<T>(static_cast<const uint8_t *>(side.weight), p.a), w);
-        unpack(load_chunk<T>(static_cast<const uint8_t *>(side.weight), p.b), w + 8);
-    }
-    if (p.turns) {
-        double t[8];
-        turns_per_step(a.inv_freq, lane, t);
-        turn_of<std::is_same<T, F32>::value>(t, a.positions != nullptr ? (long)a.positions[at] : i, c, s);
-    }
-    for (int h0 = first; h0 < last; h0 += U) {
+    if constexpr (NORM) weights_of<T>(side.weight, p, w);
+    if constexpr (PAIR != kNoTurn) turn_of(a.inv_freq, lane, p.turns, a.positions != nullptr ? (double)a.positions[token] : (double)i, c, s);
+    const bool normed = NORM && side.weight != nullptr;
+    for (int h0 = 0; h0 < count; h0 += U) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int h = h0 + u;
             float x[16];
             unpack(in[u][0], x);
             unpack(in[u][1], x + 8);
-            if (h0 + U < last) fetch(h + U, u);
-            if (side.weight != nullptr) norm<D>(x, w, a.eps);
-            rotate(x, p, c, s);
-            if (live && h < last) {
-                uint8_t *row = dst + (long)h * a.n * D * T::bytes;
-                store_chunk<T>(row, p.a, x);
-                store_chunk<T>(row, p.b, x + 8);
+            fetch(h0 + U + u, u);
+            if constexpr (NORM) norm<D>(x, w, a.eps, normed);
+            if constexpr (PAIR != kNoTurn) rotate<PAIR>(x, c, s);
+            if (h0 + u < count) {
+                uint8_t *row = dst + (long)(h0 + u) * a.n * D * T::bytes;
+                store_chunk<T, true>(row, p.a, x);
+                store_chunk<T, true>(row, p.b, x + 8);
             }
         }
     }
@@ -225,6 +215,18 @@ __device__ __forceinline__ float scale_for(float a)
     const int e = (int)(bits >> 23) - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0);  // its biased exponent
     return __builtin_bit_cast(float, (unsigned)(e < 1 ? 1 : e) << 23);
 }
+__device__ __forceinline__ float wave_largest(float x)       // over the 64 lanes of a wave
+{
+    typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+    x = fmaxf(x, across<0xB1>(x));
+    x = fmaxf(x, across<0x4E>(x));
+    x = fmaxf(x, across<0x141>(x));
+    x = fmaxf(x, across<0x140>(x));                          // mirrored within sixteen lanes
+    u32x2 r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
+    x = fmaxf(as_float(r[0]), as_float(r[1]));
+    r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
+    return fmaxf(as_float(r[0]), as_float(r[1]));
+}
 struct Divide {                                              // x / s, by a product where that is the same number
     float s, inverse;
     bool exact;
@@ -243,78 +245,93 @@ struct Divide {                                              // x / s, by a prod
 
 // One workgroup has one page of one sequence, its keys or its values, for `per_wg` heads one after the other, and one row of the page
 // per d / 16 lanes.  It is the only one that writes this page and these heads, so the page's scale, its old rows and its new ones are
-// decided here without an atomic.  The rows stay in registers between the maximum over the page and their storage.
+// decided here without an atomic.  The rows stay in registers between the maximum over the page and their storage; the next head's are
+// on their way meanwhile, and its angles and weights are this one's.
 // Values are stored with the keys of one head dim side by side, and are turned over in LDS.
-template <typename T, int D, int PAGE, bool FP8>
-__global__ __launch_bounds__(PAGE *D / 16) void page_append_kernel(PageAppendArgs a)
+// Bound by memory: 16 x 2048 rows of 8 heads to e4m3 pages of 64 42 us, 4.8 TB/s read and written.
+template <typename T, int D, int PAGE, bool FP8, bool VALUES>
+__device__ __forceinline__ void append_page(const PageAppendArgs &a, unsigned bid, unsigned *turned, float *wave_max)
 {
-    constexpr int LANES = D / 16, THREADS = PAGE * LANES, WAVES = (THREADS + 63) / 64;
+    constexpr int LANES = D / 16, WAVES = (PAGE * LANES + 63) / 64;
     constexpr int EB = FP8 ? 1 : 2;                          // bytes per stored element
-    constexpr int PITCH = D * EB + 4;                        // bytes per row in LDS: an odd number of words
-    __shared__ unsigned turned[PAGE * PITCH / 4];
-    __shared__ float wave_max[2][WAVES];
-
+    constexpr int PITCH = D * EB / 4 + 1;                    // words per row in LDS: an odd number
+    constexpr int KEYS = 16 / EB, DIMS = 4 / EB;             // a thread stores KEYS values of DIMS head dims
     const int tid = threadIdx.x, lane = tid % LANES, slot = tid / LANES;
-    unsigned bid = blockIdx.x;
-    const bool values = bid & 1;
-    bid >>= 1;
     const int group = bid % a.head_groups;
     bid /= a.head_groups;
     const int b = bid / a.pages_per_seq, j = bid % a.pages_per_seq;
 
     // ---- which rows of the page this call writes, and which it finds there
-    const long start = a.starts[b];
-    const long rows = a.n_rows != nullptr ? min(max(a.n_rows[b], 0), a.n) : a.n;
-    const long held = a.kv_lens != nullptr ? (long)a.kv_lens[b] : start;
+    const long start = uniform_load(a.starts + b);
+    const long rows = a.n_rows != nullptr ? min(max(uniform_load(a.n_rows + b), 0), a.n) : a.n;
+    const long held = a.kv_lens != nullptr ? (long)uniform_load(a.kv_lens + b) : start;
     const long page_index = (start >> a.page_log2) + j, first = page_index * PAGE;       // first: position of the page's first row
     if (page_index < 0 || page_index >= a.max_pages) return;
     if (first >= start + rows || rows == 0) return;          // (first + PAGE > start: j >= 0)
-    const int page = a.table[(long)b * a.max_pages + page_index];
+    const int page = uniform_load(a.table + (long)b * a.max_pages + page_index);
     if (page < 0 || page >= a.num_pages) return;
     const long pos = first + slot;
     const bool written = pos >= start && pos < start + rows;
     const bool kept = !written && pos < held;
     const bool keeps = min(start, held) > first || min(held, first + PAGE) > start + rows;       // some row is kept
 
-    Pairing p = pairing(lane, values ? 0 : a.rot, a.interleaved);
-    const PageAppendSide &side = values ? a.v : a.k;
+    const Pairing p = pairing(lane, VALUES ? 0 : a.rot, a.interleaved);
+    const PageAppendSide &side = VALUES ? a.v : a.k;
     const long r = written ? pos - start : (start > first ? 0 : first - start);          // (a row that exists)
     const uint8_t *src = static_cast<const uint8_t *>(side.x) + (b * side.batch + r * side.row) * T::bytes;
+    const int g_begin = group * a.per_wg, g_end = min(g_begin + a.per_wg, a.Hkv);
+    Chunk<T> in[2];
+    auto fetch = [&](int g) __attribute__((always_inline)) {
+        const uint8_t *row = src + (long)g * side.head * T::bytes;
+        in[0] = load_chunk<T>(row, p.a);
+        in[1] = load_chunk<T>(row, p.b);
+    };
+    fetch(g_begin);
     float w[16], c[8], s[8];
-    if (!values) {
-        if (a.weight != nullptr) {
-            unpack(load_chunk<T>(static_cast<const uint8_t *>(a.weight), p.a), w);
-            unpack(load_chunk<T>(static_cast<const uint8_t *>(a.weight), p.b), w + 8);
-        }
-        if (p.turns) {
-            double t[8];
-            turns_per_step(a.inv_freq, lane, t);
-            turn_of<false>(t, pos, c, s);
-        }
+    const bool normed = a.weight != nullptr, turns = a.rot > 0;
+    if constexpr (!VALUES) {
+        weights_of<T>(a.weight, p, w);
+        if (turns) turn_of(a.inv_freq, lane, p.turns, (double)pos, c, s);
     }
-    const int g_end = min((group + 1) * a.per_wg, a.Hkv);
-    for (int g = group * a.per_wg, turn = 0; g < g_end; ++g, turn ^= 1) {
-        float x[16];
-        unpack(load_chunk<T>(src + (long)g * side.head * T::bytes, p.a), x);
-        unpack(load_chunk<T>(src + (long)g * side.head * T::bytes, p.b), x + 8);
-        if (!values) {
-            if (a.weight != nullptr) norm<D>(x, w, a.eps);
-            rotate(x, p, c, s);
-        }
+
+    // the keys and head dims of values that this thread stores
+    const int k0 = tid % (PAGE / KEYS) * KEYS, dw = tid / (PAGE / KEYS);                 // first key, word of a row in LDS
+    const long at0 = first + k0;
+    const bool stores = dw < D / DIMS;
+    const bool all = at0 >= start && at0 + KEYS <= start + rows, some = at0 < start + rows && at0 + KEYS > start;
+
+    for (int g = g_begin, turn = 0; g < g_end; ++g, turn ^= 1) {
         const long at = (long)page * a.Hkv + g;              // page and head
         uint8_t *const store = static_cast<uint8_t *>(side.cache) + at * PAGE * D * EB;
+        auto place = [&](int q) __attribute__((always_inline)) { return reinterpret_cast<u32x4 *>(store + ((long)(dw * DIMS + q) * PAGE + k0) * EB); };
+        u32x4 was[DIMS];                                     // vectors of which only some keys are written
+        if (VALUES && stores && some && !all) {
+#pragma unroll
+            for (int q = 0; q < DIMS; ++q) was[q] = *place(q);
+        }
+        float old = 0.0f;
+        if (FP8 && keeps) old = side.scale[at];
+        float x[16];
+        unpack(in[0], x);
+        unpack(in[1], x + 8);
+        fetch(min(g + 1, g_end - 1));
+        if constexpr (!VALUES) {
+            if (normed) norm<D>(x, w, a.eps, true);
+            if (turns) {
+                if (a.interleaved) rotate<kNeighbours>(x, c, s);
+                else rotate<kHalves>(x, c, s);
+            }
+        }
         float by = 1.0f;                                     // kept codes: their old scale over the new one
         if constexpr (FP8) {
             float m = 0;
-            if (written) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) m = fmaxf(m, fabsf(x[i]));
-            }
-            for (int k = 32; k; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
-            if ((tid & 63) == 0) wave_max[turn][tid >> 6] = m;
-            const float old = keeps ? side.scale[at] : 0.0f;
+            for (int i = 0; i < 16; ++i) m = fmaxf(m, fabsf(x[i]));
+            m = wave_largest(written ? m : 0.0f);
+            if ((tid & 63) == 0) wave_max[turn * WAVES + (tid >> 6)] = m;
             __syncthreads();
-            for (int k = 0; k < WAVES; ++k) m = fmaxf(m, wave_max[turn][k]);
+#pragma unroll
+            for (int k = 0; k < WAVES; ++k) m = fmaxf(m, wave_max[turn * WAVES + k]);
             float scale = scale_for(m);
             if (keeps) {
                 scale = fmaxf(scale, old);
@@ -324,7 +341,7 @@ __global__ __launch_bounds__(PAGE *D / 16) void page_append_kernel(PageAppendArg
             const Divide divide(scale);
             divide(x);
         }
-        if (!values) {
+        if constexpr (!VALUES) {
             uint8_t *const row = store + (long)slot * D * EB;
             if constexpr (FP8) {
                 uint2 *const pa = reinterpret_cast<uint2 *>(row + p.a), *const pb = reinterpret_cast<uint2 *>(row + p.b);
@@ -337,67 +354,72 @@ __global__ __launch_bounds__(PAGE *D / 16) void page_append_kernel(PageAppendArg
                     *pb = make_uint2(regrown4(cb.x, by), regrown4(cb.y, by));
                 }
             } else if (written) {
-                store_chunk<Bf16>(row, p.a, x);
-                store_chunk<Bf16>(row, p.b, x + 8);
+                store_chunk<Bf16, false>(row, p.a, x);
+                store_chunk<Bf16, false>(row, p.b, x + 8);
             }
-            continue;
-        }
-        // ---- values: rows into LDS, then for four head dims the sixteen (bf16: two head dims, the eight) keys of a vector
-        unsigned *const mine = turned + slot * (PITCH / 4) + lane * (4 * EB);
-        if constexpr (FP8) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) mine[i] = codes4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
         } else {
+            // ---- values: rows into LDS, and out by words of the rows, four (bf16: two) head dims of one key
+            unsigned *const mine = turned + slot * PITCH + lane * (4 * EB);
+            if constexpr (FP8) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) mine[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
-        }
-        __syncthreads();
-        constexpr int KEYS = 16 / EB, DIMS = 4 / EB, UNITS = (PAGE / KEYS) * (D / DIMS);
-        for (int u = tid; u < UNITS; u += THREADS) {
-            const int k0 = (u % (PAGE / KEYS)) * KEYS, dw = u / (PAGE / KEYS);           // first key, word of the row
-            const long at0 = first + k0;
-            const bool all = at0 >= start && at0 + KEYS <= start + rows;
-            const bool some = at0 < start + rows && at0 + KEYS > start;
-            if (!some && by == 1.0f) continue;
-            unsigned in[KEYS];
+                for (int i = 0; i < 4; ++i) mine[i] = codes4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+            } else {
 #pragma unroll
-            for (int k = 0; k < KEYS; ++k) in[k] = turned[(k0 + k) * (PITCH / 4) + dw];
+                for (int i = 0; i < 8; ++i) mine[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
+            }
+            __syncthreads();
+            if (stores && (some || by != 1.0f)) {
+                unsigned in_row[KEYS];
 #pragma unroll
-            for (int q = 0; q < DIMS; ++q) {
-                unsigned out[4];
+                for (int k = 0; k < KEYS; ++k) in_row[k] = turned[(k0 + k) * PITCH + dw];
+                if (!some) {
 #pragma unroll
-                for (int o = 0; o < 4; ++o) {
-                    if constexpr (FP8) {
-                        const unsigned lo = __builtin_amdgcn_perm(in[4 * o + 1], in[4 * o], 0x0c0c0000u | (unsigned)(q | (q + 4) << 8));
-                        const unsigned hi = __builtin_amdgcn_perm(in[4 * o + 3], in[4 * o + 2], 0x0c0c0000u | (unsigned)(q | (q + 4) << 8));
-                        out[o] = lo | hi << 16;
-                    } else {
-                        out[o] = __builtin_amdgcn_perm(in[2 * o + 1], in[2 * o], q ? 0x07060302u : 0x05040100u);
-                    }
+                    for (int q = 0; q < DIMS; ++q) was[q] = *place(q);
                 }
-                uint4 *const to = reinterpret_cast<uint4 *>(store + ((long)(dw * DIMS + q) * PAGE + k0) * EB);
-                if (!all) {                                  // the other keys of the vector: kept codes in the new scale, the rest as it was
-                    const uint4 was = *to;
-                    const unsigned old[4] = {was.x, was.y, was.z, was.w};
+#pragma unroll
+                for (int q = 0; q < DIMS; ++q) {
+                    u32x4 out;
 #pragma unroll
                     for (int o = 0; o < 4; ++o) {
-                        unsigned grown = old[o], is_new = 0, is_kept = 0;
-                        if constexpr (FP8) grown = by != 1.0f ? regrown4(old[o], by) : old[o];
-#pragma unroll
-                        for (int e = 0; e < KEYS / 4; ++e) {
-                            const long at1 = at0 + o * (KEYS / 4) + e;
-                            const unsigned field = (FP8 ? 0xffu : 0xffffu) << (e * 8 * EB);
-                            if (at1 >= start && at1 < start + rows) is_new |= field;
-                            else if (at1 < held) is_kept |= field;
+                        if constexpr (FP8) {
+                            const unsigned lo = __builtin_amdgcn_perm(in_row[4 * o + 1], in_row[4 * o], 0x0c0c0000u | (unsigned)(q | (q + 4) << 8));
+                            const unsigned hi = __builtin_amdgcn_perm(in_row[4 * o + 3], in_row[4 * o + 2], 0x0c0c0000u | (unsigned)(q | (q + 4) << 8));
+                            out[o] = lo | hi << 16;
+                        } else {
+                            out[o] = __builtin_amdgcn_perm(in_row[2 * o + 1], in_row[2 * o], q ? 0x07060302u : 0x05040100u);
                         }
-                        out[o] = (out[o] & is_new) | (grown & is_kept) | (old[o] & ~(is_new | is_kept));
                     }
+                    if (!all) {                              // the other keys of the vector: kept codes in the new scale, the rest as it was
+#pragma unroll
+                        for (int o = 0; o < 4; ++o) {
+                            unsigned grown = was[q][o], is_new = 0, is_kept = 0;
+                            if constexpr (FP8) grown = by != 1.0f ? regrown4(was[q][o], by) : was[q][o];
+#pragma unroll
+                            for (int e = 0; e < KEYS / 4; ++e) {
+                                const long at1 = at0 + o * (KEYS / 4) + e;
+                                const unsigned field = (FP8 ? 0xffu : 0xffffu) << (e * 8 * EB);
+                                if (at1 >= start && at1 < start + rows) is_new |= field;
+                                else if (at1 < held) is_kept |= field;
+                            }
+                            out[o] = (out[o] & is_new) | (grown & is_kept) | (was[q][o] & ~(is_new | is_kept));
+                        }
+                    }
+                    *place(q) = out;
                 }
-                *to = make_uint4(out[0], out[1], out[2], out[3]);
             }
+            if (g + 1 < g_end) __syncthreads();
         }
-        __syncthreads();
     }
+}
+
+template <typename T, int D, int PAGE, bool FP8>
+__global__ __launch_bounds__(PAGE *D / 16) void page_append_kernel(PageAppendArgs a)
+{
+    constexpr int EB = FP8 ? 1 : 2, WAVES = (PAGE * D / 16 + 63) / 64;
+    __shared__ unsigned turned[PAGE * (D * EB / 4 + 1)];
+    __shared__ float wave_max[2 * WAVES];
+    if (blockIdx.x & 1) append_page<T, D, PAGE, FP8, true>(a, blockIdx.x >> 1, turned, wave_max);
+    else append_page<T, D, PAGE, FP8, false>(a, blockIdx.x >> 1, turned, wave_max);
 }
 
 template <typename T, int D, int PAGE>
@@ -416,6 +438,18 @@ template <typename T, int D> hipError_t append_rows(const PageAppendArgs &a, boo
     }
 }
 
+template <typename T, int D> hipError_t norm_rotate(const NormRotateArgs &a, dim3 grid, hipStream_t stream)
+{
+    const int pair = a.rot == 0 ? kNoTurn : a.interleaved ? kNeighbours : kHalves;
+    if (a.q.weight != nullptr || a.k.weight != nullptr)
+        return pair == kNoTurn ? launch(norm_rotate_kernel<T, D, true, kNoTurn>, grid, dim3(256), stream, a)
+             : pair == kHalves ? launch(norm_rotate_kernel<T, D, true, kHalves>, grid, dim3(256), stream, a)
+                               : launch(norm_rotate_kernel<T, D, true, kNeighbours>, grid, dim3(256), stream, a);
+    return pair == kNoTurn ? launch(norm_rotate_kernel<T, D, false, kNoTurn>, grid, dim3(256), stream, a)
+         : pair == kHalves ? launch(norm_rotate_kernel<T, D, false, kHalves>, grid, dim3(256), stream, a)
+                           : launch(norm_rotate_kernel<T, D, false, kNeighbours>, grid, dim3(256), stream, a);
+}
+
 }  // namespace
 
 hipError_t launch_norm_rotate(NormRotateArgs a, int d, bool bf16, hipStream_t stream)
@@ -423,15 +457,16 @@ hipError_t launch_norm_rotate(NormRotateArgs a, int d, bool bf16, hipStream_t st
     const int per_wg_tokens = 256 / (d / 16);
     const long tiles = ((long)a.tokens + per_wg_tokens - 1) / per_wg_tokens;
     const int heads = a.q.heads + a.k.heads;
-    // heads per workgroup: as many as leave eight workgroups per compute unit
-    long groups = (2048 + tiles - 1) / tiles;
+    // Heads per workgroup: as many as leave two workgroups per compute unit, as each makes the angles of its tokens once.  us at 512 / 2048
+    // workgroups: 16 x 64 rows of 40 heads 6.0 / 7.2, 3 x 700 rows of 32 heads in fp32 14.7 / 17.3, 16 x 2048 rows of 40 heads the same.
+    long groups = (512 + tiles - 1) / tiles;
     if (groups > heads) groups = heads;
     a.per_wg = (int)((heads + groups - 1) / groups);
     a.q_groups = (a.q.heads + a.per_wg - 1) / a.per_wg;
     const int k_groups = (a.k.heads + a.per_wg - 1) / a.per_wg;
     const dim3 grid((unsigned)tiles, (unsigned)(a.q_groups + k_groups));
-    if (bf16) return d == 128 ? launch(norm_rotate_kernel<Bf16, 128>, grid, dim3(256), stream, a) : launch(norm_rotate_kernel<Bf16, 64>, grid, dim3(256), stream, a);
-    return d == 128 ? launch(norm_rotate_kernel<F32, 128>, grid, dim3(256), stream, a) : launch(norm_rotate_kernel<F32, 64>, grid, dim3(256), stream, a);
+    if (bf16) return d == 128 ? norm_rotate<Bf16, 128>(a, grid, stream) : norm_rotate<Bf16, 64>(a, grid, stream);
+    return d == 128 ? norm_rotate<F32, 128>(a, grid, stream) : norm_rotate<F32, 64>(a, grid, stream);
 }
 
 long page_append_wgs(int n, int B, int Hkv, int page_log2)
@@ -444,7 +479,11 @@ hipError_t launch_page_append(PageAppendArgs a, int d, bool rows_bf16, bool fp8,
 {
     const long page = 1L << a.page_log2;
     a.pages_per_seq = (int)((a.n + page - 2) / page + 1);    // that n rows can touch, wherever they begin
-    a.per_wg = 1;
+    // Heads per workgroup: as many as leave two thousand threads per compute unit, what fits there; more workgroups make the angles and
+    // look up the page once more each.  us at one head / all heads / this: 16 x 2048 rows, 8 heads, e4m3 67 / 42 / 42, 4096 rows, 32 heads,
+    // bf16 pages of 16 32 / 33 / 31; 16 rows of one token 5.0 whatever it is.
+    const long threads = 2L * a.B * a.pages_per_seq * a.Hkv * (page * d / 16), per = threads / (256 * 2048);
+    a.per_wg = per < 1 ? 1 : per > a.Hkv ? a.Hkv : (int)per;
     a.head_groups = (a.Hkv + a.per_wg - 1) / a.per_wg;
     const unsigned wgs = (unsigned)(2L * a.B * a.pages_per_seq * a.head_groups);
     if (rows_bf16) return d == 128 ? append_rows<Bf16, 128>(a, fp8, wgs, stream) : append_rows<Bf16, 64>(a, fp8, wgs, stream);
