@@ -313,7 +313,7 @@ int dd_qk_norm_rope(const void *Q, int64_t q_batch, int64_t q_head, int64_t q_ro
  * The pages that a call writes must be distinct over the sequences (else which rows and which scale win is unspecified);
  * pages that are only read later (a shared prefix) may be shared.  K and V must not overlap the cache (not checked).  The
  * caller owns kv_lens: the call does not write it.
- * d in {64, 128}; B, Hkv, num_pages, max_pages >= 1; n >= 0 (0: a no-op); max_pages*page_size < 2^31, num_pages*Hkv*page_size*d < 2^40.
+ * d in {64, 128}; B, Hkv, num_pages, max_pages >= 1; n >= 0 (0: a no-op); max_pages*page_size < 2^30, num_pages*Hkv*page_size*d < 2^40.
  * Errors: DD_ERR_NULL (scales are required with DD_FP8_E4M3), DD_ERR_SHAPE, DD_ERR_DTYPE, DD_ERR_ALIGN, DD_ERR_LAUNCH.
  */
 int dd_paged_cache_append(void *Kc, void *Vc, float *k_scale, float *v_scale,
@@ -337,7 +337,7 @@ int dd_paged_cache_append(void *Kc, void *Vc, float *k_scale, float *v_scale,
  * online softmax, weights (times v_scale) rounded to bf16 before the PV product.
  * The key range is split over workgroups where those are few; the partial states live in `workspace`.  A capacity
  * max_pages*page_size far above the lengths costs workspace, not time: a sequence's own keys are shared out.
- * d in {64, 128}; H % Hkv == 0; B, H, Hkv, num_pages, max_pages >= 1; n >= 0 (0: a no-op); sizes as above, B*H*n < 2^31.
+ * d in {64, 128}; H % Hkv == 0; B, H, Hkv, num_pages, max_pages >= 1; n >= 0 (0: a no-op); sizes as above, B*H*n < 2^30.
  */
 int dd_paged_attention(const void *Q, const void *Kc, const void *Vc, const float *k_scale, const float *v_scale,
                        const int32_t *block_table, const int32_t *kv_lens, void *O,

@@ -12,12 +12,16 @@
 // sequences x 64 rows, 32/8 heads, 2048 e4m3 keys 51 us, with all loads from the nearest cache 50, with none 37; by LDS 43).
 // A workgroup's four waves are one row block x 4 streams of keys, each with a state (reference, sum, O) of its own and a tile of its
 // own in LDS, whose K is asked for again as soon as it is in registers, and V likewise; or two blocks x 2 streams with doubled tiles
-// that two waves share.  The states are merged through LDS, the key range is split over workgroups where those are few, and the
+// that two waves share.  The next tile's scores are computed beside this one's weights, so that the matrix cores and the vector units
+// have work at the same time.  The states are merged through LDS, the key range is split over workgroups where those are few, and the
 // splits' states are merged by a second kernel.
-// e4m3 codes become bf16 exactly in registers; k_scale goes into the factor of the exponent, v_scale onto the weights before they are
-// rounded to bf16 (bf16 for its range: scales span 2^-126 .. 2^119).
+// e4m3 codes become bf16 exactly in registers.  k_scale goes into the factor of the exponent; of v_scale the power of two goes into the
+// decoding of V, which is exact (bf16 for its range: scales span 2^-126 .. 2^119), and the rest, 1 where this library made the scale,
+// into the exponent.  Weights are rounded to bf16 (2^-8 of each at most, as the result is), their sum is the one of the rounded ones.
 #include "attention_common.h"
 #include "dd_internal.h"
+
+#include <type_traits>
 
 namespace dd {
 namespace {
@@ -26,60 +30,65 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef float floatx2 __attribute__((ext_vector_type(2)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef short short4v __attribute__((ext_vector_type(4)));
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kNone = -1.0e30f;        // the reference of a row that has met no key
-[[maybe_unused]] constexpr float kRaise = 4096.0f;        // a reference is raised when a lane's weights of a tile add up to more
+[[maybe_unused]] constexpr float kMargin = 7.0f;          // a reference is set this far above a tile's maximum (log2 units)
 constexpr int kMaxSplits = 64;
+[[maybe_unused]] constexpr int kWaves = 4;
+constexpr int kSplitTiles = 4;           // tiles of 64 keys that a split has at least
 
 __device__ __forceinline__ unsigned pack_bf16(float lo, float hi)
 {
     floatx2 f = {lo, hi};
     return __builtin_bit_cast(unsigned, __builtin_convertvector(f, bf16x2));
 }
-__device__ __forceinline__ bf16x8 decode8(unsigned w0, unsigned w1)                  // eight e4m3 codes, exactly
+// eight e4m3 codes times the power of two in `scale` (the instruction takes no more of it), exactly
+__device__ __forceinline__ bf16x8 decode8(unsigned w0, unsigned w1, float scale)
 {
-    const u32x4 r = {__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, 1.0f, false)),
-                     __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, 1.0f, true)),
-                     __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, 1.0f, false)),
-                     __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, 1.0f, true))};
+    const u32x4 r = {__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, scale, false)),
+                     __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, scale, true)),
+                     __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, scale, false)),
+                     __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, scale, true))};
     return __builtin_bit_cast(bf16x8, r);
 }
 // fragment `f` (eight elements) of a lane's consecutive elements
-template <bool FP8> __device__ __forceinline__ bf16x8 fragment(const u32x4 *raw, int f)
+template <bool FP8> __device__ __forceinline__ bf16x8 fragment(const u32x4 *raw, int f, float scale)
 {
-    if constexpr (FP8) return decode8(raw[f / 2][(f % 2) * 2], raw[f / 2][(f % 2) * 2 + 1]);
+    if constexpr (FP8) return decode8(raw[f / 2][(f % 2) * 2], raw[f / 2][(f % 2) * 2 + 1], scale);
     else return __builtin_bit_cast(bf16x8, raw[f]);
 }
 // across the two halves of a wave
 __device__ __forceinline__ float as_float(unsigned w) { return __builtin_bit_cast(float, w); }       // (by value: in place it takes a vector's element 0)
 __device__ __forceinline__ float halves_max(float x)
 {
-    typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
     const u32x2 r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
     return fmaxf(as_float(r[0]), as_float(r[1]));
 }
 __device__ __forceinline__ float halves_other(float x) { return __shfl_xor(x, 32); }
 
-struct PagedKernelArgs {
-    const uint8_t *Q, *Kc, *Vc;
-    const int32_t *table, *kv_lens;
+// What the first loads need is in registers when a wave starts, as leading scalar arguments (fourteen words); the rest arrives meanwhile.
+struct PagedTail {
+    const uint8_t *Q;
     const float *k_scale, *v_scale;
     uint8_t *O;
     float *part_o, *part_ml;             // [rows][splits][d], [rows][splits][2]
-    int Hkv, rows_total, num_pages, max_pages, page_log2, row_tiles, splits, wgs;
     float scale_log2;                    // log2(e) / sqrt(d)
 };
+#define DD_PAGED_HEAD const int32_t *table, const int32_t *kv_lens, const uint8_t *Kc, const uint8_t *Vc, int Hkv, int rows_total, int num_pages, \
+                      int max_pages, unsigned wgs, unsigned shape      // shape: row tiles, splits - 1 (6 bits), log2(page_size / 16) (2 bits)
 
 // How a sequence's tiles are shared out over the splits of a call: tiles per split and splits that have any.
 struct Share { int tiles, per_split, used, len; };
 __device__ __forceinline__ Share share_of(int len, int max_pages, int page_log2, int splits)
 {
     Share s;
-    const long most = (long)max_pages << page_log2;
-    s.len = len < 0 ? 0 : (long)len > most ? (int)most : len;
+    s.len = min(max(len, 0), max_pages << page_log2);        // (less than 2^30)
     s.tiles = (int)(((unsigned)s.len + 63u) >> 6);
-    s.per_split = (s.tiles + splits - 1) / splits;
+    s.per_split = max((s.tiles + splits - 1) / splits, kSplitTiles);
     s.used = s.tiles == 0 ? 0 : (s.tiles + s.per_split - 1) / s.per_split;
     return s;
 }
@@ -99,19 +108,19 @@ template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_
 // NT: score tiles of 32 keys, 32 NT keys at a time.  ONE: those lie in one page (page_size >= 32 NT).  RG: row blocks of 32 per
 // workgroup; its four waves are RG blocks x 4 / RG streams of keys.
 template <int D, bool FP8, int NT, bool ONE, int RG>
-__global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedKernelArgs a)
+__global__ __launch_bounds__(256, 2) void attn_paged_kernel(DD_PAGED_HEAD, PagedTail a)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     constexpr int EB = FP8 ? 1 : 2;
     constexpr int ROWB = D * EB, CH = ROWB / 16;     // bytes and 16-byte pieces per key
     constexpr int KR = CH / 2;                       // pieces of a lane's half of a key
     constexpr int DT = D / 32, KS = D / 16;          // head-dim tiles, k steps of S
-    constexpr int TILE = 32 * NT, STREAMS = 4 / RG, UNITS = 2 * NT;
+    constexpr int TILE = 32 * NT, STREAMS = kWaves / RG, UNITS = 2 * NT;
     constexpr int KB = TILE * ROWB, VB = D * TILE * EB, NK = KB / 1024, NV = VB / 1024;      // a tile in LDS: bytes and wave-wide loads
     constexpr int KPI = 1024 / ROWB;                 // keys per load
     constexpr int BUFS = RG == 1 ? 1 : 2;            // a wave's own tile is asked for piece by piece as it is used up; a shared one is doubled
     constexpr int PITCH = D + 4;
-    constexpr int KVB = STREAMS * BUFS * (KB + VB), MERGEB = STREAMS == 1 ? 0 : 4 * 32 * PITCH * 4;
+    constexpr int KVB = STREAMS * BUFS * (KB + VB), MERGEB = STREAMS == 1 ? 0 : kWaves * 32 * PITCH * 4;
     static_assert(TILE * EB == 64, "a head dim's keys of a tile are four pieces");
     static_assert(NK % RG == 0 && NV % RG == 0, "the waves of a stream share its loads out");
     __shared__ __attribute__((aligned(1024))) uint8_t lds[KVB > MERGEB ? KVB : MERGEB];
@@ -119,51 +128,64 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedKernelArgs a)
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int block = wave % RG, stream = wave / RG;
+    const int P_log2 = 4 + (int)(shape & 3), splits = (int)(shape >> 2 & 63) + 1;
     unsigned bid = blockIdx.x;
     {                                                // workgroups that share keys: on one XCD
-        const unsigned total = a.wgs, per = total >> 3, rem = total & 7;
+        const unsigned per = wgs >> 3, rem = wgs & 7;
         const unsigned xcd = bid & 7, slot = bid >> 3;
         bid = xcd * per + min(xcd, rem) + slot;
     }
     int rt, sp;
-    place_of(bid, a.row_tiles, rt);
-    place_of(bid, a.splits, sp);
-    const int head = bid, b = head / a.Hkv, g = head - b * a.Hkv;
-    const Share sh = share_of(uniform_load(a.kv_lens + b), a.max_pages, a.page_log2, a.splits);
+    place_of(bid, shape >> 8, rt);
+    place_of(bid, splits, sp);
+    const unsigned head = bid, b = head / (unsigned)Hkv, g = head - b * (unsigned)Hkv;
+    const int32_t *const row_of_table = table + (size_t)b * max_pages;
+    const unsigned in_page = (1u << P_log2) - 1;
+    constexpr int IDS = ONE ? 1 : UNITS;             // pages: of the tile, or of each unit of 16 keys
+    struct Pages { int id[IDS]; };
+    auto pages_of = [&](int tile) __attribute__((always_inline)) {
+        Pages p;
+#pragma unroll
+        for (int u = 0; u < IDS; ++u) p.id[u] = uniform_load(row_of_table + min((tile * TILE + 16 * u) >> P_log2, max_pages - 1));
+        return p;
+    };
+    const int held = uniform_load(kv_lens + b);
+    Pages now, next, after;
+    if (splits == 1) {                               // (not after the length: the pages are known without it)
+        now = pages_of(stream);
+        next = pages_of(stream + STREAMS);
+        after = pages_of(stream + 2 * STREAMS);
+    }
+    const Share sh = share_of(held, max_pages, P_log2, splits);
     if (sp >= sh.used && sp > 0) return;
     const int v_first = (rt * RG + block) * 32;
-    const size_t row_base = (size_t)head * a.rows_total;
+    const size_t row_base = (size_t)head * rows_total;
+    const int t_begin = sp * sh.per_split * (2 / NT), t_end = min(t_begin + sh.per_split * (2 / NT), (sh.len + TILE - 1) / TILE);
+    const int mine = t_begin + stream;
+    if (splits > 1) {
+        now = pages_of(mine);
+        next = pages_of(mine + STREAMS);
+        after = pages_of(mine + 2 * STREAMS);
+    }
 
     // ---- queries: of row l32 of the block, half of the head dims
     bf16x8 q[KS];
     {
-        const int r = min(v_first + l32, a.rows_total - 1);
+        const int r = min(v_first + l32, rows_total - 1);
         const u32x4 *p = reinterpret_cast<const u32x4 *>(a.Q + (row_base + r) * (D * 2) + hh * D);
 #pragma unroll
         for (int s = 0; s < KS; ++s) q[s] = __builtin_bit_cast(bf16x8, p[s]);
     }
 
-    const int t_begin = sp * sh.per_split * (2 / NT), t_end = min(t_begin + sh.per_split * (2 / NT), (sh.len + TILE - 1) / TILE);
-    const int32_t *const row_of_table = a.table + (size_t)b * a.max_pages;
-    const int P_log2 = a.page_log2;
-    const unsigned in_page = (1u << P_log2) - 1;
-
-    // ---- pages: of each unit of 16 keys, or of the tile
-    constexpr int IDS = ONE ? 1 : UNITS;
-    struct Pages { int id[IDS]; };
-    auto pages_of = [&](int tile) __attribute__((always_inline)) {
-        Pages p;
-#pragma unroll
-        for (int u = 0; u < IDS; ++u) p.id[u] = uniform_load(row_of_table + min((tile * TILE + 16 * u) >> P_log2, a.max_pages - 1));
-        return p;
-    };
-    auto valid = [&](int id) __attribute__((always_inline)) { return (unsigned)id < (unsigned)a.num_pages; };
-    auto place = [&](int id) __attribute__((always_inline)) { return (size_t)((valid(id) ? id : 0) * (long)a.Hkv + g); };      // page and head
+    // every stream takes as many tiles; those behind the split's last key are masked whole
+    const int rounds = (t_end - t_begin + STREAMS - 1) / STREAMS, key_end = min(sh.len, t_end * TILE);
+    auto valid = [&](int id) __attribute__((always_inline)) { return (unsigned)id < (unsigned)num_pages; };
+    auto place = [&](int id) __attribute__((always_inline)) { return (size_t)((valid(id) ? id : 0) * (long)Hkv + g); };      // page and head
 
     // ---- a tile's way into LDS: K [key][piece ^ sw(key)], V [head dim][piece ^ (dim / 2) % 4], so that the eight lanes that read at a time
     // are on different banks: lanes r of S^T's rows are keys (r & 3) + 16 NT (r & 4) / 4 + 4 (r & 24) / 8
-    const unsigned tile_lds = (unsigned)(size_t)(__attribute__((address_space(3))) uint8_t *)lds + stream * (BUFS * (KB + VB));
     uint8_t *const tile_ptr = lds + stream * (BUFS * (KB + VB));
+    const unsigned k_lds = (unsigned)(size_t)(__attribute__((address_space(3))) uint8_t *)lds + stream * (BUFS * (KB + VB)), v_lds = k_lds + BUFS * KB;
     auto sw = [&](int key, int upper) __attribute__((always_inline)) { return CH >= 8 ? (key & 3) | upper << 2 : (key >> 1 & 1) | upper << 1; };
     const int k_key = lane / CH, k_piece = lane % CH;
     const unsigned k_off[2] = {(unsigned)(k_key * ROWB + (k_piece ^ sw(k_key, 0)) * 16), (unsigned)(k_key * ROWB + (k_piece ^ sw(k_key, 1)) * 16)};
@@ -172,7 +194,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedKernelArgs a)
     auto load_k = [&](const Pages &p, int tile, unsigned buf) __attribute__((always_inline)) {
         const uint8_t *base[IDS];
 #pragma unroll
-        for (int u = 0; u < IDS; ++u) base[u] = a.Kc + ((place(p.id[u]) << P_log2) + ((unsigned)(tile * TILE + 16 * u) & in_page)) * ROWB;
+        for (int u = 0; u < IDS; ++u) base[u] = Kc + ((place(p.id[u]) << P_log2) + ((unsigned)(tile * TILE + 16 * u) & in_page)) * ROWB;
 #pragma unroll
         for (int i = 0; i < NK / RG; ++i) {
             // (with one block the loads' numbers are constants, and so are the units that they are in)
@@ -192,17 +214,17 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedKernelArgs a)
         const int first = RG == 1 ? 0 : block * (NV / RG);
         const size_t step = ((size_t)16 << P_log2) * EB;             // sixteen head dims
         if constexpr (ONE) {
-            const uint8_t *from = a.Vc + (((place(p.id[0]) * D) << P_log2) + ((unsigned)(tile * TILE) & in_page)) * EB + first * step;
+            const uint8_t *from = Vc + (((place(p.id[0]) * D) << P_log2) + ((unsigned)(tile * TILE) & in_page)) * EB + first * step;
 #pragma unroll
-            for (int i = 0; i < NV / RG; ++i) to_lds(buf + KB + (first + i) * 1024, from + i * step, v_off);
+            for (int i = 0; i < NV / RG; ++i) to_lds(buf + (first + i) * 1024, from + i * step, v_off);
         } else {
             // the page of the lane's piece, by the bits of its unit (not by an index, which would put the pages into memory)
             const unsigned u = EB == 1 ? v_piece : v_piece >> 1, m0 = 0u - (u & 1), m1 = 0u - (u >> 1);
             unsigned id = ((unsigned)p.id[0] & ~m0) | ((unsigned)p.id[1] & m0);
             if constexpr (IDS == 4) id = (id & ~m1) | ((((unsigned)p.id[2] & ~m0) | ((unsigned)p.id[3] & m0)) & m1);
-            const uint8_t *from = a.Vc + (((place((int)id) * D) << P_log2) + ((unsigned)(tile * TILE + 16 * u) & in_page)) * EB + (v_off - 16 * u * EB) + first * step;
+            const uint8_t *from = Vc + (((place((int)id) * D) << P_log2) + ((unsigned)(tile * TILE + 16 * u) & in_page)) * EB + (v_off - 16 * u * EB) + first * step;
 #pragma unroll
-            for (int i = 0; i < NV / RG; ++i) to_lds(buf + KB + (first + i) * 1024, from + i * step);
+            for (int i = 0; i < NV / RG; ++i) to_lds(buf + (first + i) * 1024, from + i * step);
         }
     };
     // scales stay in scalar registers until they are used, so that nothing waits for them where they are asked for
@@ -233,52 +255,15 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedKernelArgs a)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[dt][i] = 0;
 
-    Pages now, next, after{};
-    Scales sc{}, sc_next{};
-    const int mine = t_begin + stream;
-    now = pages_of(mine);
-    next = pages_of(mine + STREAMS);
-    if (mine < t_end) {
-        load_k(now, mine, tile_lds);
-        load_v(now, mine, tile_lds);
-    }
-    sc = load_scales(now);
-    // (the compiler's wait for the queries: here, as in the loop it would wait for every load on its way, every time)
-#pragma unroll
-    for (int k = 0; k < KS; ++k) asm volatile("" ::"v"(q[k]));
-    const int rounds = (t_end - t_begin + STREAMS - 1) / STREAMS;
-    for (int it = 0; it < rounds; ++it) {
-        const int t = mine + it * STREAMS;
-        const bool more = t + STREAMS < t_end;
-        const unsigned buf_at = BUFS == 1 ? 0 : (it & 1) * (KB + VB);
-        const uint8_t *const buf = tile_ptr + buf_at;
-        if constexpr (RG == 1) {
-            if (t >= t_end) break;
-            wait_loads<NV>();
-        } else {
-            wait_loads<0>();
-            asm volatile("s_barrier" ::: "memory");  // the tile is there for all, and the other buffer has been read by all
-            if (more) {
-                load_k(next, t + STREAMS, tile_lds + (KB + VB) - buf_at);
-                load_v(next, t + STREAMS, tile_lds + (KB + VB) - buf_at);
-            }
-            sc_next = load_scales(next);             // (the scalar loads are unconditional: a branch would wait for them at its end)
-            after = pages_of(t + 2 * STREAMS);
-            if (t >= t_end) continue;
-        }
-        // ---- scores
-        u32x4 kraw[NT][KR];
+    // ---- the scores of a tile from its K in LDS
+    auto read_k = [&](u32x4 (*kraw)[KR], int turn) __attribute__((always_inline)) {
+        const uint8_t *const buf = tile_ptr + (BUFS == 1 ? 0 : (turn & 1) * KB);
 #pragma unroll
         for (int T = 0; T < NT; ++T)
 #pragma unroll
             for (int i = 0; i < KR; ++i) kraw[T][i] = *reinterpret_cast<const u32x4 *>(buf + (my_key + 16 * T) * ROWB + ((hh * KR + i) ^ my_sw) * 16);
-        if constexpr (RG == 1) {
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            if (more) load_k(next, t + STREAMS, tile_lds);
-            sc_next = load_scales(next);             // (the scalar loads are unconditional: a branch would wait for them at its end)
-            after = pages_of(t + 2 * STREAMS);
-        }
-        floatx16 s[NT];
+    };
+    auto scores = [&](floatx16 *s, const u32x4 (*kraw)[KR]) __attribute__((always_inline)) {
 #pragma unroll
         for (int T = 0; T < NT; ++T)
 #pragma unroll
@@ -286,9 +271,40 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedKernelArgs a)
 #pragma unroll
         for (int k = 0; k < KS; ++k)
 #pragma unroll
-            for (int T = 0; T < NT; ++T) s[T] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fragment<FP8>(kraw[T], k), q[k], s[T], 0, 0, 0);
+            for (int T = 0; T < NT; ++T) s[T] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fragment<FP8>(kraw[T], k, 1.0f), q[k], s[T], 0, 0, 0);
+    };
+
+    Pages third{};
+    Scales sc = load_scales(now), sc_next{};
+    floatx16 s[NT];
+    if (rounds > 0) {
+        load_k(now, mine, k_lds);
+        load_v(now, mine, v_lds);
+        if (RG > 1 && rounds > 1) load_k(next, mine + STREAMS, k_lds + KB);
+    }
+    // (the compiler's wait for the queries: here, as in the loop it would wait for every load on its way, every time)
+#pragma unroll
+    for (int k = 0; k < KS; ++k) asm volatile("" ::"v"(q[k]));
+    if constexpr (RG > 1) {
+        wait_loads<0>();
+        asm volatile("s_barrier" ::: "memory");
+    }
+    if (rounds > 0) {
+        if constexpr (RG == 1) wait_loads<NV>();
+        u32x4 kraw[NT][KR];
+        read_k(kraw, 0);
+        if constexpr (RG == 1) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            if (rounds > 1) load_k(next, mine + STREAMS, k_lds);
+        }
+        scores(s, kraw);
+    }
+
+    // ---- tile by tile: the scores of the next one on the matrix cores beside this one's weights, then its output.  MORE: there is a next.
+    auto tile = [&](auto more_tag, int it, int t, bool more2) __attribute__((always_inline)) {
+        constexpr bool MORE = decltype(more_tag)::value;
         // ---- the last tile's end, and units without a page: their keys take no part
-        bool whole = t * TILE + TILE <= sh.len;
+        bool whole = t * TILE + TILE <= key_end;
 #pragma unroll
         for (int u = 0; u < IDS; ++u) whole = whole && valid(now.id[u]);
         float c[NT], vs[NT];
@@ -303,26 +319,68 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedKernelArgs a)
 #pragma unroll
             for (int T = 0; T < NT; ++T) {
                 const bool there = ONE ? valid(now.id[0]) : (((unsigned)valid(now.id[T % IDS]) & ~upper) | ((unsigned)valid(now.id[(NT + T) % IDS]) & upper)) != 0;
-                left[T] = there ? sh.len - (t * TILE + 16 * (NT * hh + T)) : 0;
+                left[T] = there ? key_end - (t * TILE + 16 * (NT * hh + T)) : 0;
                 if (left[T] <= 0) c[T] = vs[T] = 1.0f;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[T][i] = i < left[T] ? s[T][i] : -__builtin_inff();
             }
         }
-        // ---- weights: with the reference in use; a sum that is too large (the first always is) raises it, and they are taken again
-        float w[NT][16], sum;
-        auto weigh = [&]() __attribute__((always_inline)) {
-            sum = 0;
+        u32x4 kraw[NT][KR];
+        floatx16 s_next[NT];
+        if constexpr (MORE) {
+            if constexpr (RG == 1) {
+                if (it == 0) wait_loads<0>();        // (this tile's V was asked for before the next one's K)
+                else wait_loads<NV>();
+            }
+            read_k(kraw, it + 1);
+            if constexpr (RG == 1) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                if (more2) load_k(after, t + 2 * STREAMS, k_lds);
+            }
+        }
+        // ---- weights 2^(s c - m), times v_scale's significand in [1, 2): its power of two goes into the decoding of V.  The reference
+        // only has to be near the running maximum: the first tile sets it to its maximum + 7; a later one takes its weights with the one
+        // in use, and only if some weight reached 2 - one bit of its bf16 pattern - the reference is raised and they are taken again.
+        float shift[NT], part[NT];                   // of the significand: its logarithm, its reciprocal
+#pragma unroll
+        for (int T = 0; T < NT; ++T) {
+            const float x = as_float((__builtin_bit_cast(unsigned, (float)vs[T]) & 0x7fffffu) | 0x3f800000u);
+            shift[T] = FP8 ? __builtin_amdgcn_logf(x) : 0.0f;
+            part[T] = FP8 ? __builtin_amdgcn_rcpf(x) : 1.0f;
+        }
+        u32x4 w[2 * NT];
+        auto weigh = [&](int e) __attribute__((always_inline)) {     // a pair of scores of each T
+            unsigned bits = 0;
+#pragma unroll
+            for (int T = 0; T < NT; ++T) {
+                const float at = shift[T] - m;
+                const unsigned x = pack_bf16(__builtin_amdgcn_exp2f(__builtin_fmaf(s[T][2 * e], c[T], at)),
+                                             __builtin_amdgcn_exp2f(__builtin_fmaf(s[T][2 * e + 1], c[T], at)));
+                w[2 * T + e / 4][e % 4] = x;
+                bits |= x;
+            }
+            return bits;
+        };
+        // (a k step of the next scores, a part of the weights, and so on: left to itself the compiler puts one after the other)
+        unsigned over = 0;
+        if constexpr (MORE) {
 #pragma unroll
             for (int T = 0; T < NT; ++T)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    w[T][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[T][i], c[T], -m));
-                    sum += w[T][i];
-                }
-        };
-        weigh();
-        if (__any(sum > kRaise)) {
+                for (int i = 0; i < 16; ++i) s_next[T][i] = 0;
+        }
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+            if constexpr (MORE) {
+#pragma unroll
+                for (int T = 0; T < NT; ++T) s_next[T] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fragment<FP8>(kraw[T], k, 1.0f), q[k], s_next[T], 0, 0, 0);
+            }
+#pragma unroll
+            for (int e = k * 8 / KS; e < (k + 1) * 8 / KS; ++e) over |= weigh(e);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        over &= 0x40004000u;
+        if (__any(over != 0)) {                      // (of the rows that are over alone: a row's result is its own, whatever the others are)
             float top = -__builtin_inff();
 #pragma unroll
             for (int T = 0; T < NT; ++T) {
@@ -331,43 +389,43 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedKernelArgs a)
                 for (int i = 1; i < 16; ++i) x = fmaxf(x, s[T][i]);
                 top = fmaxf(top, x * c[T]);
             }
-            const float to = fmaxf(halves_max(top), m), by = __builtin_amdgcn_exp2f(m - to);
+            const float to = halves_max(over != 0 ? 1.0f : 0.0f) > 0 ? fmaxf(halves_max(top) + kMargin, m) : m, by = __builtin_amdgcn_exp2f(m - to);
             m = to;
             l *= by;
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[dt][i] *= by;
-            weigh();
+#pragma unroll
+            for (int e = 0; e < 8; ++e) weigh(e);
         }
-        l += sum;
-        bf16x8 p[2 * NT];
+        // their sums as they are multiplied, by the matrix instruction of sixteen 4 x 4 blocks: with ones as its A every lane gets the
+        // sum of its own
 #pragma unroll
-        for (int T = 0; T < NT; ++T)
+        for (int T = 0; T < NT; ++T) {
+            floatx4 sum = {0, 0, 0, 0};
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                u32x4 r;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float x0 = w[T][8 * j + 2 * e], x1 = w[T][8 * j + 2 * e + 1];
-                    r[e] = FP8 ? pack_bf16(x0 * vs[T], x1 * vs[T]) : pack_bf16(x0, x1);
-                }
-                p[2 * T + j] = __builtin_bit_cast(bf16x8, r);
+            for (int j = 0; j < 4; ++j) {
+                const u32x2 four = {w[2 * T + j / 2][j % 2 * 2], w[2 * T + j / 2][j % 2 * 2 + 1]};
+                sum = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(short4v{0x3F80, 0x3F80, 0x3F80, 0x3F80}, __builtin_bit_cast(short4v, four), sum, 0, 0, 0);
             }
+            l = __builtin_fmaf(sum[0], part[T], l);
+        }
         // ---- output
         if constexpr (RG == 1) {
-            if (more) wait_loads<NK>();
+            if (MORE && more2) wait_loads<NK>();
             else wait_loads<0>();
         }
         u32x4 vraw[DT][2];
+        const uint8_t *const buf = tile_ptr + BUFS * KB + (BUFS == 1 ? 0 : (it & 1) * VB);
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
             for (int i = 0; i < 2; ++i)
-                vraw[dt][i] = *reinterpret_cast<const u32x4 *>(buf + KB + (dt * 32 + l32) * 64 + ((2 * hh + i) ^ (l32 >> 1 & 3)) * 16);
+                vraw[dt][i] = *reinterpret_cast<const u32x4 *>(buf + (dt * 32 + l32) * 64 + ((2 * hh + i) ^ (l32 >> 1 & 3)) * 16);
         if constexpr (RG == 1) {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            if (more) load_v(next, t + STREAMS, tile_lds);
+            if constexpr (MORE) load_v(next, t + STREAMS, v_lds);
         }
         if (!whole) {                                // what lies behind may be no number, and 0 times it would be none
 #pragma unroll
@@ -382,17 +440,39 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedKernelArgs a)
                 }
         }
 #pragma unroll
-        for (int f = 0; f < 2 * NT; ++f)
+        for (int f = 0; f < 2 * NT; ++f) {
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fragment<FP8>(vraw[dt], f), p[f], o[dt], 0, 0, 0);
-        now = next;
-        sc = sc_next;
-        next = after;
-    }
+            for (int dt = 0; dt < DT; ++dt)
+                o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fragment<FP8>(vraw[dt], f, vs[f / 2 % NT]), __builtin_bit_cast(bf16x8, w[f]), o[dt], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if constexpr (MORE) {
+#pragma unroll
+            for (int T = 0; T < NT; ++T) s[T] = s_next[T];
+            now = next;
+            next = after;
+            after = third;
+            sc = sc_next;
+        }
+    };
+    auto round = [&](auto more_tag, int it, bool more2) __attribute__((always_inline)) {
+        const int t = mine + it * STREAMS;
+        if constexpr (RG > 1) {
+            wait_loads<0>();
+            asm volatile("s_barrier" ::: "memory");  // what was asked for is there for all, and all have read the other buffers
+            if (more2) load_k(after, t + 2 * STREAMS, k_lds + (it & 1) * KB);
+            if constexpr (decltype(more_tag)::value) load_v(next, t + STREAMS, v_lds + (~it & 1) * VB);
+        }
+        sc_next = load_scales(next);                 // (scalar loads are unconditional: a branch would wait for them at its end)
+        third = pages_of(t + 3 * STREAMS);
+        tile(more_tag, it, t, more2);
+    };
+    for (int it = 0; it + 1 < rounds; ++it) round(std::true_type{}, it, it + 2 < rounds);
+    if (rounds > 0) round(std::false_type{}, rounds - 1, false);
     l += halves_other(l);
 
     if constexpr (STREAMS == 1) {                    // a row is in one wave: four head dims of it at a time
-        if (v_first + l32 >= a.rows_total) return;
+        if (v_first + l32 >= rows_total) return;
         const size_t row = row_base + v_first + l32;
         const float inv = sh.used > 1 ? 1.0f : l > 0 ? 1.0f / l : 0.0f;              // no key at all: zeros
 #pragma unroll
@@ -402,21 +482,22 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedKernelArgs a)
                 const int d0 = dt * 32 + 8 * i + 4 * hh;
                 const float x0 = o[dt][4 * i] * inv, x1 = o[dt][4 * i + 1] * inv, x2 = o[dt][4 * i + 2] * inv, x3 = o[dt][4 * i + 3] * inv;
                 if (sh.used <= 1) *reinterpret_cast<uint2 *>(a.O + (row * D + d0) * 2) = make_uint2(pack_bf16(x0, x1), pack_bf16(x2, x3));
-                else *reinterpret_cast<float4 *>(a.part_o + (row * a.splits + sp) * D + d0) = make_float4(x0, x1, x2, x3);
+                else *reinterpret_cast<float4 *>(a.part_o + (row * splits + sp) * D + d0) = make_float4(x0, x1, x2, x3);
             }
         if (sh.used > 1 && hh == 0) {
-            a.part_ml[(row * a.splits + sp) * 2] = m;
-            a.part_ml[(row * a.splits + sp) * 2 + 1] = l;
+            a.part_ml[(row * splits + sp) * 2] = m;
+            a.part_ml[(row * splits + sp) * 2 + 1] = l;
         }
     } else {
         // ---- the streams' states, merged: every thread finishes eight head dims of a row at a time
         float (*const o_sh)[32][PITCH] = reinterpret_cast<float (*)[32][PITCH]>(lds);
-        __shared__ float ml_sh[4][2][32];
+        __shared__ float ml_sh[kWaves][2][32];
         __syncthreads();                             // the tiles have been read
         if (hh == 0) {
             ml_sh[wave][0][l32] = m;
             ml_sh[wave][1][l32] = l;
         }
+        if (v_first + l32 < rows_total)
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -427,7 +508,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedKernelArgs a)
         for (int u = tid; u < 32 * RG * (D / 8); u += 256) {
             const int r = u / (D / 8), d0 = (u % (D / 8)) * 8, blk = r / 32, in = r % 32;
             const int v = rt * RG * 32 + r;
-            if (v >= a.rows_total) break;
+            if (v >= rows_total) break;
             float M = ml_sh[blk][0][in];
 #pragma unroll
             for (int k = 1; k < STREAMS; ++k) M = fmaxf(M, ml_sh[blk + k * RG][0][in]);
@@ -447,12 +528,12 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedKernelArgs a)
                 *reinterpret_cast<uint4 *>(a.O + (row * D + d0) * 2) = make_uint4(pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv),
                                                                                  pack_bf16(x[4] * inv, x[5] * inv), pack_bf16(x[6] * inv, x[7] * inv));
             } else {
-                float *to = a.part_o + (row * a.splits + sp) * D + d0;
+                float *to = a.part_o + (row * splits + sp) * D + d0;
                 *reinterpret_cast<float4 *>(to) = make_float4(x[0], x[1], x[2], x[3]);
                 *reinterpret_cast<float4 *>(to + 4) = make_float4(x[4], x[5], x[6], x[7]);
                 if (d0 == 0) {
-                    a.part_ml[(row * a.splits + sp) * 2] = M;
-                    a.part_ml[(row * a.splits + sp) * 2 + 1] = L;
+                    a.part_ml[(row * splits + sp) * 2] = M;
+                    a.part_ml[(row * splits + sp) * 2 + 1] = L;
                 }
             }
         }
@@ -461,38 +542,62 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedKernelArgs a)
 }
 
 // The splits' states of a row, merged by D / 4 lanes; rows whose sequence took one split are finished already.
-template <int D> __global__ __launch_bounds__(256) void paged_merge_kernel(PagedKernelArgs a, int rows)
+template <int D>
+__global__ __launch_bounds__(256) void paged_merge_kernel(const int32_t *kv_lens, int Hkv, int rows_total, int max_pages, unsigned shape, int rows, PagedTail a)
 {
     constexpr int LANES = D / 4;
     const int row = blockIdx.x * (256 / LANES) + threadIdx.x / LANES, d0 = (threadIdx.x % LANES) * 4;
     if (row >= rows) return;
-    const int b = row / a.rows_total / a.Hkv;
-    const int used = share_of(a.kv_lens[b], a.max_pages, a.page_log2, a.splits).used;
+    const unsigned b = (unsigned)row / (unsigned)rows_total / (unsigned)Hkv;
+    const int splits = (int)(shape >> 2 & 63) + 1;
+    const int used = share_of(kv_lens[b], max_pages, 4 + (int)(shape & 3), splits).used;
     if (used <= 1) return;
-    const float *ml = a.part_ml + (size_t)row * a.splits * 2, *po = a.part_o + (size_t)row * a.splits * D + d0;
-    float M = kNone;
-    for (int s = 0; s < used; ++s) M = fmaxf(M, ml[2 * s]);
-    float L = 0, x[4] = {0, 0, 0, 0};
-    for (int s = 0; s < used; ++s) {
-        const float f = __builtin_amdgcn_exp2f(ml[2 * s] - M);
-        L += f * ml[2 * s + 1];
-        const float4 v = *reinterpret_cast<const float4 *>(po + (size_t)s * D);
-        x[0] += f * v.x; x[1] += f * v.y; x[2] += f * v.z; x[3] += f * v.w;
+    const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + (size_t)row * splits;
+    const floatx4 *po = reinterpret_cast<const floatx4 *>(a.part_o + (size_t)row * splits * D + d0);
+    constexpr int U = 8;                             // states on their way: a round trip to memory for eight of them
+    float M = kNone, L = 0;
+    floatx4 x = {0, 0, 0, 0};
+    for (int s0 = 0; s0 < used; s0 += U) {
+        float2 st[U];
+        floatx4 v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int s = min(s0 + u, used - 1);
+            st[u] = ml[s];
+            v[u] = po[(size_t)s * (D / 4)];
+        }
+        float top = M;
+#pragma unroll
+        for (int u = 0; u < U; ++u) top = fmaxf(top, st[u].x);
+        const float by = __builtin_amdgcn_exp2f(M - top);
+        M = top;
+        L *= by;
+        x *= by;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const float f = s0 + u < used ? __builtin_amdgcn_exp2f(st[u].x - M) : 0.0f;
+            L += f * st[u].y;
+            x += f * v[u];
+        }
     }
     const float inv = L > 0 ? 1.0f / L : 0.0f;
     *reinterpret_cast<uint2 *>(a.O + ((size_t)row * D + d0) * 2) = make_uint2(pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv));
 }
 
-struct Plan { int rg, splits; long row_tiles, wgs; };
+struct Plan { int rg, splits; long row_tiles, wgs; };        // splits: at most kMaxSplits, row tiles: less than 2^24
 Plan plan_of(int n, int B, int H, int Hkv, long capacity)
 {
     const long rows = (long)(H / Hkv) * n, heads = (long)B * Hkv;
     Plan p;
     p.rg = rows > 32 ? 2 : 1;
     p.row_tiles = (rows + 32 * p.rg - 1) / (32 * p.rg);
-    const long base = heads * p.row_tiles, target = 256;
-    long s = (target + base - 1) / base;
-    const long most = capacity / 1024;
+    const long base = heads * p.row_tiles;
+    // The merge's launch costs some 2 us, a wave's tile 1.1 (e4m3), so short streams are not split; longer ones down to a tile for each wave
+    // of a workgroup, until there is one workgroup per compute unit.  us with 1 / 2 / 4 / 8 / 16 splits, one token, 32/8 heads, e4m3:
+    // 512 positions 6.5 / 8.3 / 8.2 / - / -, 1024 8.8 / 9.3 / 8.2 / - / -, 4096 22.9 / 16.3 / 11.5 / 9.8 / 9.4; four sequences 4096 25.2 / 18.1 /
+    // 13.4 / 12.2 / 13.9; sixteen 27.6 / 26.8 / 28.0 / 30.9 / 35.6.
+    long s = (256 + base - 1) / base;
+    const long most = capacity < 1024 ? 1 : capacity / (64 * kSplitTiles);
     if (s > most) s = most;
     if (s > kMaxSplits) s = kMaxSplits;
     p.splits = s < 1 ? 1 : (int)s;
@@ -500,16 +605,18 @@ Plan plan_of(int n, int B, int H, int Hkv, long capacity)
     return p;
 }
 
-template <int D, bool FP8, int NT, bool ONE> hipError_t attend(const PagedKernelArgs &k, const Plan &p, hipStream_t stream)
+template <int D, bool FP8, int NT, bool ONE> hipError_t attend(const PagedAttnArgs &a, const PagedTail &tail, const Plan &p, unsigned shape, hipStream_t stream)
 {
-    const dim3 grid((unsigned)p.wgs), block(256);
-    return p.rg == 1 ? launch(attn_paged_kernel<D, FP8, NT, ONE, 1>, grid, block, stream, k)
-                     : launch(attn_paged_kernel<D, FP8, NT, ONE, 2>, grid, block, stream, k);
+    auto run = [&](auto kernel) {
+        return launch(kernel, dim3((unsigned)p.wgs), dim3(256), stream, a.table, a.kv_lens, static_cast<const uint8_t *>(a.Kc), static_cast<const uint8_t *>(a.Vc), a.Hkv,
+                      (a.H / a.Hkv) * a.n, a.num_pages, a.max_pages, (unsigned)p.wgs, shape, tail);
+    };
+    return p.rg == 1 ? run(attn_paged_kernel<D, FP8, NT, ONE, 1>) : run(attn_paged_kernel<D, FP8, NT, ONE, 2>);
 }
-template <int D, bool FP8> hipError_t attend(const PagedKernelArgs &k, const Plan &p, hipStream_t stream)
+template <int D, bool FP8> hipError_t attend(const PagedAttnArgs &a, const PagedTail &tail, const Plan &p, unsigned shape, hipStream_t stream)
 {
     constexpr int NT = FP8 ? 2 : 1;                  // (bf16 pieces take twice the registers)
-    return (1 << k.page_log2) >= 32 * NT ? attend<D, FP8, NT, true>(k, p, stream) : attend<D, FP8, NT, false>(k, p, stream);
+    return (1 << a.page_log2) >= 32 * NT ? attend<D, FP8, NT, true>(a, tail, p, shape, stream) : attend<D, FP8, NT, false>(a, tail, p, shape, stream);
 }
 
 }  // namespace
@@ -526,16 +633,16 @@ hipError_t launch_attention_paged(const PagedAttnArgs &a, hipStream_t stream)
     const Plan p = plan_of(a.n, a.B, a.H, a.Hkv, (long)a.max_pages << a.page_log2);
     const size_t rows = (size_t)a.B * a.H * a.n;
     const bool fp8 = a.k_scale != nullptr;
-    PagedKernelArgs k{static_cast<const uint8_t *>(a.Q), static_cast<const uint8_t *>(a.Kc), static_cast<const uint8_t *>(a.Vc), a.table, a.kv_lens,
-                      a.k_scale, a.v_scale, static_cast<uint8_t *>(a.O), static_cast<float *>(a.workspace),
-                      static_cast<float *>(a.workspace) + rows * p.splits * a.d, a.Hkv, (a.H / a.Hkv) * a.n, a.num_pages, a.max_pages, a.page_log2,
-                      (int)p.row_tiles, p.splits, (int)p.wgs, (float)(1.4426950408889634 / __builtin_sqrt((double)a.d))};
-    const hipError_t e = a.d == 128 ? (fp8 ? attend<128, true>(k, p, stream) : attend<128, false>(k, p, stream))
-                                    : (fp8 ? attend<64, true>(k, p, stream) : attend<64, false>(k, p, stream));
+    const PagedTail tail{static_cast<const uint8_t *>(a.Q), a.k_scale, a.v_scale, static_cast<uint8_t *>(a.O), static_cast<float *>(a.workspace),
+                         static_cast<float *>(a.workspace) + rows * p.splits * a.d, (float)(1.4426950408889634 / __builtin_sqrt((double)a.d))};
+    const unsigned shape = (unsigned)p.row_tiles << 8 | (unsigned)(p.splits - 1) << 2 | (unsigned)(a.page_log2 - 4);
+    const hipError_t e = a.d == 128 ? (fp8 ? attend<128, true>(a, tail, p, shape, stream) : attend<128, false>(a, tail, p, shape, stream))
+                                    : (fp8 ? attend<64, true>(a, tail, p, shape, stream) : attend<64, false>(a, tail, p, shape, stream));
     if (e != hipSuccess || p.splits <= 1) return e;
     const unsigned per_wg = 256 / (a.d / 4);
     const dim3 grid((unsigned)((rows + per_wg - 1) / per_wg));
-    return a.d == 128 ? launch(paged_merge_kernel<128>, grid, dim3(256), stream, k, (int)rows) : launch(paged_merge_kernel<64>, grid, dim3(256), stream, k, (int)rows);
+    auto merge = [&](auto kernel) { return launch(kernel, grid, dim3(256), stream, a.kv_lens, a.Hkv, (a.H / a.Hkv) * a.n, a.max_pages, shape, (int)rows, tail); };
+    return a.d == 128 ? merge(paged_merge_kernel<128>) : merge(paged_merge_kernel<64>);
 }
 
 }  // namespace dd

@@ -490,7 +490,7 @@ static int check_pages(const void *Kc, const void *Vc, const float *k_scale, con
     if (cache_dtype != DD_BF16 && cache_dtype != DD_FP8_E4M3) return DD_ERR_DTYPE;
     if (cache_dtype == DD_FP8_E4M3 && (!k_scale || !v_scale)) return DD_ERR_NULL;
     if (n < 0 || B < 1 || Hkv < 1 || (d != 64 && d != 128) || num_pages < 1 || max_pages < 1 || page_log2_of(page_size) < 0) return DD_ERR_SHAPE;
-    if ((double)max_pages * page_size >= 2147483648.0 || (double)num_pages * Hkv * page_size * d >= 1099511627776.0) return DD_ERR_SHAPE;
+    if ((double)max_pages * page_size >= 1073741824.0 || (double)num_pages * Hkv * page_size * d >= 1099511627776.0) return DD_ERR_SHAPE;
     if (misaligned16(Kc) || misaligned16(Vc)) return DD_ERR_ALIGN;
     const uintptr_t words = reinterpret_cast<uintptr_t>(k_scale) | reinterpret_cast<uintptr_t>(v_scale) | reinterpret_cast<uintptr_t>(table) |
                             reinterpret_cast<uintptr_t>(lens);
@@ -537,7 +537,7 @@ size_t dd_paged_attention_workspace_bytes(int n, int B, int H, int Hkv, int d, i
 {
     if (n < 1 || B < 1 || H < 1 || Hkv < 1 || H % Hkv != 0 || (d != 64 && d != 128) || max_pages < 1 || page_log2_of(page_size) < 0) return 0;
     if (cache_dtype != DD_BF16 && cache_dtype != DD_FP8_E4M3) return 0;
-    if ((double)max_pages * page_size >= 2147483648.0 || (double)B * H * n >= 2147483648.0) return 0;
+    if ((double)max_pages * page_size >= 1073741824.0 || (double)B * H * n >= 1073741824.0) return 0;
     return dd::paged_attention_workspace_bytes(n, B, H, Hkv, d, (long)max_pages * page_size, cache_dtype == DD_FP8_E4M3);
 }
 
@@ -551,7 +551,7 @@ int dd_paged_attention(const void *Q, const void *Kc, const void *Vc, const floa
     if (H < 1 || H % Hkv != 0) return DD_ERR_SHAPE;
     if (n == 0) return DD_OK;
     if (!Q || !O) return DD_ERR_NULL;
-    if ((double)B * H * n >= 2147483648.0) return DD_ERR_SHAPE;
+    if ((double)B * H * n >= 1073741824.0) return DD_ERR_SHAPE;
     if (misaligned16(Q) || misaligned16(O)) return DD_ERR_ALIGN;
     const bool fp8 = cache_dtype == DD_FP8_E4M3;
     rc = check_workspace(workspace, workspace_bytes, dd::paged_attention_workspace_bytes(n, B, H, Hkv, d, (long)max_pages * page_size, fp8));
