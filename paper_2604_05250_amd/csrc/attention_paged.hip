@@ -9,12 +9,14 @@
 // A unit of 16 keys (h, T) lies in one page whatever the page size, so its page and its scales are one value per lane and T.
 // Tiles go to LDS by loads that no register waits for, a kilobyte of memory each in the order in which it lies there: the operands'
 // own order, taken straight into registers, is sixteen bytes out of each of 32 rows per load, and cost more than the arithmetic (16
-// sequences x 64 rows, 32/8 heads, 2048 e4m3 keys 51 us, with all loads from the nearest cache 50, with none 37; by LDS 43).
+// sequences x 64 rows, 32/8 heads, 2048 e4m3 keys 51 us, with all loads from the nearest cache 50, with none 37; by LDS 43, in three
+// stages 40).
 // A workgroup's four waves are one row block x 4 streams of keys, each with a state (reference, sum, O) of its own and a tile of its
 // own in LDS, whose K is asked for again as soon as it is in registers, and V likewise; or two blocks x 2 streams with doubled tiles
-// that two waves share.  The next tile's scores are computed beside this one's weights, so that the matrix cores and the vector units
-// have work at the same time.  The states are merged through LDS, the key range is split over workgroups where those are few, and the
-// splits' states are merged by a second kernel.
+// that two waves share (as above 44.5 and 40.2 us; four blocks x two streams of eight waves 42.9).  The next keys' scores are computed beside
+// these keys' weights, for e4m3 pages the last keys' output beside both, so that the matrix cores and the vector units have work at the
+// same time; neither then idles for long, and the clock gives way to their load.  The states are merged through LDS, the key range is
+// split over workgroups where those are few, and the splits' states are merged by a second kernel.
 // e4m3 codes become bf16 exactly in registers.  k_scale goes into the factor of the exponent; of v_scale the power of two goes into the
 // decoding of V, which is exact (bf16 for its range: scales span 2^-126 .. 2^119), and the rest, 1 where this library made the scale,
 // into the exponent.  Weights are rounded to bf16 (2^-8 of each at most, as the result is), their sum is the one of the rounded ones.
@@ -38,8 +40,9 @@ typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 constexpr float kNone = -1.0e30f;        // the reference of a row that has met no key
 [[maybe_unused]] constexpr float kMargin = 7.0f;          // a reference is set this far above a tile's maximum (log2 units)
 constexpr int kMaxSplits = 64;
-[[maybe_unused]] constexpr int kWaves = 4;
-constexpr int kSplitTiles = 4;           // tiles of 64 keys that a split has at least
+[[maybe_unused]] constexpr int kWaves = 4;           // per workgroup
+constexpr int kFewRows = 32;             // of a key/value head: one row block
+constexpr int kSplitTiles = 4, kSplitTilesMany = 8;        // tiles of 64 keys that a split has at least, with few rows and with more
 
 __device__ __forceinline__ unsigned pack_bf16(float lo, float hi)
 {
@@ -83,12 +86,12 @@ struct PagedTail {
 
 // How a sequence's tiles are shared out over the splits of a call: tiles per split and splits that have any.
 struct Share { int tiles, per_split, used, len; };
-__device__ __forceinline__ Share share_of(int len, int max_pages, int page_log2, int splits)
+__device__ __forceinline__ Share share_of(int len, int max_pages, int page_log2, int splits, int rows_total)
 {
     Share s;
     s.len = min(max(len, 0), max_pages << page_log2);        // (less than 2^30)
     s.tiles = (int)(((unsigned)s.len + 63u) >> 6);
-    s.per_split = max((s.tiles + splits - 1) / splits, kSplitTiles);
+    s.per_split = max((s.tiles + splits - 1) / splits, rows_total <= kFewRows ? kSplitTiles : kSplitTilesMany);
     s.used = s.tiles == 0 ? 0 : (s.tiles + s.per_split - 1) / s.per_split;
     return s;
 }
@@ -156,7 +159,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(DD_PAGED_HEAD, Paged
         next = pages_of(stream + STREAMS);
         after = pages_of(stream + 2 * STREAMS);
     }
-    const Share sh = share_of(held, max_pages, P_log2, splits);
+    const Share sh = share_of(held, max_pages, P_log2, splits, rows_total);
     if (sp >= sh.used && sp > 0) return;
     const int v_first = (rt * RG + block) * 32;
     const size_t row_base = (size_t)head * rows_total;
@@ -255,28 +258,110 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(DD_PAGED_HEAD, Paged
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[dt][i] = 0;
 
-    // ---- the scores of a tile from its K in LDS
-    auto read_k = [&](u32x4 (*kraw)[KR], int turn) __attribute__((always_inline)) {
+    // ---- a tile's K from LDS, a half of the keys (T) at a time, and its V
+    auto read_k = [&](u32x4 *kraw, int T, int turn) __attribute__((always_inline)) {
         const uint8_t *const buf = tile_ptr + (BUFS == 1 ? 0 : (turn & 1) * KB);
 #pragma unroll
-        for (int T = 0; T < NT; ++T)
-#pragma unroll
-            for (int i = 0; i < KR; ++i) kraw[T][i] = *reinterpret_cast<const u32x4 *>(buf + (my_key + 16 * T) * ROWB + ((hh * KR + i) ^ my_sw) * 16);
+        for (int i = 0; i < KR; ++i) kraw[i] = *reinterpret_cast<const u32x4 *>(buf + (my_key + 16 * T) * ROWB + ((hh * KR + i) ^ my_sw) * 16);
     };
-    auto scores = [&](floatx16 *s, const u32x4 (*kraw)[KR]) __attribute__((always_inline)) {
+    auto read_v = [&](u32x4 (*vraw)[2], int first, int last, int turn) __attribute__((always_inline)) {     // pieces first .. last
+        const uint8_t *const buf = tile_ptr + BUFS * KB + (BUFS == 1 ? 0 : (turn & 1) * VB);
 #pragma unroll
-        for (int T = 0; T < NT; ++T)
+        for (int i = first; i <= last; ++i)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[T][i] = 0;
+            for (int dt = 0; dt < DT; ++dt)
+                vraw[dt][i] = *reinterpret_cast<const u32x4 *>(buf + (dt * 32 + l32) * 64 + ((2 * hh + i) ^ (l32 >> 1 & 3)) * 16);
+    };
+    auto zeros = [&]() __attribute__((always_inline)) {
+        floatx16 z;
 #pragma unroll
-        for (int k = 0; k < KS; ++k)
+        for (int i = 0; i < 16; ++i) z[i] = 0;
+        return z;
+    };
+    // ---- what a tile's scores and values are multiplied by: the factor of the exponent, v_scale, of its significand in [1, 2) the
+    // logarithm and the reciprocal (its power of two goes into the decoding of V)
+    struct Factors {
+        float c[NT], vs[NT], shift[NT], part[NT];
+        int left[NT];                                // keys of the lane's unit that count
+        bool whole;
+    };
+    auto factors_of = [&](const Pages &p, const Scales &x, int t) __attribute__((always_inline)) {
+        Factors f;
+        f.whole = t * TILE + TILE <= key_end;
 #pragma unroll
-            for (int T = 0; T < NT; ++T) s[T] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fragment<FP8>(kraw[T], k, 1.0f), q[k], s[T], 0, 0, 0);
+        for (int u = 0; u < IDS; ++u) f.whole = f.whole && valid(p.id[u]);
+#pragma unroll
+        for (int T = 0; T < NT; ++T) {
+            f.c[T] = FP8 ? a.scale_log2 * of_half(x.k, T) : a.scale_log2;
+            f.vs[T] = of_half(x.v, T);
+            f.left[T] = 16;
+        }
+        if (!f.whole) {                              // the last tile's end, and units without a page: their keys take no part
+#pragma unroll
+            for (int T = 0; T < NT; ++T) {
+                const bool there = ONE ? valid(p.id[0]) : (((unsigned)valid(p.id[T % IDS]) & ~upper) | ((unsigned)valid(p.id[(NT + T) % IDS]) & upper)) != 0;
+                f.left[T] = there ? key_end - (t * TILE + 16 * (NT * hh + T)) : 0;
+                if (f.left[T] <= 0) f.c[T] = f.vs[T] = 1.0f;
+            }
+        }
+#pragma unroll
+        for (int T = 0; T < NT; ++T) {
+            const float x = as_float((__builtin_bit_cast(unsigned, (float)f.vs[T]) & 0x7fffffu) | 0x3f800000u);
+            f.shift[T] = FP8 ? __builtin_amdgcn_logf(x) : 0.0f;
+            f.part[T] = FP8 ? __builtin_amdgcn_rcpf(x) : 1.0f;
+        }
+        return f;
+    };
+    auto mask = [&](floatx16 &s, int left) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = i < left ? s[i] : -__builtin_inff();
+    };
+    auto mask_v = [&](u32x4 (*vraw)[2], int first, int last, const Factors &f) __attribute__((always_inline)) {
+        // what lies behind may be no number, and 0 times it would be none
+#pragma unroll
+        for (int i = first; i <= last; ++i)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                constexpr int PER = 4 / EB;
+                const int n = (FP8 ? f.left[i % NT] : f.left[0] - 8 * i) - x * PER;
+                const unsigned keep = n >= PER ? ~0u : n <= 0 ? 0u : (1u << (n * 8 * EB)) - 1;
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) vraw[dt][i][x] &= keep;
+            }
+    };
+    // ---- weights 2^(s c - m) of 32 keys.  The reference only has to be near the running maximum: the first keys set it to their maximum
+    // + 7; later ones take their weights with the one in use, and only if some weight reached 2 - one bit of its bf16 pattern - the
+    // reference is raised and they are taken again: of the rows that are over alone, a row's result is its own, whatever the others are.
+    struct Weights { u32x4 w[2]; };
+    auto weigh = [&](Weights &w, const floatx16 &s, int e, float c, float at) __attribute__((always_inline)) {     // two of them
+        const unsigned x = pack_bf16(__builtin_amdgcn_exp2f(__builtin_fmaf(s[2 * e], c, at)), __builtin_amdgcn_exp2f(__builtin_fmaf(s[2 * e + 1], c, at)));
+        w.w[e / 4][e % 4] = x;
+        return x;
+    };
+    auto raise = [&](Weights &w, const floatx16 &s, float c, float shift, unsigned over) __attribute__((always_inline)) {
+        if (!__any((over & 0x40004000u) != 0)) return;
+        float top = s[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+        const float to = halves_max((over & 0x40004000u) != 0 ? 1.0f : 0.0f) > 0 ? fmaxf(halves_max(top * c) + kMargin, m) : m, by = __builtin_amdgcn_exp2f(m - to);
+        m = to;
+        l *= by;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[dt][i] *= by;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) weigh(w, s, e, c, shift - m);
+    };
+    // their sum as they are multiplied, by the matrix instruction of sixteen 4 x 4 blocks: with ones as its A every lane gets the sum of
+    // its own; four at a time
+    auto sum4 = [&](floatx4 sum, const Weights &w, int j) __attribute__((always_inline)) {
+        const u32x2 four = {w.w[j / 2][j % 2 * 2], w.w[j / 2][j % 2 * 2 + 1]};
+        return __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(short4v{0x3F80, 0x3F80, 0x3F80, 0x3F80}, __builtin_bit_cast(short4v, four), sum, 0, 0, 0);
     };
 
     Pages third{};
-    Scales sc = load_scales(now), sc_next{};
-    floatx16 s[NT];
+    Scales sc = load_scales(now), sc_next = load_scales(next);
     if (rounds > 0) {
         load_k(now, mine, k_lds);
         load_v(now, mine, v_lds);
@@ -289,186 +374,186 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(DD_PAGED_HEAD, Paged
         wait_loads<0>();
         asm volatile("s_barrier" ::: "memory");
     }
+    floatx16 s[NT];
     if (rounds > 0) {
         if constexpr (RG == 1) wait_loads<NV>();
         u32x4 kraw[NT][KR];
-        read_k(kraw, 0);
+#pragma unroll
+        for (int T = 0; T < NT; ++T) read_k(kraw[T], T, 0);
         if constexpr (RG == 1) {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             if (rounds > 1) load_k(next, mine + STREAMS, k_lds);
         }
-        scores(s, kraw);
+#pragma unroll
+        for (int T = 0; T < NT; ++T) s[T] = zeros();
+#pragma unroll
+        for (int k = 0; k < KS; ++k)
+#pragma unroll
+            for (int T = 0; T < NT; ++T) s[T] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fragment<FP8>(kraw[T], k, 1.0f), q[k], s[T], 0, 0, 0);
     }
-
-    // ---- tile by tile: the scores of the next one on the matrix cores beside this one's weights, then its output.  MORE: there is a next.
-    auto tile = [&](auto more_tag, int it, int t, bool more2) __attribute__((always_inline)) {
-        constexpr bool MORE = decltype(more_tag)::value;
-        // ---- the last tile's end, and units without a page: their keys take no part
-        bool whole = t * TILE + TILE <= key_end;
-#pragma unroll
-        for (int u = 0; u < IDS; ++u) whole = whole && valid(now.id[u]);
-        float c[NT], vs[NT];
-        int left[NT];                                // keys of the lane's unit that count
-#pragma unroll
-        for (int T = 0; T < NT; ++T) {
-            c[T] = FP8 ? a.scale_log2 * of_half(sc.k, T) : a.scale_log2;
-            vs[T] = of_half(sc.v, T);
-            left[T] = 16;
-        }
-        if (!whole) {
-#pragma unroll
-            for (int T = 0; T < NT; ++T) {
-                const bool there = ONE ? valid(now.id[0]) : (((unsigned)valid(now.id[T % IDS]) & ~upper) | ((unsigned)valid(now.id[(NT + T) % IDS]) & upper)) != 0;
-                left[T] = there ? key_end - (t * TILE + 16 * (NT * hh + T)) : 0;
-                if (left[T] <= 0) c[T] = vs[T] = 1.0f;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[T][i] = i < left[T] ? s[T][i] : -__builtin_inff();
+    if constexpr (NT == 1) {
+        // ---- tile by tile: the scores of the next one on the matrix cores beside this one's weights, then its output.  MORE: there is a next.
+        auto round = [&](auto more_tag, int it, bool more2) __attribute__((always_inline)) {
+            constexpr bool MORE = decltype(more_tag)::value;
+            const int t = mine + it * STREAMS;
+            if constexpr (RG > 1) {
+                wait_loads<0>();
+                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");         // what was asked for is there for all, and all have read the other buffers
+                if (more2) load_k(after, t + 2 * STREAMS, k_lds + (it & 1) * KB);
+                if constexpr (MORE) load_v(next, t + STREAMS, v_lds + (~it & 1) * VB);
             }
-        }
-        u32x4 kraw[NT][KR];
-        floatx16 s_next[NT];
-        if constexpr (MORE) {
-            if constexpr (RG == 1) {
-                if (it == 0) wait_loads<0>();        // (this tile's V was asked for before the next one's K)
-                else wait_loads<NV>();
-            }
-            read_k(kraw, it + 1);
-            if constexpr (RG == 1) {
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                if (more2) load_k(after, t + 2 * STREAMS, k_lds);
-            }
-        }
-        // ---- weights 2^(s c - m), times v_scale's significand in [1, 2): its power of two goes into the decoding of V.  The reference
-        // only has to be near the running maximum: the first tile sets it to its maximum + 7; a later one takes its weights with the one
-        // in use, and only if some weight reached 2 - one bit of its bf16 pattern - the reference is raised and they are taken again.
-        float shift[NT], part[NT];                   // of the significand: its logarithm, its reciprocal
-#pragma unroll
-        for (int T = 0; T < NT; ++T) {
-            const float x = as_float((__builtin_bit_cast(unsigned, (float)vs[T]) & 0x7fffffu) | 0x3f800000u);
-            shift[T] = FP8 ? __builtin_amdgcn_logf(x) : 0.0f;
-            part[T] = FP8 ? __builtin_amdgcn_rcpf(x) : 1.0f;
-        }
-        u32x4 w[2 * NT];
-        auto weigh = [&](int e) __attribute__((always_inline)) {     // a pair of scores of each T
-            unsigned bits = 0;
-#pragma unroll
-            for (int T = 0; T < NT; ++T) {
-                const float at = shift[T] - m;
-                const unsigned x = pack_bf16(__builtin_amdgcn_exp2f(__builtin_fmaf(s[T][2 * e], c[T], at)),
-                                             __builtin_amdgcn_exp2f(__builtin_fmaf(s[T][2 * e + 1], c[T], at)));
-                w[2 * T + e / 4][e % 4] = x;
-                bits |= x;
-            }
-            return bits;
-        };
-        // (a k step of the next scores, a part of the weights, and so on: left to itself the compiler puts one after the other)
-        unsigned over = 0;
-        if constexpr (MORE) {
-#pragma unroll
-            for (int T = 0; T < NT; ++T)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s_next[T][i] = 0;
-        }
-#pragma unroll
-        for (int k = 0; k < KS; ++k) {
+            third = pages_of(t + 3 * STREAMS);           // (scalar loads are unconditional: a branch would wait for them at its end)
+            const Factors f = factors_of(now, sc, t);
+            sc = sc_next;
+            sc_next = load_scales(after);
+            if (!f.whole) mask(s[0], f.left[0]);
+            u32x4 kraw[KR];
+            floatx16 s_next = zeros();
             if constexpr (MORE) {
-#pragma unroll
-                for (int T = 0; T < NT; ++T) s_next[T] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fragment<FP8>(kraw[T], k, 1.0f), q[k], s_next[T], 0, 0, 0);
+                if constexpr (RG == 1) {
+                    if (it == 0) wait_loads<0>();        // (this tile's V was asked for before the next one's K)
+                    else wait_loads<NV>();
+                }
+                read_k(kraw, 0, it + 1);
+                if constexpr (RG == 1) {
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                    if (more2) load_k(after, t + 2 * STREAMS, k_lds);
+                }
             }
+            Weights w;
+            unsigned over = 0;
 #pragma unroll
-            for (int e = k * 8 / KS; e < (k + 1) * 8 / KS; ++e) over |= weigh(e);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        over &= 0x40004000u;
-        if (__any(over != 0)) {                      // (of the rows that are over alone: a row's result is its own, whatever the others are)
-            float top = -__builtin_inff();
+            for (int k = 0; k < KS; ++k) {
+                if constexpr (MORE) s_next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fragment<FP8>(kraw, k, 1.0f), q[k], s_next, 0, 0, 0);
 #pragma unroll
-            for (int T = 0; T < NT; ++T) {
-                float x = s[T][0];
-#pragma unroll
-                for (int i = 1; i < 16; ++i) x = fmaxf(x, s[T][i]);
-                top = fmaxf(top, x * c[T]);
+                for (int e = k * 8 / KS; e < (k + 1) * 8 / KS; ++e) over |= weigh(w, s[0], e, f.c[0], f.shift[0] - m);
+                __builtin_amdgcn_sched_barrier(0);       // (left to itself the compiler puts one after the other)
             }
-            const float to = halves_max(over != 0 ? 1.0f : 0.0f) > 0 ? fmaxf(halves_max(top) + kMargin, m) : m, by = __builtin_amdgcn_exp2f(m - to);
-            m = to;
-            l *= by;
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[dt][i] *= by;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) weigh(e);
-        }
-        // their sums as they are multiplied, by the matrix instruction of sixteen 4 x 4 blocks: with ones as its A every lane gets the
-        // sum of its own
-#pragma unroll
-        for (int T = 0; T < NT; ++T) {
+            raise(w, s[0], f.c[0], f.shift[0], over);
             floatx4 sum = {0, 0, 0, 0};
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const u32x2 four = {w[2 * T + j / 2][j % 2 * 2], w[2 * T + j / 2][j % 2 * 2 + 1]};
-                sum = __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(short4v{0x3F80, 0x3F80, 0x3F80, 0x3F80}, __builtin_bit_cast(short4v, four), sum, 0, 0, 0);
+            for (int j = 0; j < 4; ++j) sum = sum4(sum, w, j);
+            l = __builtin_fmaf(sum[0], f.part[0], l);
+            if constexpr (RG == 1) {
+                if (MORE && more2) wait_loads<NK>();
+                else wait_loads<0>();
             }
-            l = __builtin_fmaf(sum[0], part[T], l);
-        }
-        // ---- output
-        if constexpr (RG == 1) {
-            if (MORE && more2) wait_loads<NK>();
-            else wait_loads<0>();
-        }
-        u32x4 vraw[DT][2];
-        const uint8_t *const buf = tile_ptr + BUFS * KB + (BUFS == 1 ? 0 : (it & 1) * VB);
+            u32x4 vraw[DT][2];
+            read_v(vraw, 0, 1, it);
+            if constexpr (RG == 1) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                if constexpr (MORE) load_v(next, t + STREAMS, v_lds);
+            }
+            if (!f.whole) mask_v(vraw, 0, 1, f);
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
+            for (int j = 0; j < 2; ++j) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-                vraw[dt][i] = *reinterpret_cast<const u32x4 *>(buf + (dt * 32 + l32) * 64 + ((2 * hh + i) ^ (l32 >> 1 & 3)) * 16);
-        if constexpr (RG == 1) {
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            if constexpr (MORE) load_v(next, t + STREAMS, v_lds);
-        }
-        if (!whole) {                                // what lies behind may be no number, and 0 times it would be none
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    constexpr int PER = 4 / EB;
-                    const int n = (FP8 ? left[i % NT] : left[0] - 8 * i) - x * PER;
-                    const unsigned keep = n >= PER ? ~0u : n <= 0 ? 0u : (1u << (n * 8 * EB)) - 1;
-#pragma unroll
-                    for (int dt = 0; dt < DT; ++dt) vraw[dt][i][x] &= keep;
-                }
-        }
-#pragma unroll
-        for (int f = 0; f < 2 * NT; ++f) {
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt)
-                o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fragment<FP8>(vraw[dt], f, vs[f / 2 % NT]), __builtin_bit_cast(bf16x8, w[f]), o[dt], 0, 0, 0);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        if constexpr (MORE) {
-#pragma unroll
-            for (int T = 0; T < NT; ++T) s[T] = s_next[T];
+                for (int dt = 0; dt < DT; ++dt)
+                    o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fragment<FP8>(vraw[dt], j, 1.0f), __builtin_bit_cast(bf16x8, w.w[j]), o[dt], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            s[0] = s_next;
             now = next;
             next = after;
             after = third;
-            sc = sc_next;
+        };
+        for (int it = 0; it + 1 < rounds; ++it) round(std::true_type{}, it, it + 2 < rounds);
+        if (rounds > 0) round(std::false_type{}, rounds - 1, false);
+    } else {
+        // ---- half a tile, 32 keys, at a time, in three stages at once: the output of keys u, the weights of keys u + 32, the scores of keys
+        // u + 64.  A matrix instruction, the decoding of the next one's operand and a share of the weights take turns, so that neither the
+        // matrix cores nor the vector units wait for the other.  MORE: there is a next tile.
+        Factors f = factors_of(now, sc, mine);
+        Weights w;
+        unsigned over = 0;
+        if (rounds > 0) {
+            if (!f.whole) mask(s[0], f.left[0]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) over |= weigh(w, s[0], e, f.c[0], f.shift[0] - m);
+            raise(w, s[0], f.c[0], f.shift[0], over);
         }
-    };
-    auto round = [&](auto more_tag, int it, bool more2) __attribute__((always_inline)) {
-        const int t = mine + it * STREAMS;
-        if constexpr (RG > 1) {
+        auto round = [&](auto more_tag, int it, bool more2) __attribute__((always_inline)) {
+            constexpr bool MORE = decltype(more_tag)::value;
+            const int t = mine + it * STREAMS;
             wait_loads<0>();
-            asm volatile("s_barrier" ::: "memory");  // what was asked for is there for all, and all have read the other buffers
-            if (more2) load_k(after, t + 2 * STREAMS, k_lds + (it & 1) * KB);
-            if constexpr (decltype(more_tag)::value) load_v(next, t + STREAMS, v_lds + (~it & 1) * VB);
-        }
-        sc_next = load_scales(next);                 // (scalar loads are unconditional: a branch would wait for them at its end)
-        third = pages_of(t + 3 * STREAMS);
-        tile(more_tag, it, t, more2);
-    };
-    for (int it = 0; it + 1 < rounds; ++it) round(std::true_type{}, it, it + 2 < rounds);
-    if (rounds > 0) round(std::false_type{}, rounds - 1, false);
+            if constexpr (RG > 1) {
+                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");         // what was asked for is there for all, and all have read the other buffers
+                if (more2) load_k(after, t + 2 * STREAMS, k_lds + (it & 1) * KB);
+                if constexpr (MORE) load_v(next, t + STREAMS, v_lds + (~it & 1) * VB);
+            }
+            u32x4 kraw[NT][KR], vraw[DT][2];
+            constexpr int READ = RG == 1 ? 1 : 0;        // the halves that are read now: a wave's own tile is to be free for the next one
+            read_v(vraw, 0, READ, it);
+            if constexpr (MORE) {
+#pragma unroll
+                for (int T = 0; T <= READ; ++T) read_k(kraw[T], T, it + 1);
+            }
+            if constexpr (RG == 1) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                if (more2) load_k(after, t + 2 * STREAMS, k_lds);
+                if constexpr (MORE) load_v(next, t + STREAMS, v_lds);
+            }
+            third = pages_of(t + 3 * STREAMS);           // (scalar loads are unconditional: a branch would wait for them at its end)
+            const Factors fn = factors_of(next, sc_next, t + STREAMS);
+            sc_next = load_scales(after);
+            if (!f.whole) {
+                mask_v(vraw, 0, READ, f);
+                mask(s[1], f.left[1]);
+            }
+            auto step = [&](auto t_tag, auto s_tag, auto w_tag, const Factors &fw, floatx16 &from, floatx16 &to) __attribute__((always_inline)) {
+                constexpr int T = decltype(t_tag)::value;
+                constexpr bool SCORES = decltype(s_tag)::value, WEIGHTS = decltype(w_tag)::value;
+                constexpr int TW = 1 - T;                // the half that is weighed
+                Weights wn;
+                unsigned over = 0;
+                floatx4 sum = {0, 0, 0, 0};
+                floatx16 acc = zeros();
+                const float c = fw.c[TW], at = fw.shift[TW] - m;
+                constexpr int SLOTS = 2 * DT;            // output instructions; KS of scores beside them
+                bf16x8 fk, fv = fragment<FP8>(vraw[0], 2 * T, f.vs[T]);
+                if constexpr (SCORES) fk = fragment<FP8>(kraw[T], 0, 1.0f);
+#pragma unroll
+                for (int i = 0; i < SLOTS; ++i) {
+                    const int dt = i % DT, j = i / DT;
+                    if constexpr (SCORES) {
+                        if (i < KS) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fk, q[i % KS], acc, 0, 0, 0);
+                        if (i + 1 < KS) fk = fragment<FP8>(kraw[T], (i + 1) % KS, 1.0f);
+                    }
+                    if constexpr (WEIGHTS) {
+                        if (i < 8) over |= weigh(wn, from, i % 8, c, at);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                    o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fv, __builtin_bit_cast(bf16x8, w.w[j]), o[dt], 0, 0, 0);
+                    if (i + 1 < SLOTS) fv = fragment<FP8>(vraw[(i + 1) % DT], 2 * T + (i + 1) / DT, f.vs[T]);
+                    if (i < 4) sum = sum4(sum, w, i);
+                    if constexpr (WEIGHTS && SLOTS < 8) over |= weigh(wn, from, (SLOTS + i) % 8, c, at);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                l = __builtin_fmaf(sum[0], f.part[T], l);
+                if constexpr (WEIGHTS) {
+                    raise(wn, from, c, fw.shift[TW], over);
+                    w = wn;
+                }
+                if constexpr (SCORES) to = acc;
+            };
+            step(std::integral_constant<int, 0>{}, more_tag, std::true_type{}, f, s[1], s[0]);
+            if constexpr (READ == 0) {
+                read_v(vraw, 1, 1, it);
+                if constexpr (MORE) read_k(kraw[1], 1, it + 1);
+                if (!f.whole) mask_v(vraw, 1, 1, f);
+            }
+            if constexpr (MORE) {
+                if (!fn.whole) mask(s[0], fn.left[0]);
+            }
+            step(std::integral_constant<int, 1>{}, more_tag, more_tag, fn, s[0], s[1]);
+            f = fn;
+            now = next;
+            next = after;
+            after = third;
+        };
+        for (int it = 0; it + 1 < rounds; ++it) round(std::true_type{}, it, it + 2 < rounds);
+        if (rounds > 0) round(std::false_type{}, rounds - 1, false);
+    }
     l += halves_other(l);
 
     if constexpr (STREAMS == 1) {                    // a row is in one wave: four head dims of it at a time
@@ -550,7 +635,7 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(const int32_t *kv_lens
     if (row >= rows) return;
     const unsigned b = (unsigned)row / (unsigned)rows_total / (unsigned)Hkv;
     const int splits = (int)(shape >> 2 & 63) + 1;
-    const int used = share_of(kv_lens[b], max_pages, 4 + (int)(shape & 3), splits).used;
+    const int used = share_of(kv_lens[b], max_pages, 4 + (int)(shape & 3), splits, rows_total).used;
     if (used <= 1) return;
     const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + (size_t)row * splits;
     const floatx4 *po = reinterpret_cast<const floatx4 *>(a.part_o + (size_t)row * splits * D + d0);
@@ -585,20 +670,31 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(const int32_t *kv_lens
 }
 
 struct Plan { int rg, splits; long row_tiles, wgs; };        // splits: at most kMaxSplits, row tiles: less than 2^24
-Plan plan_of(int n, int B, int H, int Hkv, long capacity)
+Plan plan_of(int n, int B, int H, int Hkv, long capacity, bool fp8)
 {
-    const long rows = (long)(H / Hkv) * n, heads = (long)B * Hkv;
+    const long rows = (long)(H / Hkv) * n, heads = (long)B * Hkv, blocks = heads * ((rows + 31) / 32), tiles = capacity / 64;
+    const bool few = rows <= kFewRows;               // no two workgroups read the same keys: memory bounds them
     Plan p;
-    p.rg = rows > 32 ? 2 : 1;
+    // Two row blocks per workgroup read the cache once for both, but the workgroups are half as many and their waves wait for each other.
+    // 256 compute units hold two workgroups each, so that up to 512 of one block run at once; bf16 pages wait for memory sooner.  us with
+    // one / two row blocks.  e4m3: 128 blocks, 2048 positions 15.1 / 18.9; 512, 2048 24.7 / 28.5; 1024, 2048 44.5 / 40.2.  bf16: 256 blocks, 1024
+    // positions 14.6 / 20.0; 320, 2048 28.8 / 30.5; 512, 4096 75.6 / 58.0; 1024, 1024 59.6 / 47.3.
+    p.rg = !few && blocks > (fp8 ? 512 : 256) ? 2 : 1;
     p.row_tiles = (rows + 32 * p.rg - 1) / (32 * p.rg);
     const long base = heads * p.row_tiles;
-    // The merge's launch costs some 2 us, a wave's tile 1.1 (e4m3), so short streams are not split; longer ones down to a tile for each wave
-    // of a workgroup, until there is one workgroup per compute unit.  us with 1 / 2 / 4 / 8 / 16 splits, one token, 32/8 heads, e4m3:
-    // 512 positions 6.5 / 8.3 / 8.2 / - / -, 1024 8.8 / 9.3 / 8.2 / - / -, 4096 22.9 / 16.3 / 11.5 / 9.8 / 9.4; four sequences 4096 25.2 / 18.1 /
-    // 13.4 / 12.2 / 13.9; sixteen 27.6 / 26.8 / 28.0 / 30.9 / 35.6.
-    long s = (256 + base - 1) / base;
-    const long most = capacity < 1024 ? 1 : capacity / (64 * kSplitTiles);
-    if (s > most) s = most;
+    // Splits: the merge's launch costs some 2 us and each split a state per row, written and read again, for 32 rows as many bytes as a
+    // tile of 64 keys; so up to one workgroup per compute unit, and up to two where arithmetic bounds them and the splits stay long.  us with
+    // 1 / 2 / 4 / 8 / 16 splits, 32/8 heads, e4m3.  One token: one sequence, 512 positions 6.3 / 8.0 / 8.0 / - / -, 1024 8.6 / 8.9 / 8.0 / - / -,
+    // 4096 22.2 / 15.8 / 11.3 / 9.4 / 9.0; four 4096 25.1 / 18.0 / 13.2 / 11.9 / 13.7; 24 4096 35.1 / 41.0 / 39.6 / 42.1 / -.  64 tokens: one sequence
+    // 1024 9.9 / 11.2 / 11.1 / - / -, 2048 14.6 / 13.4 / 12.3 / 15.1 / -, 16384 83.1 / 48.2 / 29.4 / 28.8 / 33.8; three 2048 16.1 / 20.7 / 24.3 /
+    // 30.1 / -, 8192 46.7 / 42.2 / 39.9 / 45.3 / -; four 2048 16.2 / 22.6 / 26.5 / 35.9 / -, 8192 46.8 / 48.4 / 51.3 / 58.5 / -.
+    auto up_to = [&](long want, long least) { return want < tiles / least ? want : tiles / least; };
+    long s = p.rg == 1 ? up_to(256 / base, few ? kSplitTiles : kSplitTilesMany) : 1;
+    if (!few) {
+        const long twice = up_to(512 / base, 4 * kSplitTilesMany);
+        s = s > twice ? s : twice;
+    }
+    if (capacity < (few ? 1024 : 2048)) s = 1;
     if (s > kMaxSplits) s = kMaxSplits;
     p.splits = s < 1 ? 1 : (int)s;
     p.wgs = base * p.splits;
@@ -623,16 +719,15 @@ template <int D, bool FP8> hipError_t attend(const PagedAttnArgs &a, const Paged
 
 size_t paged_attention_workspace_bytes(int n, int B, int H, int Hkv, int d, long capacity, bool fp8)
 {
-    (void)fp8;
-    const Plan p = plan_of(n, B, H, Hkv, capacity);
+    const Plan p = plan_of(n, B, H, Hkv, capacity, fp8);
     return p.splits <= 1 ? 0 : (size_t)B * H * n * (size_t)p.splits * (size_t)(d + 2) * sizeof(float);
 }
 
 hipError_t launch_attention_paged(const PagedAttnArgs &a, hipStream_t stream)
 {
-    const Plan p = plan_of(a.n, a.B, a.H, a.Hkv, (long)a.max_pages << a.page_log2);
-    const size_t rows = (size_t)a.B * a.H * a.n;
     const bool fp8 = a.k_scale != nullptr;
+    const Plan p = plan_of(a.n, a.B, a.H, a.Hkv, (long)a.max_pages << a.page_log2, fp8);
+    const size_t rows = (size_t)a.B * a.H * a.n;
     const PagedTail tail{static_cast<const uint8_t *>(a.Q), a.k_scale, a.v_scale, static_cast<uint8_t *>(a.O), static_cast<float *>(a.workspace),
                          static_cast<float *>(a.workspace) + rows * p.splits * a.d, (float)(1.4426950408889634 / __builtin_sqrt((double)a.d))};
     const unsigned shape = (unsigned)p.row_tiles << 8 | (unsigned)(p.splits - 1) << 2 | (unsigned)(a.page_log2 - 4);

@@ -86,6 +86,30 @@ def test_long_sequences_are_split(cache, B, H, Hkv, n):
     _check(B, H, Hkv, n, 128, 64, cache, lens)
 
 
+@pytest.mark.parametrize("d,P", [(64, 16), (64, 128), (128, 32), (128, 64)])
+@pytest.mark.parametrize("cache", ["fp8", "bf16"])
+def test_many_row_blocks(cache, d, P):
+    # more than 512 blocks of 32 rows, every one of them short of a whole one: lengths around a tile's and a page's end, and none
+    _check(6, 48, 48, 43, d, P, cache, [0, 1, 63, 64, 65, 200], per=-(-200 // P), poison=True, seed=d + P)
+
+
+@pytest.mark.parametrize("n,lens", [(43, [4096, 130]), (33, [4095, 0])])
+def test_many_row_blocks_and_splits(n, lens):
+    # the pages of a long sequence are some few that recur: what its table says counts, not which page it is
+    rng = np.random.default_rng(n)
+    assert dd.dd_paged_attention_workspace_bytes(n, 2, 70, 70, 64, 128, 32, dd.BF16) > 0
+    _check(2, 70, 70, n, 64, 128, "bf16", lens, per=32, table=rng.integers(0, 12, (2, 32)))
+
+
+@pytest.mark.parametrize("cache", ["fp8", "bf16"])
+@pytest.mark.parametrize("n", [2, 40])
+def test_lengths_around_the_splits_ends(cache, n):
+    # a capacity of 2304 positions, sequences whose shares end exactly at a split's end, one key before it and one behind it
+    lens = [2304, 2303, 256, 255, 257, 513, 1024, 1]
+    assert dd.dd_paged_attention_workspace_bytes(n, len(lens), 2, 1, 128, 32, 72, dd.FP8_E4M3) > 0
+    _check(len(lens), 2, 1, n, 128, 32, cache, lens, per=72)
+
+
 def test_capacity_beyond_the_lengths():
     # a table for 100000 positions, sequences of a few: shared out by their own lengths
     (Q, Kc, Vc, table, lens, ks, vs), o = _case(2, 8, 2, 1, 128, 64, "fp8", [100, 700], per=11)
