@@ -275,13 +275,15 @@ int dd_cache_insert_rows(void *Kc, void *Vc, const void *Krows, const void *Vrow
  *         stay as they are; rot_dim == 0 (inv_freq == NULL): no rotation
  * and K likewise with k_weight.
  *   Q  element (b,h,i,c) at q_batch*b + q_head*h + q_row*i + c (strides in elements, >= 0; an axis of one entry may have
- *      any; otherwise a multiple of 16 bytes, the last element less than 2^40 elements from the first); dtype DD_F32 or DD_BF16.  So a view of a fused projection's output serves.
+ *      any; otherwise a multiple of 16 bytes, the last element less than 2^40 elements from the first); dtype DD_F32 or
+ *      DD_BF16.  So a view of a fused projection's output serves.
  *   K  the same with Hkv heads and its own strides; K == NULL (then Ko == NULL): queries only
- *   Qo [B,H,n,d], Ko [B,Hkv,n,d]  dense, dtype.  Qo may be Q (and Ko may be K) where that is dense itself; any other overlap of an
- *      output with an input, or of the two outputs, is DD_ERR_SHAPE
+ *   Qo [B,H,n,d], Ko [B,Hkv,n,d]  dense, dtype.  Qo may be Q (and Ko may be K) where that is dense itself; any other overlap of
+ *      an output with Q or K, or of the two outputs, is DD_ERR_SHAPE
  *   q_weight, k_weight [d] dtype, 16-byte aligned; each may be NULL; with either, eps must be > 0 and finite
  *   inv_freq [rot_dim/2] f32; rot_dim a multiple of 16, at most d        positions [B*n] i32, any value
- * d in {64, 128}; B, H >= 1, Hkv >= 1 with K; n >= 0 (0: a no-op); B*n < 2^31, B*H*n*d and B*Hkv*n*d < 2^40.
+ * d in {64, 128}; B, H >= 1, Hkv >= 1 with K; n >= 0 (0: a no-op); B*n < 2^31, B*n*d < 2^36, B*H*n*d and
+ * B*Hkv*n*d < 2^40.
  * Arithmetic: fp32, angles reduced in fp64 (so that far positions turn by the right angle), results rounded once.
  * Errors: DD_ERR_NULL, DD_ERR_SHAPE, DD_ERR_DTYPE, DD_ERR_ALIGN, DD_ERR_LAUNCH.
  */
@@ -309,11 +311,13 @@ int dd_qk_norm_rope(const void *Q, int64_t q_batch, int64_t q_head, int64_t q_ro
  * that gets rows, keys and values each for themselves: a = max |x| over those rows, s = 2^e with the least e >= -126 such that
  * a <= 448 * 2^e; if the page holds other positions below kv_lens[b], s = max(s, its scale so far), and where that grows their
  * codes become rne(code * old / s); rows become rne(x / s) (to nearest, ties to even).  Positions that are neither written
- * nor below kv_lens[b] are left as they are.  A scale is positive and finite wherever the page holds positions.
- * The pages that a call writes must be distinct over the sequences (else which rows and which scale win is unspecified);
- * pages that are only read later (a shared prefix) may be shared.  K and V must not overlap the cache (not checked).  The
- * caller owns kv_lens: the call does not write it.
- * d in {64, 128}; B, Hkv, num_pages, max_pages >= 1; n >= 0 (0: a no-op); max_pages*page_size < 2^30, num_pages*Hkv*page_size*d < 2^40.
+ * nor below kv_lens[b] are left as they are.  A scale is positive, finite and normal (not subnormal) wherever the page holds
+ * positions; rows for DD_FP8_E4M3 pages are finite (one that is not spoils its own page and head, no other).
+ * The pages that a call writes must be distinct (else which rows and which scale win is unspecified); pages that are only read
+ * later (a shared prefix) may be shared.  Kc and Vc overlap neither each other nor K or V (DD_ERR_SHAPE).  The caller owns
+ * kv_lens: the call does not write it.
+ * d in {64, 128}; B, Hkv, num_pages, max_pages >= 1; n >= 0 (0: a no-op); max_pages*page_size < 2^30, num_pages*Hkv*page_size*d
+ * < 2^40, B*Hkv*n*d < 2^40, B*(n + 2 page_size)*d < 2^34.
  * Errors: DD_ERR_NULL (scales are required with DD_FP8_E4M3), DD_ERR_SHAPE, DD_ERR_DTYPE, DD_ERR_ALIGN, DD_ERR_LAUNCH.
  */
 int dd_paged_cache_append(void *Kc, void *Vc, float *k_scale, float *v_scale,
@@ -331,13 +335,15 @@ int dd_paged_cache_append(void *Kc, void *Vc, float *k_scale, float *v_scale,
  * with K_j, V_j of kv head h*Hkv/H as the cache holds them; the block's own rows take part by being appended first.
  * kv_lens[b] is clamped to [0, max_pages*page_size]; positions whose page is not in [0, num_pages) take no part; a sequence
  * without a position that does gets zeros.  Slots that hold no position may hold anything, NaN included.
- *   Q, O [B,H,n,d] DD_BF16, dense;  cache_dtype DD_BF16 or DD_FP8_E4M3 (then k_scale and v_scale are required, positive and finite
- *   wherever a page holds positions)
+ *   Q, O [B,H,n,d] DD_BF16, dense;  O overlaps neither Q nor the cache (DD_ERR_SHAPE);  cache_dtype DD_BF16 or DD_FP8_E4M3 (then
+ *   k_scale and v_scale are required; wherever a page holds positions they are positive, finite, normal and at most 2^119)
  * Arithmetic: matrix cores with fp32 accumulation, e4m3 codes decoded exactly to bf16, k_scale in the exponent's factor, fp32
- * online softmax, weights (times v_scale) rounded to bf16 before the PV product.
+ * online softmax, weights (times the significand of v_scale, in [1, 2)) rounded to bf16 before the PV product.
  * The key range is split over workgroups where those are few; the partial states live in `workspace`.  A capacity
  * max_pages*page_size far above the lengths costs workspace, not time: a sequence's own keys are shared out.
- * d in {64, 128}; H % Hkv == 0; B, H, Hkv, num_pages, max_pages >= 1; n >= 0 (0: a no-op); sizes as above, B*H*n < 2^30.
+ * d in {64, 128}; H % Hkv == 0; B, H, Hkv, num_pages, max_pages >= 1; n >= 0 (0: a no-op); max_pages*page_size < 2^30,
+ * num_pages*Hkv*page_size*d < 2^40, B*H*n < 2^30, B*Hkv*ceil(n*H/Hkv / 32) < 2^24.
+ * Errors: as above, and DD_ERR_WORKSPACE.
  */
 int dd_paged_attention(const void *Q, const void *Kc, const void *Vc, const float *k_scale, const float *v_scale,
                        const int32_t *block_table, const int32_t *kv_lens, void *O,

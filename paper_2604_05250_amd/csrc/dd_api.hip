@@ -448,7 +448,8 @@ int dd_qk_norm_rope(const void *Q, int64_t q_batch, int64_t q_head, int64_t q_ro
     if (!Q || !Qo || (K == nullptr) != (Ko == nullptr)) return DD_ERR_NULL;
     if (B < 1 || H < 1 || n < 0 || (K && Hkv < 1) || (d != 64 && d != 128)) return DD_ERR_SHAPE;
     const int kv = K ? Hkv : 0, eb = dtype == DD_BF16 ? 2 : 4;
-    if ((double)B * n >= 2147483648.0 || (double)B * (H > kv ? H : kv) * n * d >= 1099511627776.0) return DD_ERR_SHAPE;
+    // (a thread has 16 elements of a token, and a launch fewer than 2^32 threads along an axis)
+    if ((double)B * n >= 2147483648.0 || (double)B * n * d >= 68719476736.0 || (double)B * (H > kv ? H : kv) * n * d >= 1099511627776.0) return DD_ERR_SHAPE;
     int rc = check_rotation(q_weight ? q_weight : K ? k_weight : nullptr, eps, inv_freq, rot_dim, d);
     if (rc != DD_OK) return rc;
     const int64_t qs[3] = {q_batch, q_head, q_row}, ks[3] = {k_batch, k_head, k_row};
@@ -517,7 +518,13 @@ int dd_paged_cache_append(void *Kc, void *Vc, float *k_scale, float *v_scale,
     if ((rc = check_strides(ks, extent, eb)) != DD_OK || (rc = check_strides(vs, extent, eb)) != DD_OK) return rc;
     if (misaligned16(K) || misaligned16(V) || ((reinterpret_cast<uintptr_t>(kv_lens) | reinterpret_cast<uintptr_t>(n_rows)) & 3u) != 0) return DD_ERR_ALIGN;
     const int log2 = page_log2_of(page_size);
-    if (dd::page_append_wgs(n, B, Hkv, log2) >= (1L << 31)) return DD_ERR_SHAPE;
+    // (2 B pages (page_size d / 16) threads, for up to n + 2 page_size positions' pages: fewer than 2^31)
+    if ((double)B * ((double)n + 2.0 * page_size) * d >= 17179869184.0) return DD_ERR_SHAPE;
+    const uintptr_t cache_bytes = (uintptr_t)num_pages * Hkv * page_size * d * (cache_dtype == DD_BF16 ? 2 : 1);
+    const uintptr_t k_reach = reach(ks, extent, d, eb), v_reach = reach(vs, extent, d, eb);
+    if (overlap(Kc, cache_bytes, Vc, cache_bytes) || overlap(Kc, cache_bytes, K, k_reach) || overlap(Kc, cache_bytes, V, v_reach) ||
+        overlap(Vc, cache_bytes, K, k_reach) || overlap(Vc, cache_bytes, V, v_reach))
+        return DD_ERR_SHAPE;
     dd::PageAppendArgs a;
     auto side = [&](dd::PageAppendSide &s, const void *x, void *cache, float *scale, const int64_t *st) {
         s.x = x; s.cache = cache; s.scale = cache_dtype == DD_FP8_E4M3 ? scale : nullptr;
@@ -533,11 +540,18 @@ int dd_paged_cache_append(void *Kc, void *Vc, float *k_scale, float *v_scale,
     return e == hipSuccess ? DD_OK : DD_ERR_LAUNCH;
 }
 
+// rows, and row blocks of 32 of each key/value head, that one launch of 256 threads for a row block can have
+static bool attends_in_one_launch(int n, int B, int H, int Hkv)
+{
+    const double rows = (double)(H / Hkv) * n;
+    return rows * B * Hkv < 1073741824.0 && __builtin_ceil(rows / 32) * B * Hkv < 16777216.0;
+}
+
 size_t dd_paged_attention_workspace_bytes(int n, int B, int H, int Hkv, int d, int page_size, int max_pages, dd_dtype cache_dtype)
 {
     if (n < 1 || B < 1 || H < 1 || Hkv < 1 || H % Hkv != 0 || (d != 64 && d != 128) || max_pages < 1 || page_log2_of(page_size) < 0) return 0;
     if (cache_dtype != DD_BF16 && cache_dtype != DD_FP8_E4M3) return 0;
-    if ((double)max_pages * page_size >= 1073741824.0 || (double)B * H * n >= 1073741824.0) return 0;
+    if ((double)max_pages * page_size >= 1073741824.0 || !attends_in_one_launch(n, B, H, Hkv)) return 0;
     return dd::paged_attention_workspace_bytes(n, B, H, Hkv, d, (long)max_pages * page_size, cache_dtype == DD_FP8_E4M3);
 }
 
@@ -551,11 +565,13 @@ int dd_paged_attention(const void *Q, const void *Kc, const void *Vc, const floa
     if (H < 1 || H % Hkv != 0) return DD_ERR_SHAPE;
     if (n == 0) return DD_OK;
     if (!Q || !O) return DD_ERR_NULL;
-    if ((double)B * H * n >= 1073741824.0) return DD_ERR_SHAPE;
+    if (!attends_in_one_launch(n, B, H, Hkv)) return DD_ERR_SHAPE;
     if (misaligned16(Q) || misaligned16(O)) return DD_ERR_ALIGN;
     const bool fp8 = cache_dtype == DD_FP8_E4M3;
     rc = check_workspace(workspace, workspace_bytes, dd::paged_attention_workspace_bytes(n, B, H, Hkv, d, (long)max_pages * page_size, fp8));
     if (rc != DD_OK) return rc;
+    const uintptr_t rows_bytes = (uintptr_t)B * H * n * d * 2, cache_bytes = (uintptr_t)num_pages * Hkv * page_size * d * (fp8 ? 1 : 2);
+    if (overlap(O, rows_bytes, Q, rows_bytes) || overlap(O, rows_bytes, Kc, cache_bytes) || overlap(O, rows_bytes, Vc, cache_bytes)) return DD_ERR_SHAPE;
     dd::PagedAttnArgs a;
     a.Q = Q; a.Kc = Kc; a.Vc = Vc; a.O = O;
     a.k_scale = fp8 ? k_scale : nullptr; a.v_scale = fp8 ? v_scale : nullptr;

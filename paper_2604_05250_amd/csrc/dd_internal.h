@@ -184,7 +184,6 @@ struct PageAppendArgs {
     float eps = 0;
     int pages_per_seq = 0, per_wg = 0, head_groups = 0;      // set by the launcher
 };
-long page_append_wgs(int n, int B, int Hkv, int page_log2);  // the most workgroups that a call can take
 hipError_t launch_page_append(PageAppendArgs a, int d, bool rows_bf16, bool fp8, hipStream_t stream);
 
 // ---- attention over a paged cache (attention_paged.hip) ----------------------------

@@ -469,12 +469,6 @@ hipError_t launch_norm_rotate(NormRotateArgs a, int d, bool bf16, hipStream_t st
     return d == 128 ? norm_rotate<F32, 128>(a, grid, stream) : norm_rotate<F32, 64>(a, grid, stream);
 }
 
-long page_append_wgs(int n, int B, int Hkv, int page_log2)
-{
-    const long page = 1L << page_log2;
-    return 2L * B * Hkv * ((n + page - 2) / page + 1);
-}
-
 hipError_t launch_page_append(PageAppendArgs a, int d, bool rows_bf16, bool fp8, hipStream_t stream)
 {
     const long page = 1L << a.page_log2;

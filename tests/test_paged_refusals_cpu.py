@@ -57,6 +57,28 @@ def test_append_is_refused(want, kw):
     assert append(**kw) == want
 
 
+@pytest.mark.parametrize("kw", [
+    dict(Vc=FAKE), dict(Vc=FAKE + 9 * 2 * 16 * 64 - 16), dict(K=FAKE), dict(V=FAKE + 9 * 2 * 16 * 64 - 16), dict(K=2 * FAKE + 64), dict(V=2 * FAKE),
+    dict(K=2 * FAKE - (2 * 2 * 5 * 64 * 2 - 16))])
+def test_append_refuses_rows_in_the_cache(kw):
+    assert append(**kw) == SHAPE
+
+
+def test_launches_have_fewer_than_2_32_threads():
+    big = 1 << 29
+    assert rope(B=1, n=big, d=128, rot=128, K=None, Ko=None, H=1, q=(0, 0, 128), Qo=1 << 50) == SHAPE
+    assert append(B=1, n=1 << 27, d=128, Hkv=1, k=(0, 0, 128), v=(0, 0, 128)) == SHAPE
+    assert append(B=1 << 22, n=1, d=128, P=128, Hkv=1, k=(128, 0, 0), v=(128, 0, 0)) == SHAPE
+    assert attend(B=1 << 21, H=8, Hkv=8) == SHAPE and attend(B=1, H=1, Hkv=1, n=1 << 29) == SHAPE
+    assert dd.dd_paged_attention_workspace_bytes(1, 1 << 21, 8, 8, 128, 64, 64, dd.BF16) == 0
+
+
+@pytest.mark.parametrize("kw", [
+    dict(O=1 << 40), dict(O=(1 << 40) + 8 * 128 * 2 - 16), dict(O=1 << 30), dict(O=(1 << 30) + 99 * 2 * 64 * 128 - 16), dict(O=(1 << 31) - (8 * 128 * 2 - 16))])
+def test_attention_refuses_an_output_over_its_inputs(kw):
+    assert attend(Q=1 << 40, Kc=1 << 30, Vc=1 << 31, ws=1 << 45, wsn=1 << 40, **kw) == SHAPE
+
+
 def test_append_without_rows_does_nothing():
     assert append(n=0) == 0 and append(n=0, K=None, V=None) == 0
 
