@@ -149,6 +149,25 @@ def test_zero_rows_and_page_after_page():
     assert np.array_equal(np.concatenate([got[1, 0], got[0, 0]])[3:23], host(rows)[0, 0])
 
 
+def test_a_row_that_is_not_finite_stays_in_its_page_and_head():
+    import torch
+    rng = np.random.default_rng(3)
+    x, _ = rounded(rng.standard_normal((2, 2, 40, 64)), torch.bfloat16)
+    y = x.clone()
+    y[0, 1, 20, 3], y[1, 0, 39, 0] = float("inf"), float("nan")             # pages 1 and 2 of their sequences
+    table, caches = ints([[0, 1, 2], [3, 4, 5]]), []
+    for rows in (x, y):
+        Kc, Vc = torch.zeros((6, 2, 16, 64), dtype=torch.uint8, device="cuda"), torch.zeros((6, 2, 64, 16), dtype=torch.uint8, device="cuda")
+        ks, vs = torch.ones((6, 2), device="cuda"), torch.ones((6, 2), device="cuda")
+        dd.dd_paged_cache_append(Kc, Vc, rows, rows, table, ints([0, 0]), k_scale=ks, v_scale=vs)
+        caches.append((Kc, Vc, ks, vs))
+    others = torch.ones((6, 2), dtype=torch.bool, device="cuda")
+    others[1, 1] = others[5, 0] = False
+    for a, b in zip(*caches):
+        assert torch.equal(a[others], b[others])
+    assert all(s.isfinite().all() and (s > 0).all() for s in caches[1][2:])
+
+
 def test_no_rows():
     import torch
     Kc = torch.zeros((2, 1, 16, 64), dtype=torch.bfloat16, device="cuda")

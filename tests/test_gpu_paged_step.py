@@ -149,6 +149,41 @@ def test_graph_replays_match_eager_calls():
         assert all(torch.equal(a, b) for a, b in zip(want, (O, s.Kc, s.Vc, s.ks, s.vs))), f"replay {rep} on other inputs"
 
 
+@pytest.mark.parametrize("cache", ["fp8", "bf16"])
+def test_two_graphs_at_once(cache):
+    # two captured steps whose attention is split, each with a scratch of its own, replayed on two streams between eager calls on a third
+    import torch
+    served = [Served(B=1, prompt=2300 + 700 * k, bl=3, steps=1, seed=k, cache=cache) for k in range(2)]
+    graphs, want = [], []
+    for s in served:
+        s.append(s.rows["prompt"], ints([0]))
+        s.args, s.O = (ints(s.lens), ints(s.lens + 3), ints(s.lens[:, None] + np.arange(3))), torch.zeros((1, s.H, 3, s.d), dtype=torch.bfloat16, device="cuda")
+        assert dd.dd_paged_attention_workspace_bytes(3, 1, s.H, s.Hkv, s.d, 64, s.table.shape[1], dd.FP8_E4M3 if cache == "fp8" else dd.BF16) > 0
+
+        def step(s=s, O=s.O):
+            s.append(s.rows[0], s.args[0])
+            s.attend(s.rows[0], s.args[2], s.args[1], O=O)
+
+        step()
+        torch.cuda.synchronize()
+        want.append(s.O.clone())
+        graphs.append(capture_step(step))
+    streams = [torch.cuda.Stream() for _ in graphs]
+    for rep in range(5):
+        for s in served:
+            s.O.zero_()
+        torch.cuda.synchronize()
+        for graph, stream in zip(graphs, streams):
+            with torch.cuda.stream(stream):
+                graph.replay()
+        q = dd.dd_qk_norm_rope(served[0].split(served[0].rows[0])[0], q_weight=served[0].qw, inv_freq=served[0].f, positions=served[0].args[2])[0]
+        eager = dd.dd_paged_attention(q, served[1].Kc, served[1].Vc, served[1].table, ints([1999]), k_scale=served[1].ks, v_scale=served[1].vs)
+        torch.cuda.synchronize()
+        assert all(torch.equal(s.O, w) for s, w in zip(served, want)), f"replay {rep}"
+        again = dd.dd_paged_attention(q, served[1].Kc, served[1].Vc, served[1].table, ints([1999]), k_scale=served[1].ks, v_scale=served[1].vs)
+        assert torch.equal(eager, again)
+
+
 def test_streams_side_by_side():
     import torch
     batches = [Served(B=1, prompt=900, bl=4, steps=1, seed=k) for k in range(3)]

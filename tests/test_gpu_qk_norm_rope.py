@@ -48,6 +48,20 @@ def test_parity(dtype, B, H, Hkv, n, d, rot, norm, interleaved):
     _check(B, H, Hkv, n, d, dtype, rot, norm, interleaved)
 
 
+@pytest.mark.parametrize("which", ["queries", "keys"])
+def test_one_side_is_normed(which):
+    # the other side's rows are rotated as they are, in the same bits as without any weight
+    import torch
+    rng = np.random.default_rng(4)
+    x, x64 = rounded(rng.standard_normal((2, 3, 9, 64)) * 3, torch.bfloat16)
+    w, w64 = rounded(1 + 0.2 * rng.standard_normal(64), torch.bfloat16)
+    f, pos = _freq(64), np.broadcast_to(np.arange(9), (2, 9))
+    both = dd.dd_qk_norm_rope(x, x, q_weight=w if which == "queries" else None, k_weight=w if which == "keys" else None, inv_freq=dev(f))
+    normed, plain = both if which == "queries" else both[::-1]
+    assert torch.equal(plain, dd.dd_qk_norm_rope(x, inv_freq=dev(f))[0])
+    assert_rows(host(normed), paged.norm_rope(x64, w64, float(np.float32(1e-6)), f, pos, False), 2.0 ** -8, ROW_FAST)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_far_and_negative_positions(dtype):
     import torch
