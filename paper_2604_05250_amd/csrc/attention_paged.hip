@@ -12,11 +12,11 @@
 // sequences x 64 rows, 32/8 heads, 2048 e4m3 keys 51 us, with all loads from the nearest cache 50, with none 37; by LDS 43, in three
 // stages 40).
 // A workgroup's four waves are one row block x 4 streams of keys, each with a state (reference, sum, O) of its own and a tile of its
-// own in LDS, whose K is asked for again as soon as it is in registers, and V likewise; or two blocks x 2 streams with doubled tiles
-// that two waves share (as above 44.5 and 40.2 us; four blocks x two streams of eight waves 42.9).  The next keys' scores are computed beside
-// these keys' weights, for e4m3 pages the last keys' output beside both, so that the matrix cores and the vector units have work at the
-// same time; neither then idles for long, and the clock gives way to their load.  The states are merged through LDS, the key range is
-// split over workgroups where those are few, and the splits' states are merged by a second kernel.
+// own in LDS, whose K is asked for again as soon as it is in registers, and V likewise; or two blocks x 2 streams or four x 1, with
+// doubled tiles that two or four waves share (as above 44.5, 40.2 and 49.0 us; four blocks x 2 streams in eight waves 42.9).  The next
+// keys' scores are computed beside these keys' weights, for e4m3 pages the last keys' output beside both, so that the matrix cores and
+// the vector units have work at the same time; neither then idles for long, and the clock gives way to their load.  The states are
+// merged through LDS, the key range is split over workgroups where those are few, and the splits' states are merged by a second kernel.
 // e4m3 codes become bf16 exactly in registers.  k_scale goes into the factor of the exponent; of v_scale the power of two goes into the
 // decoding of V, which is exact (bf16 for its range: scales span 2^-126 .. 2^119), and the rest, 1 where this library made the scale,
 // into the exponent.  Weights are rounded to bf16 (2^-8 of each at most, as the result is), their sum is the one of the rounded ones.
@@ -556,23 +556,18 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(DD_PAGED_HEAD, Paged
     }
     l += halves_other(l);
 
-    if constexpr (STREAMS == 1) {                    // a row is in one wave: four head dims of it at a time
+    if constexpr (STREAMS == 1) {                    // a row is in one wave, four head dims of it at a time (and its keys are not split)
         if (v_first + l32 >= rows_total) return;
         const size_t row = row_base + v_first + l32;
-        const float inv = sh.used > 1 ? 1.0f : l > 0 ? 1.0f / l : 0.0f;              // no key at all: zeros
+        const float inv = l > 0 ? 1.0f / l : 0.0f;   // no key at all: zeros
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int d0 = dt * 32 + 8 * i + 4 * hh;
                 const float x0 = o[dt][4 * i] * inv, x1 = o[dt][4 * i + 1] * inv, x2 = o[dt][4 * i + 2] * inv, x3 = o[dt][4 * i + 3] * inv;
-                if (sh.used <= 1) *reinterpret_cast<uint2 *>(a.O + (row * D + d0) * 2) = make_uint2(pack_bf16(x0, x1), pack_bf16(x2, x3));
-                else *reinterpret_cast<float4 *>(a.part_o + (row * splits + sp) * D + d0) = make_float4(x0, x1, x2, x3);
+                *reinterpret_cast<uint2 *>(a.O + (row * D + d0) * 2) = make_uint2(pack_bf16(x0, x1), pack_bf16(x2, x3));
             }
-        if (sh.used > 1 && hh == 0) {
-            a.part_ml[(row * splits + sp) * 2] = m;
-            a.part_ml[(row * splits + sp) * 2 + 1] = l;
-        }
     } else {
         // ---- the streams' states, merged: every thread finishes eight head dims of a row at a time
         float (*const o_sh)[32][PITCH] = reinterpret_cast<float (*)[32][PITCH]>(lds);
@@ -675,11 +670,14 @@ Plan plan_of(int n, int B, int H, int Hkv, long capacity, bool fp8)
     const long rows = (long)(H / Hkv) * n, heads = (long)B * Hkv, blocks = heads * ((rows + 31) / 32), tiles = capacity / 64;
     const bool few = rows <= kFewRows;               // no two workgroups read the same keys: memory bounds them
     Plan p;
-    // Two row blocks per workgroup read the cache once for both, but the workgroups are half as many and their waves wait for each other.
+    // Two or four row blocks per workgroup read the cache once for all, but the workgroups are fewer and their waves wait for each other.
     // 256 compute units hold two workgroups each, so that up to 512 of one block run at once; bf16 pages wait for memory sooner.  us with
-    // one / two row blocks.  e4m3: 128 blocks, 2048 positions 15.1 / 18.9; 512, 2048 24.7 / 28.5; 1024, 2048 44.5 / 40.2.  bf16: 256 blocks, 1024
-    // positions 14.6 / 20.0; 320, 2048 28.8 / 30.5; 512, 4096 75.6 / 58.0; 1024, 1024 59.6 / 47.3.
-    p.rg = !few && blocks > (fp8 ? 512 : 256) ? 2 : 1;
+    // one / two / four row blocks.  e4m3: 128 blocks, 2048 positions 15.1 / 18.9 / -; 512, 2048 25.6 / 28.5 / 48.2; 1024, 2048 46.3 / 41.6 / 49.0; 1536,
+    // 2048 - / 65.3 / 67.2; 1920, 2048 - / 80.6 / 75.4; 8192, 2048 338 / 301 / 276.  bf16: 256 blocks, 1024 positions 14.6 / 20.0 / -; 320, 2048 28.8 /
+    // 30.5 / -; 512, 4096 76.1 / 68.6 / 104; 1024, 2048 76.7 / 51.1 / 57.6; 1152, 2048 - / 74.9 / 70.4; 2048, 1024 80.1 / 56.6 / 50.2.  Where a
+    // workgroup's last rows are missing, their work is not: 320 rows of 128 heads, 700 positions - / 32.7 / 34.5.
+    const bool full = (rows + 127) / 128 * 128 * 8 <= rows * 9;
+    p.rg = few || blocks <= (fp8 ? 512 : 256) ? 1 : full && blocks > (fp8 ? 1792 : 1024) ? 4 : 2;
     p.row_tiles = (rows + 32 * p.rg - 1) / (32 * p.rg);
     const long base = heads * p.row_tiles;
     // Splits: the merge's launch costs some 2 us and each split a state per row, written and read again, for 32 rows as many bytes as a
@@ -690,7 +688,7 @@ Plan plan_of(int n, int B, int H, int Hkv, long capacity, bool fp8)
     // 30.1 / -, 8192 46.7 / 42.2 / 39.9 / 45.3 / -; four 2048 16.2 / 22.6 / 26.5 / 35.9 / -, 8192 46.8 / 48.4 / 51.3 / 58.5 / -.
     auto up_to = [&](long want, long least) { return want < tiles / least ? want : tiles / least; };
     long s = p.rg == 1 ? up_to(256 / base, few ? kSplitTiles : kSplitTilesMany) : 1;
-    if (!few) {
+    if (!few && p.rg < 4) {
         const long twice = up_to(512 / base, 4 * kSplitTilesMany);
         s = s > twice ? s : twice;
     }
@@ -707,7 +705,7 @@ template <int D, bool FP8, int NT, bool ONE> hipError_t attend(const PagedAttnAr
         return launch(kernel, dim3((unsigned)p.wgs), dim3(256), stream, a.table, a.kv_lens, static_cast<const uint8_t *>(a.Kc), static_cast<const uint8_t *>(a.Vc), a.Hkv,
                       (a.H / a.Hkv) * a.n, a.num_pages, a.max_pages, (unsigned)p.wgs, shape, tail);
     };
-    return p.rg == 1 ? run(attn_paged_kernel<D, FP8, NT, ONE, 1>) : run(attn_paged_kernel<D, FP8, NT, ONE, 2>);
+    return p.rg == 1 ? run(attn_paged_kernel<D, FP8, NT, ONE, 1>) : p.rg == 2 ? run(attn_paged_kernel<D, FP8, NT, ONE, 2>) : run(attn_paged_kernel<D, FP8, NT, ONE, 4>);
 }
 template <int D, bool FP8> hipError_t attend(const PagedAttnArgs &a, const PagedTail &tail, const Plan &p, unsigned shape, hipStream_t stream)
 {

@@ -93,6 +93,13 @@ def test_many_row_blocks(cache, d, P):
     _check(6, 48, 48, 43, d, P, cache, [0, 1, 63, 64, 65, 200], per=-(-200 // P), poison=True, seed=d + P)
 
 
+@pytest.mark.parametrize("d,P", [(64, 32), (64, 16), (128, 128), (128, 16)])
+@pytest.mark.parametrize("cache", ["fp8", "bf16"])
+def test_many_more_row_blocks(cache, d, P):
+    # 250 rows of each of 230 key/value heads, 1840 blocks of which every eighth is short of a whole one
+    _check(5, 92, 46, 125, d, P, cache, [0, 1, 65, 128, 190], per=-(-190 // P), poison=True, seed=d + P)
+
+
 @pytest.mark.parametrize("n,lens", [(43, [4096, 130]), (33, [4095, 0])])
 def test_many_row_blocks_and_splits(n, lens):
     # the pages of a long sequence are some few that recur: what its table says counts, not which page it is
