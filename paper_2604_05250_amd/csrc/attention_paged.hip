@@ -126,6 +126,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(DD_PAGED_HEAD, Paged
     constexpr int KVB = STREAMS * BUFS * (KB + VB), MERGEB = STREAMS == 1 ? 0 : kWaves * 32 * PITCH * 4;
     static_assert(TILE * EB == 64, "a head dim's keys of a tile are four pieces");
     static_assert(NK % RG == 0 && NV % RG == 0, "the waves of a stream share its loads out");
+    static_assert(RG == 1 || (NK + NV) / RG <= 8, "eight loads are asked for in a round");
     __shared__ __attribute__((aligned(1024))) uint8_t lds[KVB > MERGEB ? KVB : MERGEB];
 
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
@@ -194,41 +195,49 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(DD_PAGED_HEAD, Paged
     const unsigned k_off[2] = {(unsigned)(k_key * ROWB + (k_piece ^ sw(k_key, 0)) * 16), (unsigned)(k_key * ROWB + (k_piece ^ sw(k_key, 1)) * 16)};
     const int v_piece = lane % 4 ^ (lane >> 3 & 3);
     const unsigned v_off = (((unsigned)lane / 4) << P_log2) * EB + v_piece * 16;
-    auto load_k = [&](const Pages &p, int tile, unsigned buf) __attribute__((always_inline)) {
-        const uint8_t *base[IDS];
+    struct KFrom { const uint8_t *base[IDS]; };
+    auto k_from = [&](const Pages &p, int tile) __attribute__((always_inline)) {
+        KFrom f;
 #pragma unroll
-        for (int u = 0; u < IDS; ++u) base[u] = Kc + ((place(p.id[u]) << P_log2) + ((unsigned)(tile * TILE + 16 * u) & in_page)) * ROWB;
-#pragma unroll
-        for (int i = 0; i < NK / RG; ++i) {
-            // (with one block the loads' numbers are constants, and so are the units that they are in)
-            const int I = RG == 1 ? i : block * (NK / RG) + i, u = I * KPI / 16;
-            const uint8_t *from;
-            if constexpr (ONE) {
-                from = base[0] + I * 1024;
-            } else {
-                from = base[0] + I * 1024;
-#pragma unroll
-                for (int k = 1; k < IDS; ++k) from = u == k ? base[k] + (I * KPI - 16 * k) * ROWB : from;
-            }
-            to_lds(buf + I * 1024, from, u >= NT ? k_off[1] : k_off[0]);
-        }
+        for (int u = 0; u < IDS; ++u) f.base[u] = Kc + ((place(p.id[u]) << P_log2) + ((unsigned)(tile * TILE + 16 * u) & in_page)) * ROWB;
+        return f;
     };
-    auto load_v = [&](const Pages &p, int tile, unsigned buf) __attribute__((always_inline)) {
-        const int first = RG == 1 ? 0 : block * (NV / RG);
-        const size_t step = ((size_t)16 << P_log2) * EB;             // sixteen head dims
-        if constexpr (ONE) {
-            const uint8_t *from = Vc + (((place(p.id[0]) * D) << P_log2) + ((unsigned)(tile * TILE) & in_page)) * EB + first * step;
+    auto put_k = [&](const KFrom &f, unsigned buf, int i) __attribute__((always_inline)) {
+        // (with one block the loads' numbers are constants, and so are the units that they are in)
+        const int I = RG == 1 ? i : block * (NK / RG) + i, u = I * KPI / 16;
+        const uint8_t *from = f.base[0] + I * 1024;
+        if constexpr (!ONE) {
 #pragma unroll
-            for (int i = 0; i < NV / RG; ++i) to_lds(buf + (first + i) * 1024, from + i * step, v_off);
+            for (int k = 1; k < IDS; ++k) from = u == k ? f.base[k] + (I * KPI - 16 * k) * ROWB : from;
+        }
+        to_lds(buf + I * 1024, from, u >= NT ? k_off[1] : k_off[0]);
+    };
+    const size_t v_step = ((size_t)16 << P_log2) * EB;               // sixteen head dims
+    const int v_begin = RG == 1 ? 0 : block * (NV / RG);
+    auto v_from = [&](const Pages &p, int tile) __attribute__((always_inline)) {         // the tile's, or the lane's, first address
+        if constexpr (ONE) {
+            return Vc + (((place(p.id[0]) * D) << P_log2) + ((unsigned)(tile * TILE) & in_page)) * EB + v_begin * v_step;
         } else {
             // the page of the lane's piece, by the bits of its unit (not by an index, which would put the pages into memory)
             const unsigned u = EB == 1 ? v_piece : v_piece >> 1, m0 = 0u - (u & 1), m1 = 0u - (u >> 1);
             unsigned id = ((unsigned)p.id[0] & ~m0) | ((unsigned)p.id[1] & m0);
             if constexpr (IDS == 4) id = (id & ~m1) | ((((unsigned)p.id[2] & ~m0) | ((unsigned)p.id[3] & m0)) & m1);
-            const uint8_t *from = Vc + (((place((int)id) * D) << P_log2) + ((unsigned)(tile * TILE + 16 * u) & in_page)) * EB + (v_off - 16 * u * EB) + first * step;
-#pragma unroll
-            for (int i = 0; i < NV / RG; ++i) to_lds(buf + (first + i) * 1024, from + i * step);
+            return Vc + (((place((int)id) * D) << P_log2) + ((unsigned)(tile * TILE + 16 * u) & in_page)) * EB + (v_off - 16 * u * EB) + v_begin * v_step;
         }
+    };
+    auto put_v = [&](const uint8_t *from, unsigned buf, int i) __attribute__((always_inline)) {
+        if constexpr (ONE) to_lds(buf + (v_begin + i) * 1024, from + i * v_step, v_off);
+        else to_lds(buf + (v_begin + i) * 1024, from + i * v_step);
+    };
+    auto load_k = [&](const Pages &p, int tile, unsigned buf) __attribute__((always_inline)) {
+        const KFrom f = k_from(p, tile);
+#pragma unroll
+        for (int i = 0; i < NK / RG; ++i) put_k(f, buf, i);
+    };
+    auto load_v = [&](const Pages &p, int tile, unsigned buf) __attribute__((always_inline)) {
+        const uint8_t *const f = v_from(p, tile);
+#pragma unroll
+        for (int i = 0; i < NV / RG; ++i) put_v(f, buf, i);
     };
     // scales stay in scalar registers until they are used, so that nothing waits for them where they are asked for
     struct Scales { float k[IDS], v[IDS]; };
@@ -462,7 +471,8 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(DD_PAGED_HEAD, Paged
     } else {
         // ---- half a tile, 32 keys, at a time, in three stages at once: the output of keys u, the weights of keys u + 32, the scores of keys
         // u + 64.  A matrix instruction, the decoding of the next one's operand and a share of the weights take turns, so that neither the
-        // matrix cores nor the vector units wait for the other.  MORE: there is a next tile.
+        // matrix cores nor the vector units wait for the other.  MORE, MORE2: one tile, two follow
+        // (MORE2 for shared tiles, others go by more2).
         Factors f = factors_of(now, sc, mine);
         Weights w;
         unsigned over = 0;
@@ -472,14 +482,12 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(DD_PAGED_HEAD, Paged
             for (int e = 0; e < 8; ++e) over |= weigh(w, s[0], e, f.c[0], f.shift[0] - m);
             raise(w, s[0], f.c[0], f.shift[0], over);
         }
-        auto round = [&](auto more_tag, int it, bool more2) __attribute__((always_inline)) {
-            constexpr bool MORE = decltype(more_tag)::value;
+        auto round = [&](auto tag, int it, bool more2) __attribute__((always_inline)) {
+            constexpr bool MORE = decltype(tag)::value > 0, MORE2 = decltype(tag)::value > 1;
             const int t = mine + it * STREAMS;
             wait_loads<0>();
             if constexpr (RG > 1) {
                 asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");         // what was asked for is there for all, and all have read the other buffers
-                if (more2) load_k(after, t + 2 * STREAMS, k_lds + (it & 1) * KB);
-                if constexpr (MORE) load_v(next, t + STREAMS, v_lds + (~it & 1) * VB);
             }
             u32x4 kraw[NT][KR], vraw[DT][2];
             constexpr int READ = RG == 1 ? 1 : 0;        // the halves that are read now: a wave's own tile is to be free for the next one
@@ -493,6 +501,20 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(DD_PAGED_HEAD, Paged
                 if (more2) load_k(after, t + 2 * STREAMS, k_lds);
                 if constexpr (MORE) load_v(next, t + STREAMS, v_lds);
             }
+            // Shared tiles are asked for one load at a time, beside the arithmetic: a wave waits where it asks faster than they are taken (16 x 64
+            // rows as above, 8192 keys 156.6 -> 151.9 us; bf16 pages, which wait for memory, take 29.2 at once and 31.0 one by one).
+            KFrom kf;
+            const uint8_t *vf;
+            if constexpr (RG > 1 && MORE2) kf = k_from(after, t + 2 * STREAMS);
+            if constexpr (RG > 1 && MORE) vf = v_from(next, t + STREAMS);
+            auto ask = [&](int i) __attribute__((always_inline)) {
+                if constexpr (RG > 1 && MORE) {
+                    if (i < NV / RG) put_v(vf, v_lds + (~it & 1) * VB, i);
+                }
+                if constexpr (RG > 1 && MORE2) {
+                    if (i >= NV / RG && i < NV / RG + NK / RG) put_k(kf, k_lds + (it & 1) * KB, i - NV / RG);
+                }
+            };
             third = pages_of(t + 3 * STREAMS);           // (scalar loads are unconditional: a branch would wait for them at its end)
             const Factors fn = factors_of(next, sc_next, t + STREAMS);
             sc_next = load_scales(after);
@@ -525,6 +547,10 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(DD_PAGED_HEAD, Paged
                     __builtin_amdgcn_sched_barrier(0);
                     o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fv, __builtin_bit_cast(bf16x8, w.w[j]), o[dt], 0, 0, 0);
                     if (i + 1 < SLOTS) fv = fragment<FP8>(vraw[(i + 1) % DT], 2 * T + (i + 1) / DT, f.vs[T]);
+                    if constexpr (T == 0) {
+#pragma unroll
+                        for (int e = i * 8 / SLOTS; e < (i + 1) * 8 / SLOTS; ++e) ask(e);
+                    }
                     if (i < 4) sum = sum4(sum, w, i);
                     if constexpr (WEIGHTS && SLOTS < 8) over |= weigh(wn, from, (SLOTS + i) % 8, c, at);
                     __builtin_amdgcn_sched_barrier(0);
@@ -536,7 +562,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(DD_PAGED_HEAD, Paged
                 }
                 if constexpr (SCORES) to = acc;
             };
-            step(std::integral_constant<int, 0>{}, more_tag, std::true_type{}, f, s[1], s[0]);
+            step(std::integral_constant<int, 0>{}, std::integral_constant<bool, MORE>{}, std::true_type{}, f, s[1], s[0]);
             if constexpr (READ == 0) {
                 read_v(vraw, 1, 1, it);
                 if constexpr (MORE) read_k(kraw[1], 1, it + 1);
@@ -545,14 +571,19 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(DD_PAGED_HEAD, Paged
             if constexpr (MORE) {
                 if (!fn.whole) mask(s[0], fn.left[0]);
             }
-            step(std::integral_constant<int, 1>{}, more_tag, more_tag, fn, s[0], s[1]);
+            step(std::integral_constant<int, 1>{}, std::integral_constant<bool, MORE>{}, std::integral_constant<bool, MORE>{}, fn, s[0], s[1]);
             f = fn;
             now = next;
             next = after;
             after = third;
         };
-        for (int it = 0; it + 1 < rounds; ++it) round(std::true_type{}, it, it + 2 < rounds);
-        if (rounds > 0) round(std::false_type{}, rounds - 1, false);
+        if constexpr (RG == 1) {
+            for (int it = 0; it + 1 < rounds; ++it) round(std::integral_constant<int, 1>{}, it, it + 2 < rounds);
+        } else {
+            for (int it = 0; it + 2 < rounds; ++it) round(std::integral_constant<int, 2>{}, it, true);
+            if (rounds > 1) round(std::integral_constant<int, 1>{}, rounds - 2, false);
+        }
+        if (rounds > 0) round(std::integral_constant<int, 0>{}, rounds - 1, false);
     }
     l += halves_other(l);
 
