@@ -146,6 +146,59 @@ def test_sharp_and_large_scores():
     assert b[0, 0, 5].isnan().all() and torch.equal(a[0, 0, rest], b[0, 0, rest])
 
 
+# batch, heads, key/value heads, rows, positions: one row block per workgroup, two, four, and keys that are split
+FORMS = [(2, 4, 2, 5, 700), (6, 48, 48, 43, 260), (5, 92, 46, 125, 200), (1, 2, 1, 3, 3000)]
+
+
+@pytest.mark.parametrize("cache", ["fp8", "bf16"])
+@pytest.mark.parametrize("order", ["rising", "falling"])
+@pytest.mark.parametrize("B,H,Hkv,n,N", FORMS)
+def test_scores_that_rise_or_fall_over_the_keys(cache, order, B, H, Hkv, n, N):
+    # the largest score so far grows from tile to tile, or all that follows is small: up to 40 in either sign, by the sign of a row
+    import torch
+    rng = np.random.default_rng(N)
+    P, d = 32, 128
+    per = -(-N // P)
+    v = np.sign(rng.standard_normal(d))
+    ramp = np.arange(1, N + 1) / N
+    if order == "falling":
+        ramp = ramp[::-1]
+    K, _ = rounded((ramp[None, None, :, None] * v * 2).repeat(B, 0).repeat(Hkv, 1), torch.bfloat16)
+    V, _ = rounded(rng.standard_normal((B, Hkv, N, d)), torch.bfloat16)
+    sign = np.where(np.arange(n) % 2 == 0, 1.0, -1.0)[:, None]
+    Q, q64 = rounded((sign * v * 40 / (2 * d / np.sqrt(d)))[None, None].repeat(B, 0).repeat(H, 1), torch.bfloat16)
+    t = torch.uint8 if cache == "fp8" else torch.bfloat16
+    Kc, Vc = torch.zeros((B * per, Hkv, P, d), dtype=t, device="cuda"), torch.zeros((B * per, Hkv, d, P), dtype=t, device="cuda")
+    ks, vs = (torch.ones((B * per, Hkv), device="cuda") for _ in range(2)) if cache == "fp8" else (None, None)
+    table = rng.permutation(B * per).reshape(B, per)
+    dd.dd_paged_cache_append(Kc, Vc, K, V, ints(table), ints(np.zeros(B)), k_scale=ks, v_scale=vs)
+    got = host(dd.dd_paged_attention(Q, Kc, Vc, ints(table), ints(np.full(B, N)), k_scale=ks, v_scale=vs))
+    from _paged import E4M3
+    values = (lambda c: E4M3[codes_of(c)]) if cache == "fp8" else host
+    want, A = paged.paged_attention(q64, values(Kc), values(Vc), None if ks is None else host(ks), None if vs is None else host(vs), table, [N] * B)
+    # products of one sign whose magnitudes add to 40 (43 where e4m3 rounded up): 140 steps of 2^-24 x 43 x log2 e < 2^-10 of a weight, in O and its divisor
+    assert (np.abs(got - want) <= (2.0 ** -8 + 2 * 2.0 ** -10) * A + 2.0 ** -8 * np.abs(want) + 1e-30).all()
+
+
+@pytest.mark.parametrize("cache", ["fp8", "bf16"])
+@pytest.mark.parametrize("B,H,Hkv,n,N", FORMS)
+def test_a_query_row_of_nan_stays_alone(cache, B, H, Hkv, n, N):
+    import torch
+    (Q, Kc, Vc, table, lens, ks, vs), _ = _case(B, H, Hkv, n, 128, 64, cache, [N] * B)
+    Q2 = Q.clone()
+    Q2[B - 1, H - 1, n // 2, 3] = float("nan")
+    a, b = (dd.dd_paged_attention(q, Kc, Vc, table, lens, k_scale=ks, v_scale=vs) for q in (Q, Q2))
+    assert b[B - 1, H - 1, n // 2].isnan().all()
+    b[B - 1, H - 1, n // 2] = a[B - 1, H - 1, n // 2]
+    assert torch.equal(a, b)
+
+
+def test_no_queries():
+    import torch
+    (Q, Kc, Vc, table, lens, ks, vs), _ = _case(2, 4, 2, 1, 64, 16, "fp8", [20, 7])
+    assert dd.dd_paged_attention(Q[:, :, :0].contiguous(), Kc, Vc, table, lens, k_scale=ks, v_scale=vs).shape == (2, 4, 0, 64)
+
+
 def test_scales_far_apart():
     # one page's values are 2^40 times the others': weights keep their range
     import torch
