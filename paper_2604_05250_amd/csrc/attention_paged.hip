@@ -653,46 +653,57 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(DD_PAGED_HEAD, Paged
 }
 
 // The splits' states of a row, merged by D / 4 lanes; rows whose sequence took one split are finished already.
+// The first states are asked for before it is known how many of them there are (one token, 4 x 4096 keys 12.1 -> 11.5 us with this and
+// with leading scalar arguments, as above).
 template <int D>
-__global__ __launch_bounds__(256) void paged_merge_kernel(const int32_t *kv_lens, int Hkv, int rows_total, int max_pages, unsigned shape, int rows, PagedTail a)
+__global__ __launch_bounds__(256) void paged_merge_kernel(const float *part_ml, const float *part_o, const int32_t *kv_lens, uint8_t *O, int Hkv, int rows_total,
+                                                          int max_pages, unsigned shape, int rows)
 {
     constexpr int LANES = D / 4;
     const int row = blockIdx.x * (256 / LANES) + threadIdx.x / LANES, d0 = (threadIdx.x % LANES) * 4;
     if (row >= rows) return;
-    const unsigned b = (unsigned)row / (unsigned)rows_total / (unsigned)Hkv;
     const int splits = (int)(shape >> 2 & 63) + 1;
-    const int used = share_of(kv_lens[b], max_pages, 4 + (int)(shape & 3), splits, rows_total).used;
-    if (used <= 1) return;
-    const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + (size_t)row * splits;
-    const floatx4 *po = reinterpret_cast<const floatx4 *>(a.part_o + (size_t)row * splits * D + d0);
+    const float2 *ml = reinterpret_cast<const float2 *>(part_ml) + (size_t)row * splits;
+    const floatx4 *po = reinterpret_cast<const floatx4 *>(part_o + (size_t)row * splits * D + d0);
     constexpr int U = 8;                             // states on their way: a round trip to memory for eight of them
-    float M = kNone, L = 0;
-    floatx4 x = {0, 0, 0, 0};
-    for (int s0 = 0; s0 < used; s0 += U) {
-        float2 st[U];
-        floatx4 v[U];
+    float2 st[U];
+    floatx4 v[U];
+    auto fetch = [&](int s0) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int s = min(s0 + u, used - 1);
+            const int s = min(s0 + u, splits - 1);
             st[u] = ml[s];
             v[u] = po[(size_t)s * (D / 4)];
         }
+    };
+    fetch(0);
+    const unsigned b = (unsigned)row / (unsigned)rows_total / (unsigned)Hkv;
+    const int used = share_of(kv_lens[b], max_pages, 4 + (int)(shape & 3), splits, rows_total).used;
+    if (used <= 1) return;
+    float M = kNone, L = 0;
+    floatx4 x = {0, 0, 0, 0};
+    for (int s0 = 0;;) {
         float top = M;
 #pragma unroll
-        for (int u = 0; u < U; ++u) top = fmaxf(top, st[u].x);
+        for (int u = 0; u < U; ++u) top = fmaxf(top, s0 + u < used ? st[u].x : M);
         const float by = __builtin_amdgcn_exp2f(M - top);
         M = top;
         L *= by;
         x *= by;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const float f = s0 + u < used ? __builtin_amdgcn_exp2f(st[u].x - M) : 0.0f;
-            L += f * st[u].y;
-            x += f * v[u];
+            if (s0 + u < used) {
+                const float f = __builtin_amdgcn_exp2f(st[u].x - M);
+                L += f * st[u].y;
+                x += f * v[u];
+            }
         }
+        s0 += U;
+        if (s0 >= used) break;
+        fetch(s0);
     }
     const float inv = L > 0 ? 1.0f / L : 0.0f;
-    *reinterpret_cast<uint2 *>(a.O + ((size_t)row * D + d0) * 2) = make_uint2(pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv));
+    *reinterpret_cast<uint2 *>(O + ((size_t)row * D + d0) * 2) = make_uint2(pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv));
 }
 
 struct Plan { int rg, splits; long row_tiles, wgs; };        // splits: at most kMaxSplits, row tiles: less than 2^24
@@ -765,7 +776,7 @@ hipError_t launch_attention_paged(const PagedAttnArgs &a, hipStream_t stream)
     if (e != hipSuccess || p.splits <= 1) return e;
     const unsigned per_wg = 256 / (a.d / 4);
     const dim3 grid((unsigned)((rows + per_wg - 1) / per_wg));
-    auto merge = [&](auto kernel) { return launch(kernel, grid, dim3(256), stream, a.kv_lens, a.Hkv, (a.H / a.Hkv) * a.n, a.max_pages, shape, (int)rows, tail); };
+    auto merge = [&](auto kernel) { return launch(kernel, grid, dim3(256), stream, tail.part_ml, tail.part_o, a.kv_lens, tail.O, a.Hkv, (a.H / a.Hkv) * a.n, a.max_pages, shape, (int)rows); };
     return a.d == 128 ? merge(paged_merge_kernel<128>) : merge(paged_merge_kernel<64>);
 }
 
