@@ -714,20 +714,20 @@ Plan plan_of(int n, int B, int H, int Hkv, long capacity, bool fp8)
     Plan p;
     // Two or four row blocks per workgroup read the cache once for all, but the workgroups are fewer and their waves wait for each other.
     // 256 compute units hold two workgroups each, so that up to 512 of one block run at once; bf16 pages wait for memory sooner.  us with
-    // one / two / four row blocks.  e4m3: 128 blocks, 2048 positions 15.1 / 18.9 / -; 512, 2048 25.6 / 28.5 / 48.2; 1024, 2048 46.3 / 41.6 / 49.0; 1536,
-    // 2048 - / 65.3 / 67.2; 1920, 2048 - / 80.6 / 75.4; 8192, 2048 338 / 301 / 276.  bf16: 256 blocks, 1024 positions 14.6 / 20.0 / -; 320, 2048 28.8 /
-    // 30.5 / -; 512, 4096 76.1 / 68.6 / 104; 1024, 2048 76.7 / 51.1 / 57.6; 1152, 2048 - / 74.9 / 70.4; 2048, 1024 80.1 / 56.6 / 50.2.  Where a
-    // workgroup's last rows are missing, their work is not: 320 rows of 128 heads, 700 positions - / 32.7 / 34.5.
+    // one / two / four row blocks, unsplit.  e4m3: 128 blocks, 2048 positions 15.5 / 25.2 / -; 512, 2048 25.0 / 27.1 / 46.1; 1024, 2048 45.5 / 40.0 /
+    // 46.6; 1536, 2048 73.9 / 62.2 / 65.6; 1920, 2048 91.5 / 78.2 / 75.5; 8192, 2048 335 / 290 / 272.  bf16: 256 blocks, 1024 positions 14.6 / 19.3 /
+    // -; 320, 2048 28.8 / 32.0 / -; 512, 4096 75.5 / 68.0 / 104; 1024, 2048 76.3 / 50.7 / 57.3; 1152, 2048 89.5 / 74.5 / 71.0; 2048, 1024 80.0 / 56.5 /
+    // 50.0.  Where a workgroup's last rows are missing, their work is not: 320 rows of 128 heads, 700 positions 35.3 / 32.6 / 34.7.
     const bool full = (rows + 127) / 128 * 128 * 8 <= rows * 9;
     p.rg = few || blocks <= (fp8 ? 512 : 256) ? 1 : full && blocks > (fp8 ? 1792 : 1024) ? 4 : 2;
     p.row_tiles = (rows + 32 * p.rg - 1) / (32 * p.rg);
     const long base = heads * p.row_tiles;
-    // Splits: the merge's launch costs some 2 us and each split a state per row, written and read again, for 32 rows as many bytes as a
+    // Splits: the merge's launch costs some 1.5 us and each split a state per row, written and read again, for 32 rows as many bytes as a
     // tile of 64 keys; so up to one workgroup per compute unit, and up to two where arithmetic bounds them and the splits stay long.  us with
-    // 1 / 2 / 4 / 8 / 16 splits, 32/8 heads, e4m3.  One token: one sequence, 512 positions 6.3 / 8.0 / 8.0 / - / -, 1024 8.6 / 8.9 / 8.0 / - / -,
-    // 4096 22.2 / 15.8 / 11.3 / 9.4 / 9.0; four 4096 25.1 / 18.0 / 13.2 / 11.9 / 13.7; 24 4096 35.1 / 41.0 / 39.6 / 42.1 / -.  64 tokens: one sequence
-    // 1024 9.9 / 11.2 / 11.1 / - / -, 2048 14.6 / 13.4 / 12.3 / 15.1 / -, 16384 83.1 / 48.2 / 29.4 / 28.8 / 33.8; three 2048 16.1 / 20.7 / 24.3 /
-    // 30.1 / -, 8192 46.7 / 42.2 / 39.9 / 45.3 / -; four 2048 16.2 / 22.6 / 26.5 / 35.9 / -, 8192 46.8 / 48.4 / 51.3 / 58.5 / -.
+    // 1 / 2 / 4 / 8 / 16 splits, 32/8 heads, e4m3.  One token: one sequence, 512 positions 6.1 / 7.4 / 7.4 / - / -, 1024 8.6 / 8.6 / 7.4 / - / -,
+    // 4096 22.2 / 15.6 / 11.0 / 8.8 / 8.4; four 4096 25.1 / 17.5 / 12.7 / 11.3 / 13.1; 24 4096 35.2 / 40.9 / 39.5 / 42.3 / -.  64 tokens: one sequence
+    // 1024 9.9 / 10.7 / 10.8 / - / -, 2048 14.8 / 13.1 / 12.0 / - / -, 16384 83.2 / 47.6 / 29.1 / 28.9 / 33.8; three 2048 16.1 / 20.6 / 23.9 / - / -,
+    // 8192 46.6 / 42.9 / 41.1 / 46.0 / -; four 2048 16.3 / 22.8 / 26.1 / - / -, 8192 47.7 / 48.3 / 51.3 / 59.6 / -.
     auto up_to = [&](long want, long least) { return want < tiles / least ? want : tiles / least; };
     long s = p.rg == 1 ? up_to(256 / base, few ? kSplitTiles : kSplitTilesMany) : 1;
     if (!few && p.rg < 4) {
