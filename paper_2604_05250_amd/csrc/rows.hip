@@ -6,8 +6,9 @@
 //   e4m3      code = rne(x / s), s = 2^e: one scale per page and head
 //
 // A row of d elements belongs to d / 16 lanes, each with two chunks of eight elements (16-byte accesses in bf16).  The chunks of a lane
-// are chosen so that the two members of every pair are in one lane - chunk c and chunk c + rot/2 where halves are paired, neighbours
-// otherwise - so a rotation needs no exchange, and lane c needs the angles 8c .. 8c + 7 in both pairings.
+// are chosen so that the two members of every pair are in one lane, and so a rotation needs no exchange; and so that the first chunks of
+// the lanes lie side by side, and the second ones.  (Both of a lane side by side - every other piece of a row for each load and store -
+// made the pairing of neighbours slower: 4 x 2046 rows of 64 heads of 64, fp32, 122 us, 13 x 2613 of 32 heads of 128, bf16, 178.)
 // Angles: position * inv_freq in revolutions, in fp64, and its fraction to fp32 (a product in fp32 is off by 2^-24 of the angle:
 // a hundredth of a radian at position 130000).  The hardware's sine and cosine take revolutions and are off by 2^-23 (measured over
 // [0, 1] against fp64).
@@ -86,28 +87,41 @@ template <int LANES> __device__ __forceinline__ float row_sum(float x)
 
 struct Pairing {                                             // where a lane's two chunks are, and how they are paired
     int a, b;                                                // first elements
-    bool turns, halves;
+    int fa, fb;                                              // which angles: of the first four pairs, of the last four
+    bool ta, tb;                                             // whether those turn
 };
-__device__ __forceinline__ Pairing pairing(int lane, int rot, bool interleaved)
+template <int D> __device__ __forceinline__ Pairing pairing(int lane, int rot, bool interleaved)
 {
     Pairing p;
-    p.turns = 16 * lane < rot;
-    p.halves = p.turns && !interleaved;
-    p.a = p.halves ? 8 * lane : 16 * lane;
-    p.b = p.halves ? rot / 2 + 8 * lane : 16 * lane + 8;
+    if (interleaved) {                                       // pairs within a chunk
+        p.a = 8 * lane;
+        p.b = D / 2 + 8 * lane;
+        p.ta = p.a < rot;
+        p.tb = p.b < rot;
+        p.fa = p.a / 2;
+        p.fb = p.b / 2;
+    } else {                                                 // chunk and chunk + rot / 2; what stays as it is behind them
+        const int rest = 8 * lane - rot / 2;
+        p.ta = p.tb = rest < 0;
+        p.a = p.ta ? 8 * lane : rot + rest;
+        p.b = p.ta ? rot / 2 + 8 * lane : rot + (D - rot) / 2 + rest;
+        p.fa = 8 * lane;
+        p.fb = 8 * lane + 4;
+    }
     return p;
 }
 
 enum { kNoTurn = 0, kHalves = 1, kNeighbours = 2 };
 
-// cos and sin of the eight angles of a lane at a position; a lane whose elements stay as they are gets 1 and 0
-__device__ __forceinline__ void turn_of(const float *inv_freq, int lane, bool turns, double position, float *c, float *s)
+// cos and sin of the eight angles of a lane at a position; elements that stay as they are get 1 and 0
+__device__ __forceinline__ void turn_of(const float *inv_freq, const Pairing &p, double position, float *c, float *s)
 {
-    const double p = position * 0.15915494309189533577;      // 1 / 2 pi
-    const float *const f = inv_freq + (turns ? 8 * lane : 0);
+    const double q = position * 0.15915494309189533577;      // 1 / 2 pi
+    const float *const fa = inv_freq + (p.ta ? p.fa : 0), *const fb = inv_freq + (p.tb ? p.fb : 0);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float r = (float)__builtin_amdgcn_fract((double)f[i] * p);             // revolutions
+        const float r = (float)__builtin_amdgcn_fract((double)(i < 4 ? fa[i] : fb[i - 4]) * q);      // revolutions
+        const bool turns = i < 4 ? p.ta : p.tb;
         c[i] = turns ? __builtin_amdgcn_cosf(r) : 1.0f;
         s[i] = turns ? __builtin_amdgcn_sinf(r) : 0.0f;
     }
@@ -162,7 +176,7 @@ __global__ __launch_bounds__(256) void norm_rotate_kernel(NormRotateArgs a)
     const bool is_q = (int)blockIdx.y < a.q_groups;
     const NormRotateSide &side = is_q ? a.q : a.k;
     const int first = ((int)blockIdx.y - (is_q ? 0 : a.q_groups)) * a.per_wg, count = min(a.per_wg, side.heads - first);
-    const Pairing p = pairing(lane, a.rot, PAIR == kNeighbours);
+    const Pairing p = pairing<D>(lane, a.rot, PAIR == kNeighbours);
 
     const uint8_t *src = static_cast<const uint8_t *>(side.x) + ((long)b * side.batch + first * side.head + (long)i * side.row) * T::bytes;
     uint8_t *dst = static_cast<uint8_t *>(side.y) + (((long)b * side.heads + first) * a.n + i) * D * T::bytes;
@@ -177,7 +191,7 @@ __global__ __launch_bounds__(256) void norm_rotate_kernel(NormRotateArgs a)
 
     float w[16], c[8], s[8];
     if constexpr (NORM) weights_of<T>(side.weight, p, w);
-    if constexpr (PAIR != kNoTurn) turn_of(a.inv_freq, lane, p.turns, a.positions != nullptr ? (double)a.positions[token] : (double)i, c, s);
+    if constexpr (PAIR != kNoTurn) turn_of(a.inv_freq, p, a.positions != nullptr ? (double)a.positions[token] : (double)i, c, s);
     const bool normed = NORM && side.weight != nullptr;
     for (int h0 = 0; h0 < count; h0 += U) {
 #pragma unroll
@@ -275,7 +289,7 @@ __device__ __forceinline__ void append_page(const PageAppendArgs &a, unsigned bi
     const bool kept = !written && pos < held;
     const bool keeps = min(start, held) > first || min(held, first + PAGE) > start + rows;       // some row is kept
 
-    const Pairing p = pairing(lane, VALUES ? 0 : a.rot, a.interleaved);
+    const Pairing p = pairing<D>(lane, VALUES ? 0 : a.rot, a.interleaved);
     const PageAppendSide &side = VALUES ? a.v : a.k;
     const long r = written ? pos - start : (start > first ? 0 : first - start);          // (a row that exists)
     const uint8_t *src = static_cast<const uint8_t *>(side.x) + (b * side.batch + r * side.row) * T::bytes;
@@ -291,7 +305,7 @@ __device__ __forceinline__ void append_page(const PageAppendArgs &a, unsigned bi
     const bool normed = a.weight != nullptr, turns = a.rot > 0;
     if constexpr (!VALUES) {
         weights_of<T>(a.weight, p, w);
-        if (turns) turn_of(a.inv_freq, lane, p.turns, (double)pos, c, s);
+        if (turns) turn_of(a.inv_freq, p, (double)pos, c, s);
     }
 
     // the keys and head dims of values that this thread stores
@@ -359,13 +373,13 @@ __device__ __forceinline__ void append_page(const PageAppendArgs &a, unsigned bi
             }
         } else {
             // ---- values: rows into LDS, and out by words of the rows, four (bf16: two) head dims of one key
-            unsigned *const mine = turned + slot * PITCH + lane * (4 * EB);
+            unsigned *const at_a = turned + slot * PITCH + p.a * EB / 4, *const at_b = turned + slot * PITCH + p.b * EB / 4;
             if constexpr (FP8) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) mine[i] = codes4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+                for (int i = 0; i < 4; ++i) (i < 2 ? at_a : at_b)[i % 2] = codes4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
             } else {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) mine[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
+                for (int i = 0; i < 8; ++i) (i < 4 ? at_a : at_b)[i % 4] = pack_bf16(x[2 * i], x[2 * i + 1]);
             }
             __syncthreads();
             if (stores && (some || by != 1.0f)) {
