@@ -257,20 +257,21 @@ struct Divide {                                              // x / s, by a prod
     }
 };
 
-// One workgroup has one page of one sequence, its keys or its values, for `per_wg` heads one after the other, and one row of the page
-// per d / 16 lanes.  It is the only one that writes this page and these heads, so the page's scale, its old rows and its new ones are
+// One workgroup has one page of one sequence, its keys or its values, for `per_wg` heads one after the other, and one row per d / 16
+// lanes: ROWS rows, all of the page or, where a call has no more than that for each sequence, the ones from its first new row on.  It is the only one that writes this page and these heads, so the page's scale, its old rows and its new ones are
 // decided here without an atomic.  The rows stay in registers between the maximum over the page and their storage; the next head's are
 // on their way meanwhile, and its angles and weights are this one's.
 // Values are stored with the keys of one head dim side by side, and are turned over in LDS.
 // Bound by memory: 16 x 2048 rows of 8 heads to e4m3 pages of 64 42 us, 4.8 TB/s read and written.
-template <typename T, int D, int PAGE, bool FP8, bool VALUES>
+template <typename T, int D, int PAGE, int ROWS, bool FP8, bool VALUES>
 __device__ __forceinline__ void append_page(const PageAppendArgs &a, unsigned bid, unsigned *turned, float *wave_max)
 {
-    constexpr int LANES = D / 16, WAVES = (PAGE * LANES + 63) / 64;
+    constexpr int LANES = D / 16, THREADS = ROWS * LANES, WAVES = (THREADS + 63) / 64;
     constexpr int EB = FP8 ? 1 : 2;                          // bytes per stored element
     constexpr int PITCH = D * EB / 4 + 1;                    // words per row in LDS: an odd number
     constexpr int KEYS = 16 / EB, DIMS = 4 / EB;             // a thread stores KEYS values of DIMS head dims
-    const int tid = threadIdx.x, lane = tid % LANES, slot = tid / LANES;
+    constexpr int JOBS = D / DIMS * (PAGE / KEYS), TURNS = (JOBS + THREADS - 1) / THREADS;
+    const int tid = threadIdx.x, lane = tid % LANES;
     const int group = bid % a.head_groups;
     bid /= a.head_groups;
     const int b = bid / a.pages_per_seq, j = bid % a.pages_per_seq;
@@ -284,9 +285,10 @@ __device__ __forceinline__ void append_page(const PageAppendArgs &a, unsigned bi
     if (first >= start + rows || rows == 0) return;          // (first + PAGE > start: j >= 0)
     const int page = uniform_load(a.table + (long)b * a.max_pages + page_index);
     if (page < 0 || page >= a.num_pages) return;
+    const long base = ROWS == PAGE || start < first ? first : start;                     // position of the first row that this workgroup has
+    const int slot = (int)(base - first) + tid / LANES;      // (ROWS < PAGE: may be behind the page; nothing is written there)
     const long pos = first + slot;
-    const bool written = pos >= start && pos < start + rows;
-    const bool kept = !written && pos < held;
+    const bool written = slot < PAGE && pos >= start && pos < start + rows;
     const bool keeps = min(start, held) > first || min(held, first + PAGE) > start + rows;       // some row is kept
 
     const Pairing p = pairing<D>(lane, VALUES ? 0 : a.rot, a.interleaved);
@@ -308,21 +310,31 @@ __device__ __forceinline__ void append_page(const PageAppendArgs &a, unsigned bi
         if (turns) turn_of(a.inv_freq, p, (double)pos, c, s);
     }
 
-    // the keys and head dims of values that this thread stores
-    const int k0 = tid % (PAGE / KEYS) * KEYS, dw = tid / (PAGE / KEYS);                 // first key, word of a row in LDS
-    const long at0 = first + k0;
-    const bool stores = dw < D / DIMS;
-    const bool all = at0 >= start && at0 + KEYS <= start + rows, some = at0 < start + rows && at0 + KEYS > start;
+    // the keys and head dims of values that this thread stores: TURNS times 16 bytes of each of DIMS head dims
+    int k0[TURNS], dw[TURNS];                                // first key, word of a row in LDS
+    bool stores[TURNS], all[TURNS], some[TURNS];
+#pragma unroll
+    for (int t = 0; t < TURNS; ++t) {
+        const int job = tid + t * THREADS;
+        k0[t] = job % (PAGE / KEYS) * KEYS;
+        dw[t] = job / (PAGE / KEYS);
+        stores[t] = job < JOBS;
+        const long at0 = first + k0[t];
+        all[t] = at0 >= start && at0 + KEYS <= start + rows;
+        some[t] = at0 < start + rows && at0 + KEYS > start;
+    }
 
     for (int g = g_begin, turn = 0; g < g_end; ++g, turn ^= 1) {
         const long at = (long)page * a.Hkv + g;              // page and head
         uint8_t *const store = static_cast<uint8_t *>(side.cache) + at * PAGE * D * EB;
-        auto place = [&](int q) __attribute__((always_inline)) { return reinterpret_cast<u32x4 *>(store + ((long)(dw * DIMS + q) * PAGE + k0) * EB); };
-        u32x4 was[DIMS];                                     // vectors of which only some keys are written
-        if (VALUES && stores && some && !all) {
+        auto place = [&](int t, int q) __attribute__((always_inline)) { return reinterpret_cast<u32x4 *>(store + ((long)(dw[t] * DIMS + q) * PAGE + k0[t]) * EB); };
+        u32x4 was[TURNS][DIMS];                              // vectors of which only some keys are written
 #pragma unroll
-            for (int q = 0; q < DIMS; ++q) was[q] = *place(q);
-        }
+        for (int t = 0; t < TURNS; ++t)
+            if (VALUES && stores[t] && some[t] && !all[t]) {
+#pragma unroll
+                for (int q = 0; q < DIMS; ++q) was[t][q] = *place(t, q);
+            }
         float old = 0.0f;
         if (FP8 && keeps) old = side.scale[at];
         float x[16];
@@ -358,14 +370,21 @@ __device__ __forceinline__ void append_page(const PageAppendArgs &a, unsigned bi
         if constexpr (!VALUES) {
             uint8_t *const row = store + (long)slot * D * EB;
             if constexpr (FP8) {
-                uint2 *const pa = reinterpret_cast<uint2 *>(row + p.a), *const pb = reinterpret_cast<uint2 *>(row + p.b);
                 if (written) {
-                    *pa = make_uint2(codes4(x[0], x[1], x[2], x[3]), codes4(x[4], x[5], x[6], x[7]));
-                    *pb = make_uint2(codes4(x[8], x[9], x[10], x[11]), codes4(x[12], x[13], x[14], x[15]));
-                } else if (kept && by != 1.0f) {
-                    const uint2 ca = *pa, cb = *pb;
-                    *pa = make_uint2(regrown4(ca.x, by), regrown4(ca.y, by));
-                    *pb = make_uint2(regrown4(cb.x, by), regrown4(cb.y, by));
+                    *reinterpret_cast<uint2 *>(row + p.a) = make_uint2(codes4(x[0], x[1], x[2], x[3]), codes4(x[4], x[5], x[6], x[7]));
+                    *reinterpret_cast<uint2 *>(row + p.b) = make_uint2(codes4(x[8], x[9], x[10], x[11]), codes4(x[12], x[13], x[14], x[15]));
+                }
+                if (by != 1.0f) {
+#pragma unroll
+                    for (int k = 0; k < PAGE / ROWS; ++k) {
+                        const int s1 = k * ROWS + tid / LANES;
+                        const long at1 = first + s1;
+                        if (at1 >= held || (at1 >= start && at1 < start + rows)) continue;
+                        uint2 *const pa = reinterpret_cast<uint2 *>(store + (long)s1 * D + p.a), *const pb = reinterpret_cast<uint2 *>(store + (long)s1 * D + p.b);
+                        const uint2 ca = *pa, cb = *pb;
+                        *pa = make_uint2(regrown4(ca.x, by), regrown4(ca.y, by));
+                        *pb = make_uint2(regrown4(cb.x, by), regrown4(cb.y, by));
+                    }
                 }
             } else if (written) {
                 store_chunk<Bf16, false>(row, p.a, x);
@@ -373,7 +392,7 @@ __device__ __forceinline__ void append_page(const PageAppendArgs &a, unsigned bi
             }
         } else {
             // ---- values: rows into LDS, and out by words of the rows, four (bf16: two) head dims of one key
-            unsigned *const at_a = turned + slot * PITCH + p.a * EB / 4, *const at_b = turned + slot * PITCH + p.b * EB / 4;
+            unsigned *const at_a = turned + tid / LANES * PITCH + p.a * EB / 4, *const at_b = turned + tid / LANES * PITCH + p.b * EB / 4;
             if constexpr (FP8) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) (i < 2 ? at_a : at_b)[i % 2] = codes4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
@@ -382,13 +401,16 @@ __device__ __forceinline__ void append_page(const PageAppendArgs &a, unsigned bi
                 for (int i = 0; i < 8; ++i) (i < 4 ? at_a : at_b)[i % 4] = pack_bf16(x[2 * i], x[2 * i + 1]);
             }
             __syncthreads();
-            if (stores && (some || by != 1.0f)) {
+#pragma unroll
+            for (int t = 0; t < TURNS; ++t) {
+                if (!stores[t] || !(some[t] || by != 1.0f)) continue;
+                const int from = k0[t] - (int)(base - first);            // row of the first key in LDS; (ROWS < PAGE) of keys that are not there, any row
                 unsigned in_row[KEYS];
 #pragma unroll
-                for (int k = 0; k < KEYS; ++k) in_row[k] = turned[(k0 + k) * PITCH + dw];
-                if (!some) {
+                for (int k = 0; k < KEYS; ++k) in_row[k] = turned[(ROWS == PAGE ? from + k : min(max(from + k, 0), ROWS - 1)) * PITCH + dw[t]];
+                if (!some[t]) {
 #pragma unroll
-                    for (int q = 0; q < DIMS; ++q) was[q] = *place(q);
+                    for (int q = 0; q < DIMS; ++q) was[t][q] = *place(t, q);
                 }
 #pragma unroll
                 for (int q = 0; q < DIMS; ++q) {
@@ -403,22 +425,22 @@ __device__ __forceinline__ void append_page(const PageAppendArgs &a, unsigned bi
                             out[o] = __builtin_amdgcn_perm(in_row[2 * o + 1], in_row[2 * o], q ? 0x07060302u : 0x05040100u);
                         }
                     }
-                    if (!all) {                              // the other keys of the vector: kept codes in the new scale, the rest as it was
+                    if (!all[t]) {                              // the other keys of the vector: kept codes in the new scale, the rest as it was
 #pragma unroll
                         for (int o = 0; o < 4; ++o) {
-                            unsigned grown = was[q][o], is_new = 0, is_kept = 0;
-                            if constexpr (FP8) grown = by != 1.0f ? regrown4(was[q][o], by) : was[q][o];
+                            unsigned grown = was[t][q][o], is_new = 0, is_kept = 0;
+                            if constexpr (FP8) grown = by != 1.0f ? regrown4(was[t][q][o], by) : was[t][q][o];
 #pragma unroll
                             for (int e = 0; e < KEYS / 4; ++e) {
-                                const long at1 = at0 + o * (KEYS / 4) + e;
+                                const long at1 = first + k0[t] + o * (KEYS / 4) + e;
                                 const unsigned field = (FP8 ? 0xffu : 0xffffu) << (e * 8 * EB);
                                 if (at1 >= start && at1 < start + rows) is_new |= field;
                                 else if (at1 < held) is_kept |= field;
                             }
-                            out[o] = (out[o] & is_new) | (grown & is_kept) | (was[q][o] & ~(is_new | is_kept));
+                            out[o] = (out[o] & is_new) | (grown & is_kept) | (was[t][q][o] & ~(is_new | is_kept));
                         }
                     }
-                    *place(q) = out;
+                    *place(t, q) = out;
                 }
             }
             if (g + 1 < g_end) __syncthreads();
@@ -426,21 +448,29 @@ __device__ __forceinline__ void append_page(const PageAppendArgs &a, unsigned bi
     }
 }
 
-template <typename T, int D, int PAGE, bool FP8>
-__global__ __launch_bounds__(PAGE *D / 16) void page_append_kernel(PageAppendArgs a)
+template <typename T, int D, int PAGE, int ROWS, bool FP8>
+__global__ __launch_bounds__(ROWS *D / 16) void page_append_kernel(PageAppendArgs a)
 {
-    constexpr int EB = FP8 ? 1 : 2, WAVES = (PAGE * D / 16 + 63) / 64;
-    __shared__ unsigned turned[PAGE * (D * EB / 4 + 1)];
+    constexpr int EB = FP8 ? 1 : 2, WAVES = (ROWS * D / 16 + 63) / 64;
+    __shared__ unsigned turned[ROWS * (D * EB / 4 + 1)];
     __shared__ float wave_max[2 * WAVES];
-    if (blockIdx.x & 1) append_page<T, D, PAGE, FP8, true>(a, blockIdx.x >> 1, turned, wave_max);
-    else append_page<T, D, PAGE, FP8, false>(a, blockIdx.x >> 1, turned, wave_max);
+    if (blockIdx.x & 1) append_page<T, D, PAGE, ROWS, FP8, true>(a, blockIdx.x >> 1, turned, wave_max);
+    else append_page<T, D, PAGE, ROWS, FP8, false>(a, blockIdx.x >> 1, turned, wave_max);
 }
 
-template <typename T, int D, int PAGE>
-hipError_t append_rows(const PageAppendArgs &a, bool fp8, unsigned wgs, hipStream_t stream)
+// Rows of a workgroup: as many as a sequence can have, of 16, 64 or all of the page: a workgroup of few waves starts and meets sooner.  us
+// with this / with all: one token, 8 sequences, 32 heads, e4m3 pages of 128 6.8 / 9.7, ten 6.4 / 14.2, 16 rows of 11 sequences, 8 heads, pages of 64
+// 5.2 / 5.9.
+int rows_of(int n, int page) { return n <= 16 ? 16 : n <= 64 && page > 64 ? 64 : page; }
+template <typename T, int D, int PAGE> hipError_t append_rows(const PageAppendArgs &a, bool fp8, unsigned wgs, hipStream_t stream)
 {
-    const dim3 block(PAGE * D / 16);
-    return fp8 ? launch(page_append_kernel<T, D, PAGE, true>, dim3(wgs), block, stream, a) : launch(page_append_kernel<T, D, PAGE, false>, dim3(wgs), block, stream, a);
+    const int rows = rows_of(a.n, PAGE);
+    auto run = [&](auto kernel) { return launch(kernel, dim3(wgs), dim3(rows * D / 16), stream, a); };
+    if constexpr (PAGE > 16)
+        if (rows == 16) return fp8 ? run(page_append_kernel<T, D, PAGE, 16, true>) : run(page_append_kernel<T, D, PAGE, 16, false>);
+    if constexpr (PAGE > 64)
+        if (rows == 64) return fp8 ? run(page_append_kernel<T, D, PAGE, 64, true>) : run(page_append_kernel<T, D, PAGE, 64, false>);
+    return fp8 ? run(page_append_kernel<T, D, PAGE, PAGE, true>) : run(page_append_kernel<T, D, PAGE, PAGE, false>);
 }
 template <typename T, int D> hipError_t append_rows(const PageAppendArgs &a, bool fp8, unsigned wgs, hipStream_t stream)
 {
@@ -490,7 +520,7 @@ hipError_t launch_page_append(PageAppendArgs a, int d, bool rows_bf16, bool fp8,
     // Heads per workgroup: as many as leave two thousand threads per compute unit, what fits there; more workgroups make the angles and
     // look up the page once more each.  us at one head / all heads / this: 16 x 2048 rows, 8 heads, e4m3 67 / 42 / 42, 4096 rows, 32 heads,
     // bf16 pages of 16 32 / 33 / 31; 16 rows of one token 5.0 whatever it is.
-    const long threads = 2L * a.B * a.pages_per_seq * a.Hkv * (page * d / 16), per = threads / (256 * 2048);
+    const long threads = 2L * a.B * a.pages_per_seq * a.Hkv * (rows_of(a.n, (int)page) * d / 16), per = threads / (256 * 2048);
     a.per_wg = per < 1 ? 1 : per > a.Hkv ? a.Hkv : (int)per;
     a.head_groups = (a.Hkv + a.per_wg - 1) / a.per_wg;
     const unsigned wgs = (unsigned)(2L * a.B * a.pages_per_seq * a.head_groups);

@@ -86,6 +86,17 @@ def test_options(cache, kw):
 
 
 @pytest.mark.parametrize("cache", ["fp8", "bf16"])
+@pytest.mark.parametrize("d,P", [(128, 128), (64, 128), (128, 64), (64, 32)])
+@pytest.mark.parametrize("n", [1, 15, 16, 17, 63, 64, 65])
+def test_few_rows(cache, d, P, n):
+    # at the pages' borders and across them, at the end and within sequences, with rows that are small beside what the pages hold and large
+    for scale in (1e-3, 1.5, 300.0):
+        _check(4, 3, n, d, P, cache, [P - n, P - 1, 5, 2 * P], rows="f32" if n % 16 == 15 else "bf16", per=4, scale=scale, norm=False, seed=n)
+    _check(4, 3, n, d, P, cache, [P - n, P - 1, 5, 2 * P - 3], kv_lens=[4 * P, P + 3, 5, 2 * P + n], per=4, scale=40.0, interleaved=True, seed=n)
+    _check(4, 3, n, d, P, cache, [P - n, P - 1, -5, 4 * P - 3], n_rows=[n - 1, 1, n, n], per=4, rot=32, seed=n)
+
+
+@pytest.mark.parametrize("cache", ["fp8", "bf16"])
 def test_rows_and_pages_that_are_skipped(cache):
     # positions before the sequence and behind the table, pages that are none, and a start near the type's end
     _check(3, 2, 50, 64, 16, cache, [-7, 30, 2**31 - 20], table=[[0, 99, 2, 3], [4, 5, -1, 7], [8, 9, 10, 11]], per=4)
