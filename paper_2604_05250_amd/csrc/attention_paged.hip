@@ -726,8 +726,9 @@ Plan plan_of(int n, int B, int H, int Hkv, long capacity, bool fp8)
     // tile of 64 keys; so up to one workgroup per compute unit, and up to two where arithmetic bounds them and the splits stay long.  us with
     // 1 / 2 / 4 / 8 / 16 splits, 32/8 heads, e4m3.  One token: one sequence, 512 positions 6.1 / 7.4 / 7.4 / - / -, 1024 8.6 / 8.6 / 7.4 / - / -,
     // 4096 22.2 / 15.6 / 11.0 / 8.8 / 8.4; four 4096 25.1 / 17.5 / 12.7 / 11.3 / 13.1; 24 4096 35.2 / 40.9 / 39.5 / 42.3 / -.  64 tokens: one sequence
-    // 1024 9.9 / 10.7 / 10.8 / - / -, 1500 12.5 / 12.3 / 11.8 / - / -, 2048 14.8 / 13.1 / 12.0 / - / -, 16384 83.2 / 47.6 / 29.1 / 28.9 / 33.8; three 2048 16.1 / 20.6 / 23.9 / - / -,
-    // 8192 46.6 / 42.9 / 41.1 / 46.0 / -; four 2048 16.3 / 22.8 / 26.1 / - / -, 8192 47.7 / 48.3 / 51.3 / 59.6 / -.
+    // 1024 9.9 / 10.7 / 10.8 / - / -, 1500 12.5 / 12.3 / 11.8 / - / -, 2048 14.8 / 13.1 / 12.0 / - / -, 16384 83.2 / 47.6 / 29.1 / 28.9 / 33.8; three
+    // 2048 16.1 / 20.6 / 23.9 / - / -, 8192 46.6 / 42.9 / 41.1 / 46.0 / -; four 2048 16.3 / 22.8 / 26.1 / - / -, 8192 47.7 / 48.3 / 51.3 / 59.6 / -.
+    // Calls a little past one or two workgroups per compute unit wait for the few that share one: 264 of 3937 positions 34.1 / 38.5 / 37.9 / - / -.
     auto up_to = [&](long want, long least) { return want < tiles / least ? want : tiles / least; };
     long s = p.rg == 1 ? up_to(256 / base, kSplitTiles) : 1;
     if (!few && p.rg < 4) {
