@@ -519,7 +519,7 @@ hipError_t launch_page_append(PageAppendArgs a, int d, bool rows_bf16, bool fp8,
     a.pages_per_seq = (int)((a.n + page - 2) / page + 1);    // that n rows can touch, wherever they begin
     // Heads per workgroup: as many as leave two thousand threads per compute unit, what fits there; more workgroups make the angles and
     // look up the page once more each.  us at one head / all heads / this: 16 x 2048 rows, 8 heads, e4m3 67 / 42 / 42, 4096 rows, 32 heads,
-    // bf16 pages of 16 32 / 33 / 31; 16 rows of one token 5.0 whatever it is.
+    // bf16 pages of 16 32 / 33 / 31; short calls have one head each.
     const long threads = 2L * a.B * a.pages_per_seq * a.Hkv * (rows_of(a.n, (int)page) * d / 16), per = threads / (256 * 2048);
     a.per_wg = per < 1 ? 1 : per > a.Hkv ? a.Hkv : (int)per;
     a.head_groups = (a.Hkv + a.per_wg - 1) / a.per_wg;
