@@ -11,6 +11,13 @@
 
 #include "dd_internal.h"
 
+// How an asm block that loads from memory into LDS begins: m0 has the place in LDS.  An instruction that writes m0 has to be one wait
+// state before the load that reads it, and a vector instruction that writes a scalar register (a readlane, which the compiler makes by
+// itself where scalar registers are short) five before a load that takes its address from there.  The compiler sees to both only
+// outside such blocks.  _BASE: for loads from a scalar base.
+#define DD_SET_M0 "s_mov_b32 m0, %0\n\ts_nop 0\n\t"
+#define DD_SET_M0_BASE "s_mov_b32 m0, %0\n\ts_nop 3\n\t"
+
 namespace dd {
 
 // Block-completion refresh of the cache (Sec. 2.3: the cache is brought up to date when a block is done):

@@ -126,10 +126,10 @@ void attn_duo_kernel(DD_ATTN_HEAD, const AttnTail a)
     const uint8_t *const vb_ = blen ? static_cast<const uint8_t *>(a.Vblk) + kv_head * blen * (size_t)ROWB : nullptr;
     const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) void *)KV;
     auto load_at = [&](unsigned dst, const uint8_t *src) __attribute__((always_inline)) {                    // per-lane address
-        asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(dst), "v"(src) : "memory", "m0");
+        asm volatile(DD_SET_M0 "global_load_lds_dwordx4 %1, off" ::"s"(dst), "v"(src) : "memory", "m0");
     };
     auto load4_at = [&](unsigned dst, const void *src) __attribute__((always_inline)) {                      // four bytes per lane
-        asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, off" ::"s"(dst), "v"(src) : "memory", "m0");
+        asm volatile(DD_SET_M0 "global_load_lds_dword %1, off" ::"s"(dst), "v"(src) : "memory", "m0");
     };
     const int whole = (kend - kbeg) / TK;            // tiles [0, whole) hold TK rows of the range, ...
     int blk0 = 0, blk1 = 0;                          // ... those outside [blk0, blk1) among them rows of the cache only

@@ -100,11 +100,11 @@ __device__ __forceinline__ Share share_of(int len, int max_pages, int page_log2,
 // counts nor waits for it.
 __device__ __forceinline__ void to_lds(unsigned lds, const uint8_t *base, unsigned lane_offset)
 {
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(lane_offset), "s"(base) : "memory", "m0");
+    asm volatile(DD_SET_M0_BASE "global_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(lane_offset), "s"(base) : "memory", "m0");
 }
 __device__ __forceinline__ void to_lds(unsigned lds, const uint8_t *lane_address)
 {
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(lane_address) : "memory", "m0");
+    asm volatile(DD_SET_M0 "global_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(lane_address) : "memory", "m0");
 }
 template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 

@@ -135,7 +135,7 @@ __device__ __forceinline__ void attn_solo(const AttnHead &h, const AttnTail &a)
     for (int i = wave; i < RB * NK; i += NW) {
         const int r = min(v_first + i * KDMA_ROWS + krow0, rows_total - 1);
         const uint8_t *const src = h.Q + (row_base + r) * KROWB + kchunk(i);
-        asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_addr(QS) + i * 1024), "v"(src) : "memory", "m0");
+        asm volatile(DD_SET_M0 "global_load_lds_dwordx4 %1, off" ::"s"(lds_addr(QS) + i * 1024), "v"(src) : "memory", "m0");
     }
 
     const int kbeg = sp * h.keys_per_split;
@@ -183,11 +183,11 @@ __device__ __forceinline__ void attn_solo(const AttnHead &h, const AttnTail &a)
                 if constexpr (PARTIAL) {
                     const uint8_t *const at = sbase - BIAS + I * VDMA_ROWS * PITCH;
                     const unsigned di = d - BIAS + I * 1024;
-                    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(di), "v"(o), "s"(at) : "memory", "m0");
+                    asm volatile(DD_SET_M0_BASE "global_load_lds_dwordx4 %1, %2" ::"s"(di), "v"(o), "s"(at) : "memory", "m0");
                 } else if constexpr (IMM >= 0)
-                    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2 offset:%3" ::"s"(d), "v"(o), "s"(sbase), "n"(IMM) : "memory", "m0");
+                    asm volatile(DD_SET_M0_BASE "global_load_lds_dwordx4 %1, %2 offset:%3" ::"s"(d), "v"(o), "s"(sbase), "n"(IMM) : "memory", "m0");
                 else
-                    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2 offset:-%3" ::"s"(d), "v"(o), "s"(sbase), "n"(-IMM) : "memory", "m0");
+                    asm volatile(DD_SET_M0_BASE "global_load_lds_dwordx4 %1, %2 offset:-%3" ::"s"(d), "v"(o), "s"(sbase), "n"(-IMM) : "memory", "m0");
             });
         } else {
             static_for<0, NL>([&](auto i) __attribute__((always_inline)) {
@@ -197,7 +197,7 @@ __device__ __forceinline__ void attn_solo(const AttnHead &h, const AttnTail &a)
                 const uint8_t *const src = (K ? (in_blk ? kb_ : kc) : (in_blk ? vb_ : vc)) +
                                            (size_t)(in_blk ? j - bstart : j) * PITCH + (K ? kchunk(I) : vchunk);
                 const unsigned d = dst - BIAS + I * 1024;
-                asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(d), "v"(src) : "memory", "m0");
+                asm volatile(DD_SET_M0 "global_load_lds_dwordx4 %1, off" ::"s"(d), "v"(src) : "memory", "m0");
             });
         }
     };
@@ -209,7 +209,7 @@ __device__ __forceinline__ void attn_solo(const AttnHead &h, const AttnTail &a)
     // (through LDS like the rows: the compiler's own wait for a load of its own would wait for every load after it as well)
     if (a.q_scale && wave == 0) {
         const float *const src = a.q_scale + kv_head * a.group + min(v_first + (RB == 2 ? lane : l32), rows_total - 1) / a.Nq;
-        asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, off" ::"s"(lds_addr(qs_sh)), "v"(src) : "memory", "m0");
+        asm volatile(DD_SET_M0 "global_load_lds_dword %1, off" ::"s"(lds_addr(qs_sh)), "v"(src) : "memory", "m0");
     }
     if (wave < nunits) {
         load_rows(of_k, wave);

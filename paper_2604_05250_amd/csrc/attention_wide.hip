@@ -407,9 +407,9 @@ void attn_wide_kernel(const AttnKernelArgs a)
         // compiler prefers to carry a 64-bit address per lane and per load).  It therefore knows nothing of
         // these loads: every wait for them in this kernel is explicit.
         if (i & 1)
-            asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(d), "v"(lane_off), "s"(sbase) : "memory", "m0");
+            asm volatile(DD_SET_M0_BASE "global_load_lds_dwordx4 %1, %2" : : "s"(d), "v"(lane_off), "s"(sbase) : "memory", "m0");
         else
-            asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2 offset:-4096" : : "s"(d), "v"(lane_off), "s"(sbase) : "memory", "m0");
+            asm volatile(DD_SET_M0_BASE "global_load_lds_dwordx4 %1, %2 offset:-4096" : : "s"(d), "v"(lane_off), "s"(sbase) : "memory", "m0");
     };
     // MX: the scale words of the tile whose first row is source row `row` of kv head `bk`: wave 0 loads K's, wave 1 V's
     auto dma_scales = [&](unsigned *dk, unsigned *dv, int bk, int row) __attribute__((always_inline)) {
@@ -417,7 +417,7 @@ void attn_wide_kernel(const AttnKernelArgs a)
             if (wave < 2) {                          // uniform
                 const uint8_t *src = scalar_ptr((wave == 0 ? a.k_mx : a.v_mx) + ((size_t)bk * a.kv_stride + row) * 4);
                 const unsigned d = wave == 0 ? lds_addr(dk) : lds_addr(dv), o = lane * 4;
-                asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, %2" : : "s"(d), "v"(o), "s"(src) : "memory", "m0");
+                asm volatile(DD_SET_M0_BASE "global_load_lds_dword %1, %2" : : "s"(d), "v"(o), "s"(src) : "memory", "m0");
             }
         }
     };
@@ -448,7 +448,7 @@ void attn_wide_kernel(const AttnKernelArgs a)
         const int drow = ln / KCH, dpos = ln % KCH;
         if constexpr (MX) {
             const uint8_t *src = a.q_mx + (t.row_base + min(t.v0 + wave * kRowsWave + (ln & (kRowsWave - 1)), rows_total - 1)) * 4;
-            asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, off" : : "s"(lds_addr(QX) + wave * 256), "v"(src) : "memory", "m0");
+            asm volatile(DD_SET_M0 "global_load_lds_dword %1, off" : : "s"(lds_addr(QX) + wave * 256), "v"(src) : "memory", "m0");
         }
         if (__builtin_expect(t.v0 + kRowsWG <= rows_total, 1)) {
             // whole tile: 1 KB per load, contiguous on both sides - scalar bases 8 KB apart and immediates;
@@ -462,10 +462,10 @@ void attn_wide_kernel(const AttnKernelArgs a)
                 const uint8_t *sbase = scalar_ptr(qg + mid);
                 const unsigned d = dst + mid, o = off[(i * KDMA_ROWS / 4) & 1];
                 if constexpr (imm >= 0)
-                    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2 offset:%3"
+                    asm volatile(DD_SET_M0_BASE "global_load_lds_dwordx4 %1, %2 offset:%3"
                                  : : "s"(d), "v"(o), "s"(sbase), "n"(imm) : "memory", "m0");
                 else
-                    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2 offset:-%3"
+                    asm volatile(DD_SET_M0_BASE "global_load_lds_dwordx4 %1, %2 offset:-%3"
                                  : : "s"(d), "v"(o), "s"(sbase), "n"(-imm) : "memory", "m0");
             });
         } else {
@@ -473,7 +473,7 @@ void attn_wide_kernel(const AttnKernelArgs a)
             for (int i = 0; i < NQDMA; ++i) {
                 const int row = min(i * KDMA_ROWS + drow, rows_total - 1 - t.v0 - wave * kRowsWave);
                 const uint8_t *src = qg + (ptrdiff_t)row * KROWB + (dpos ^ ((i * KDMA_ROWS + drow) & 7)) * 16;
-                asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(dst + i * 1024), "v"(src) : "memory", "m0");
+                asm volatile(DD_SET_M0 "global_load_lds_dwordx4 %1, off" : : "s"(dst + i * 1024), "v"(src) : "memory", "m0");
             }
         }
     };
