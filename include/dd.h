@@ -25,7 +25,8 @@
  *   - `workspace` is device memory of at least dd_*_workspace_bytes(...) bytes (same
  *     shape arguments), 256-byte aligned, contents undefined on entry and exit.  It may
  *     be NULL when the query function returns 0.  Calls that share a workspace must be
- *     ordered on one stream.
+ *     ordered on one stream, and one must have returned before the next is made, by
+ *     whichever thread: a call can be several launches that hand data over in it.
  *   - All tensors are dense, row-major, contiguous, base pointers 16-byte aligned.
  *   - Return value: DD_OK, or a negative dd_status.  Arguments are validated on the
  *     host before any GPU call; on error nothing is launched and no output is touched.
@@ -410,7 +411,8 @@ size_t dd_verify_remask_workspace_bytes(int B, int G, int V, dd_dtype logit_dtyp
  *     the current device.
  *   - All calls on one GPU share the one array, which keeps the last call's contents (no call depends on them):
  *     two calls of this entry point that overlap in time on one GPU (different streams) race and give wrong
- *     results; calls on one stream, or ordered by events, are fine.  Calls with 192 rows or more use no scratch.
+ *     results; calls on one stream, or ordered by events, are fine where one has returned before the next is
+ *     made.  Calls with 192 rows or more use no scratch.
  */
 int dd_verify_remask_static(const void *logits_d, const void *logits_v, const uint8_t *mask,
                             dd_mode mode, float threshold, uint64_t seed,

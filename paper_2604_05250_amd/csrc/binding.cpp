@@ -25,6 +25,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <map>
+#include <mutex>
 #include <utility>
 
 #include "../../include/dd.h"
@@ -196,9 +197,14 @@ hipStream_t current_stream() { return c10::hip::getCurrentHIPStream().stream(); 
 // ---- scratch memory: one tensor per (device, stream) - calls on one stream run in order and may share it, calls on
 // different streams may overlap and must not - or the one a fixed_workspace() block has set.  Guarded by the interpreter
 // lock; never destroyed (the runtime may be gone by then).
+// A call that uses it can be several launches, of which the later ones read what the first one left there, and it is made without the
+// interpreter lock.  So that no other thread's launches on the stream come in between, each scratch tensor has a lock of its own, held
+// from a call's first launch to its last, and taken only without the interpreter lock.
 struct Scratch {
-    std::map<std::pair<int, hipStream_t>, at::Tensor> by_stream;
+    struct Held { at::Tensor memory; std::mutex launches; };
+    std::map<std::pair<int, hipStream_t>, Held> by_stream;
     at::Tensor fixed;
+    std::mutex fixed_launches, static_launches;              // (the second: of the calls that use the library's own array)
     size_t peak = 0;
 };
 Scratch &scratch()
@@ -206,10 +212,11 @@ Scratch &scratch()
     static Scratch *s = new Scratch;
     return *s;
 }
+struct Workspace { at::Tensor memory; std::mutex *launches = nullptr; };
 // (`or_less`: the library itself says whether a fixed workspace of fewer bytes serves the call)
-at::Tensor workspace(size_t nbytes, const at::Device &device, hipStream_t stream, bool or_less)
+Workspace workspace(size_t nbytes, const at::Device &device, hipStream_t stream, bool or_less)
 {
-    if (nbytes == 0) return at::Tensor();
+    if (nbytes == 0) return {};
     Scratch &s = scratch();
     if (nbytes > s.peak) s.peak = nbytes;
     if (s.fixed.defined()) {
@@ -218,7 +225,7 @@ at::Tensor workspace(size_t nbytes, const at::Device &device, hipStream_t stream
                          (long long)s.fixed.numel(), s.fixed.device().str().c_str(), nbytes, device.str().c_str());
             throw Raised{};
         }
-        return s.fixed;
+        return {s.fixed, &s.fixed_launches};
     }
     if (c10::hip::currentStreamCaptureStatusMayInitCtx() != c10::hip::CaptureStatus::None) {
         // memory allocated under capture would come from that graph's private pool and a cached tensor of it
@@ -228,27 +235,33 @@ at::Tensor workspace(size_t nbytes, const at::Device &device, hipStream_t stream
                         "capture through paper_2604_05250_amd.step.capture_step, or inside fixed_workspace()");
         throw Raised{};
     }
-    at::Tensor &t = s.by_stream[{device.index(), stream}];
-    if (!t.defined() || (size_t)t.numel() < nbytes)
-        t = at::empty({(int64_t)(nbytes > (1u << 20) ? nbytes : (1u << 20))}, at::TensorOptions().dtype(at::kByte).device(device));
-    return t;
+    Scratch::Held &h = s.by_stream[{device.index(), stream}];
+    if (!h.memory.defined() || (size_t)h.memory.numel() < nbytes)
+        h.memory = at::empty({(int64_t)(nbytes > (1u << 20) ? nbytes : (1u << 20))}, at::TensorOptions().dtype(at::kByte).device(device));
+    return {h.memory, &h.launches};
 }
 
-struct Call {                                                // one library call: stream, scratch
-    hipStream_t stream;
-    at::Tensor ws;
-    Call(size_t need, const at::Tensor &on, bool or_less = false) : stream(current_stream()), ws(workspace(need, on.device(), stream, or_less)) {}
-    void *ptr() const { return ws.defined() ? ws.data_ptr() : nullptr; }
-    size_t bytes() const { return ws.defined() ? (size_t)ws.numel() : 0; }
-};
-template <typename F> int unlocked(F &&f)                     // the library call itself runs without the interpreter lock
+template <typename F> int unlocked(F &&f, std::mutex *launches = nullptr)      // the library call itself runs without the interpreter lock
 {
     int rc;
     Py_BEGIN_ALLOW_THREADS
-    rc = f();
+    if (launches != nullptr) {
+        const std::lock_guard<std::mutex> whole(*launches);
+        rc = f();
+    } else {
+        rc = f();
+    }
     Py_END_ALLOW_THREADS
     return rc;
 }
+struct Call {                                                // one library call: stream, scratch
+    hipStream_t stream;
+    Workspace ws;
+    Call(size_t need, const at::Tensor &on, bool or_less = false) : stream(current_stream()), ws(workspace(need, on.device(), stream, or_less)) {}
+    void *ptr() const { return ws.memory.defined() ? ws.memory.data_ptr() : nullptr; }
+    size_t bytes() const { return ws.memory.defined() ? (size_t)ws.memory.numel() : 0; }
+    template <typename F> int run(F &&f) const { return unlocked(f, ws.launches); }
+};
 
 // An output.  The allocator is asked directly, past the dispatcher (a cycle of ten calls in fp32 51.1 -> 47.5 us on the host's side, 59.5 -> 56.1
 // where it is slower), unless something may be listening there: a dispatch mode, tracer or transform (each adds keys to this thread's
@@ -287,7 +300,7 @@ PyObject *bidir(PyObject *const *a, Py_ssize_t n)
     void *const o = dev(out, "O");
     const float *q_s = (const float *)dev(qs, "q_scale"), *k_s = (const float *)dev(ks, "k_scale");
     const Call c(dd_bidir_attention_workspace_bytes(B, H, Hkv, N, d, (dd_dtype)qk, (dd_dtype)vd), Q);
-    check(unlocked([&] { return dd_bidir_attention(q, k, v, o, B, H, Hkv, N, d, (dd_dtype)qk, (dd_dtype)vd, q_s, k_s, c.ptr(),
+    check(c.run([&] { return dd_bidir_attention(q, k, v, o, B, H, Hkv, N, d, (dd_dtype)qk, (dd_dtype)vd, q_s, k_s, c.ptr(),
                                                    c.bytes(), c.stream); }), "dd_bidir_attention");
     return THPVariable_Wrap(out);
 }
@@ -333,19 +346,19 @@ PyObject *block(PyObject *const *a, Py_ssize_t n)
                                  : dd_block_attention_cached_workspace_bytes(bl, B, H, Hkv, N, d, tq, tv), Q);
     switch (kind) {
     case kCached:
-        check(unlocked([&] { return dd_block_attention_cached(q, k, v, o, bs, bl, kb, vb, B, H, Hkv, N, d, tq, tv, q_s, k_s, c.ptr(),
+        check(c.run([&] { return dd_block_attention_cached(q, k, v, o, bs, bl, kb, vb, B, H, Hkv, N, d, tq, tv, q_s, k_s, c.ptr(),
                                                               c.bytes(), c.stream); }), "dd_block_attention_cached");
         break;
     case kRefresh:
-        check(unlocked([&] { return dd_block_attention_refresh(q, k, v, o, bs, bl, kb, vb, B, H, Hkv, N, d, tq, tv, q_s, k_s, c.ptr(),
+        check(c.run([&] { return dd_block_attention_refresh(q, k, v, o, bs, bl, kb, vb, B, H, Hkv, N, d, tq, tv, q_s, k_s, c.ptr(),
                                                                c.bytes(), c.stream); }), "dd_block_attention_refresh");
         break;
     case kWindow:
-        check(unlocked([&] { return dd_block_attention_window(q, k, v, o, bs, bl, ws0, wsn, kb, vb, B, H, Hkv, N, d, tq, tv, q_s, k_s,
+        check(c.run([&] { return dd_block_attention_window(q, k, v, o, bs, bl, ws0, wsn, kb, vb, B, H, Hkv, N, d, tq, tv, q_s, k_s,
                                                               c.ptr(), c.bytes(), c.stream); }), "dd_block_attention_window");
         break;
     default:
-        check(unlocked([&] { return dd_block_attention_batched(q, k, v, o, st, bl, kb, vb, B, H, Hkv, N, d, tq, tv, q_s, k_s, c.ptr(),
+        check(c.run([&] { return dd_block_attention_batched(q, k, v, o, st, bl, kb, vb, B, H, Hkv, N, d, tq, tv, q_s, k_s, c.ptr(),
                                                                c.bytes(), c.stream); }), "dd_block_attention_batched");
     }
     return THPVariable_Wrap(out);
@@ -420,7 +433,7 @@ PyObject *block_fp8v(PyObject *const *a, Py_ssize_t n)
     void *const o = dev(out, "O");
     const float *q_s = (const float *)dev(qs, "q_scale"), *k_s = (const float *)dev(ks, "k_scale"), *v_s = (const float *)dev(vs, "v_scale");
     const Call c(dd_block_attention_cached_fp8v_workspace_bytes(bl, B, H, Hkv, N, d), Q);
-    check(unlocked([&] { return dd_block_attention_cached_fp8v(q, k, v, o, bs, bl, kb, vb, B, H, Hkv, N, d, q_s, k_s, v_s, c.ptr(), c.bytes(),
+    check(c.run([&] { return dd_block_attention_cached_fp8v(q, k, v, o, bs, bl, kb, vb, B, H, Hkv, N, d, q_s, k_s, v_s, c.ptr(), c.bytes(),
                                                                c.stream); }), "dd_block_attention_cached_fp8v");
     return THPVariable_Wrap(out);
 }
@@ -491,11 +504,11 @@ PyObject *verify_remask(PyObject *const *a, Py_ssize_t n)
     float *const ps = (float *)dev(rs.defined() ? &rs : nullptr, "out_scores");
     if (fixed_scratch) {
         const hipStream_t stream = current_stream();
-        check(unlocked([&] { return dd_verify_remask_static(ld, lv, (const uint8_t *)mk, (dd_mode)mode, threshold, seed, pm, pt, ps, B, G, V, dt, stream); }),
-              "dd_verify_remask_static");
+        check(unlocked([&] { return dd_verify_remask_static(ld, lv, (const uint8_t *)mk, (dd_mode)mode, threshold, seed, pm, pt, ps, B, G, V, dt, stream); },
+                       &scratch().static_launches), "dd_verify_remask_static");
     } else {
         const Call c(dd_verify_remask_workspace_bytes(B, G, V, dt), L, true);
-        check(unlocked([&] { return dd_verify_remask(ld, lv, (const uint8_t *)mk, (dd_mode)mode, threshold, seed, pm, pt, ps, B, G, V, dt, c.ptr(),
+        check(c.run([&] { return dd_verify_remask(ld, lv, (const uint8_t *)mk, (dd_mode)mode, threshold, seed, pm, pt, ps, B, G, V, dt, c.ptr(),
                                                      c.bytes(), c.stream); }), "dd_verify_remask");
     }
     return triple(rm, rt, rs);
@@ -530,7 +543,7 @@ PyObject *unmask(PyObject *const *a, Py_ssize_t n)
     int32_t *const pt = (int32_t *)dev(rt, "out_tokens");
     float *const pc = (float *)dev(rc, "out_conf");
     const Call c(dd_unmask_workspace_bytes(B, G, V, dt), L, true);
-    check(unlocked([&] { return dd_unmask(ld, (const uint8_t *)mk, (dd_unmask_mode)mode, threshold, px, pm, pt, pc, B, G, V, dt, c.ptr(), c.bytes(),
+    check(c.run([&] { return dd_unmask(ld, (const uint8_t *)mk, (dd_unmask_mode)mode, threshold, px, pm, pt, pc, B, G, V, dt, c.ptr(), c.bytes(),
                                           c.stream); }), "dd_unmask");
     return triple(rm, rt, rc);
 }
@@ -555,7 +568,7 @@ PyObject *verify_scores(PyObject *const *a, Py_ssize_t n)
     const Call c(dd_verify_scores_workspace_bytes(P, V, dt), L, true);
     float *const pk = (float *)kl.data_ptr(), *const pcv = (float *)cv.data_ptr(), *const pcd = drafter ? (float *)cd.data_ptr() : nullptr;
     int32_t *const ptv = (int32_t *)tv.data_ptr(), *const ptd = drafter ? (int32_t *)td.data_ptr() : nullptr;
-    check(unlocked([&] { return dd_verify_scores(ld, lv, pk, pcv, ptv, pcd, ptd, P, V, dt, c.ptr(), c.bytes(), c.stream); }), "dd_verify_scores");
+    check(c.run([&] { return dd_verify_scores(ld, lv, pk, pcv, ptv, pcd, ptd, P, V, dt, c.ptr(), c.bytes(), c.stream); }), "dd_verify_scores");
     PyObject *t = PyTuple_New(5);
     if (t == nullptr) throw Raised{};
     PyTuple_SET_ITEM(t, 0, THPVariable_Wrap(kl));
@@ -742,7 +755,7 @@ PyObject *paged_attention(PyObject *const *a, Py_ssize_t n)
     const at::Tensor out = O ? *O : empty_like_type({p.B, H, rows, p.d}, Q.scalar_type(), Q);
     void *const o = dev(out, "O");
     const Call c(dd_paged_attention_workspace_bytes(rows, p.B, H, p.Hkv, p.d, p.size, p.max, (dd_dtype)p.tag), Q);
-    check(unlocked([&] { return dd_paged_attention(q, kc, vc, (const float *)sk, (const float *)sv, (const int32_t *)t, (const int32_t *)ln, o, rows, p.B, H, p.Hkv,
+    check(c.run([&] { return dd_paged_attention(q, kc, vc, (const float *)sk, (const float *)sv, (const int32_t *)t, (const int32_t *)ln, o, rows, p.B, H, p.Hkv,
                                                    p.d, p.num, p.size, p.max, (dd_dtype)p.tag, c.ptr(), c.bytes(), c.stream); }), "dd_paged_attention");
     return THPVariable_Wrap(out);
 }
