@@ -143,13 +143,13 @@ def reset_workspace_peak() -> None:
 
 
 def workspace_peak() -> int:
-    """The largest scratch size any call has asked for since reset_workspace_peak()."""
+    """The largest scratch size any call of this thread has asked for since its reset_workspace_peak()."""
     return native().workspace_peak()
 
 
 class fixed_workspace:
-    """Context manager: calls of the binding inside it use `tensor` (uint8, on the GPU) as their scratch memory
-    instead of the per-stream cached one; they must all be ordered on one stream.  For graph capture: the
+    """Context manager: calls of the binding that its thread makes inside it use `tensor` (uint8, on the GPU) as their scratch
+    memory instead of the per-stream cached one; they must all be ordered on one stream.  For graph capture: the
     tensor is allocated before the capture and kept alive by whoever keeps the graph."""
 
     def __init__(self, tensor):

@@ -195,7 +195,7 @@ void check(int rc, const char *where)
 hipStream_t current_stream() { return c10::hip::getCurrentHIPStream().stream(); }
 
 // ---- scratch memory: one tensor per (device, stream) - calls on one stream run in order and may share it, calls on
-// different streams may overlap and must not - or the one a fixed_workspace() block has set.  Guarded by the interpreter
+// different streams may overlap and must not - or the one a fixed_workspace() block of this thread has set.  Guarded by the interpreter
 // lock; never destroyed (the runtime may be gone by then).
 // A call that uses it can be several launches, of which the later ones read what the first one left there, and it is made without the
 // interpreter lock.  So that no other thread's launches on the stream come in between, each scratch tensor has a lock of its own, held
@@ -203,29 +203,30 @@ hipStream_t current_stream() { return c10::hip::getCurrentHIPStream().stream(); 
 struct Scratch {
     struct Held { at::Tensor memory; std::mutex launches; };
     std::map<std::pair<int, hipStream_t>, Held> by_stream;
-    at::Tensor fixed;
-    std::mutex fixed_launches, static_launches;              // (the second: of the calls that use the library's own array)
-    size_t peak = 0;
+    std::mutex fixed_launches, static_launches;              // of calls in fixed workspaces, and of those that use the library's own array
 };
 Scratch &scratch()
 {
     static Scratch *s = new Scratch;
     return *s;
 }
+// What a thread has set, and the most that its calls have asked for: its own, so that one that captures a graph neither lends its
+// scratch tensor to the calls of others nor takes their needs for its own.  (A pointer, as nothing may be freed when a thread ends late.)
+thread_local at::Tensor *fixed = nullptr;
+thread_local size_t peak = 0;
 struct Workspace { at::Tensor memory; std::mutex *launches = nullptr; };
 // (`or_less`: the library itself says whether a fixed workspace of fewer bytes serves the call)
 Workspace workspace(size_t nbytes, const at::Device &device, hipStream_t stream, bool or_less)
 {
     if (nbytes == 0) return {};
-    Scratch &s = scratch();
-    if (nbytes > s.peak) s.peak = nbytes;
-    if (s.fixed.defined()) {
-        if (((size_t)s.fixed.numel() < nbytes && !or_less) || s.fixed.device() != device) {
+    if (nbytes > peak) peak = nbytes;
+    if (fixed != nullptr) {
+        if (((size_t)fixed->numel() < nbytes && !or_less) || fixed->device() != device) {
             PyErr_Format(PyExc_RuntimeError, "the fixed workspace holds %lld bytes on %s; this call needs %zu on %s",
-                         (long long)s.fixed.numel(), s.fixed.device().str().c_str(), nbytes, device.str().c_str());
+                         (long long)fixed->numel(), fixed->device().str().c_str(), nbytes, device.str().c_str());
             throw Raised{};
         }
-        return {s.fixed, &s.fixed_launches};
+        return {*fixed, &scratch().fixed_launches};
     }
     if (c10::hip::currentStreamCaptureStatusMayInitCtx() != c10::hip::CaptureStatus::None) {
         // memory allocated under capture would come from that graph's private pool and a cached tensor of it
@@ -235,7 +236,7 @@ Workspace workspace(size_t nbytes, const at::Device &device, hipStream_t stream,
                         "capture through paper_2604_05250_amd.step.capture_step, or inside fixed_workspace()");
         throw Raised{};
     }
-    Scratch::Held &h = s.by_stream[{device.index(), stream}];
+    Scratch::Held &h = scratch().by_stream[{device.index(), stream}];
     if (!h.memory.defined() || (size_t)h.memory.numel() < nbytes)
         h.memory = at::empty({(int64_t)(nbytes > (1u << 20) ? nbytes : (1u << 20))}, at::TensorOptions().dtype(at::kByte).device(device));
     return {h.memory, &h.launches};
@@ -775,21 +776,22 @@ PyObject *set_fixed_workspace(PyObject *const *a, Py_ssize_t n)
     want(n, 1);
     const at::Tensor *t = opt_tensor(a[0], "workspace");
     if (t) dev(t, "workspace");
-    at::Tensor prev = scratch().fixed;
-    scratch().fixed = t ? *t : at::Tensor();
+    const at::Tensor prev = fixed != nullptr ? *fixed : at::Tensor();
+    delete fixed;
+    fixed = t ? new at::Tensor(*t) : nullptr;
     if (!prev.defined()) Py_RETURN_NONE;
     return THPVariable_Wrap(prev);
 }
 PyObject *reset_workspace_peak(PyObject *const *, Py_ssize_t n)
 {
     want(n, 0);
-    scratch().peak = 0;
+    peak = 0;
     Py_RETURN_NONE;
 }
 PyObject *workspace_peak(PyObject *const *, Py_ssize_t n)
 {
     want(n, 0);
-    return PyLong_FromSize_t(scratch().peak);
+    return PyLong_FromSize_t(peak);
 }
 
 template <PyObject *(*F)(PyObject *const *, Py_ssize_t)>
