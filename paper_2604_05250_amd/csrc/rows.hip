@@ -9,9 +9,11 @@
 // are chosen so that the two members of every pair are in one lane, and so a rotation needs no exchange; and so that the first chunks of
 // the lanes lie side by side, and the second ones.  (Both of a lane side by side - every other piece of a row for each load and store -
 // made the pairing of neighbours slower: 4 x 2046 rows of 64 heads of 64, fp32, 122 us, 13 x 2613 of 32 heads of 128, bf16, 178.)
-// Angles: position * inv_freq in revolutions, in fp64, and its fraction to fp32 (a product in fp32 is off by 2^-24 of the angle:
-// a hundredth of a radian at position 130000).  The hardware's sine and cosine take revolutions and are off by 2^-23 (measured over
-// [0, 1] against fp64).
+// Angles: position * inv_freq in revolutions, in fp64, and its distance from the nearest whole one to fp32 (a product in fp32 is off by
+// 2^-24 of the angle: a hundredth of a radian at position 130000).  The hardware's sine and cosine take revolutions.  They are off by
+// 2^-23 (measured over [0, 1] against fp64) and the angle in fp32 by up to 2^-26 revolutions, 1.6 x 2^-24 rad: far below half a step of
+// bf16 and e4m3.  Where rows stay fp32, whose half step is 2^-24, sine and cosine are the exact functions of the fp32 angle, corrected by
+// what it leaves out, and the norm's root and reciprocal are the rounded ones.
 #include "attention_common.h"
 #include "dd_internal.h"
 
@@ -113,17 +115,35 @@ template <int D> __device__ __forceinline__ Pairing pairing(int lane, int rot, b
 
 enum { kNoTurn = 0, kHalves = 1, kNeighbours = 2 };
 
-// cos and sin of the eight angles of a lane at a position; elements that stay as they are get 1 and 0
-__device__ __forceinline__ void turn_of(const float *inv_freq, const Pairing &p, double position, float *c, float *s)
+// cos and sin of the eight angles of a lane at a position; elements that stay as they are get 1 and 0.  EXACT: to fp32's last bits.
+// (fp32, us exact / with the hardware's functions: 4 x 2048 rows of 40 heads 62 / 75, neighbours paired 65 / 64; 16 x 64 rows 7.9 / 9.9,
+// neighbours 7.8 / 7.0.  Relative error of random rows against fp64, rms: 4.1e-8 / 9.3e-8.)
+template <bool EXACT> __device__ __forceinline__ void turn_of(const float *inv_freq, const Pairing &p, double position, float *c, float *s)
 {
-    const double q = position * 0.15915494309189533577;      // 1 / 2 pi
+    constexpr double kTurn = 0.15915494309189535, kTurnRest = -9.839338337591243e-18;        // 1 / 2 pi, and what the first number lacks
+    const double q = position * kTurn;
     const float *const fa = inv_freq + (p.ta ? p.fa : 0), *const fb = inv_freq + (p.tb ? p.fb : 0);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float r = (float)__builtin_amdgcn_fract((double)(i < 4 ? fa[i] : fb[i - 4]) * q);      // revolutions
+        const double f = (double)(i < 4 ? fa[i] : fb[i - 4]);
+        float cs, sn;
+        if constexpr (EXACT) {
+            const double a = position * f, turns = a * kTurn;                                // (a product has 55 bits)
+            const double r = (turns - __builtin_rint(turns)) + (__builtin_fma(a, kTurn, -turns) + __builtin_fma(__builtin_fma(position, f, -a), kTurn, a * kTurnRest));
+            const float near = (float)r, rest = 6.2831853f * (float)(r - (double)near);
+            float s0, c0;
+            sincospif(2.0f * near, &s0, &c0);
+            cs = __builtin_fmaf(-s0, rest, c0);
+            sn = __builtin_fmaf(c0, rest, s0);
+        } else {
+            const double turns = f * q;
+            const float r = (float)(turns - __builtin_rint(turns));
+            cs = __builtin_amdgcn_cosf(r);
+            sn = __builtin_amdgcn_sinf(r);
+        }
         const bool turns = i < 4 ? p.ta : p.tb;
-        c[i] = turns ? __builtin_amdgcn_cosf(r) : 1.0f;
-        s[i] = turns ? __builtin_amdgcn_sinf(r) : 0.0f;
+        c[i] = turns ? cs : 1.0f;
+        s[i] = turns ? sn : 0.0f;
     }
 }
 template <int PAIR> __device__ __forceinline__ void rotate(float *x, const float *c, const float *s)     // x: both chunks, 16 values
@@ -147,12 +167,12 @@ template <typename T> __device__ __forceinline__ void weights_of(const void *wei
     unpack(load_chunk<T>(static_cast<const uint8_t *>(weight), p.a), w);
     unpack(load_chunk<T>(static_cast<const uint8_t *>(weight), p.b), w + 8);
 }
-template <int D> __device__ __forceinline__ void norm(float *x, const float *w, float eps, bool normed)
+template <int D, bool EXACT> __device__ __forceinline__ void norm(float *x, const float *w, float eps, bool normed)
 {
     float q = 0;
 #pragma unroll
     for (int i = 0; i < 16; ++i) q += x[i] * x[i];
-    const float root = __builtin_amdgcn_rsqf(row_sum<D / 16>(q) * (1.0f / D) + eps), r = normed ? root : 1.0f;
+    const float mean = row_sum<D / 16>(q) * (1.0f / D) + eps, root = EXACT ? 1.0f / sqrtf(mean) : __builtin_amdgcn_rsqf(mean), r = normed ? root : 1.0f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) x[i] = x[i] * r * w[i];
 }
@@ -168,6 +188,7 @@ template <typename T, int D, bool NORM, int PAIR>
 __global__ __launch_bounds__(256) void norm_rotate_kernel(NormRotateArgs a)
 {
     constexpr int LANES = D / 16, TOKENS = 256 / LANES;
+    constexpr bool EXACT = std::is_same<T, F32>::value;
     constexpr int U = 4 / (T::bytes / 2);                    // heads on their way
     const int lane = threadIdx.x % LANES;
     const unsigned token = blockIdx.x * TOKENS + threadIdx.x / LANES;
@@ -191,7 +212,7 @@ __global__ __launch_bounds__(256) void norm_rotate_kernel(NormRotateArgs a)
 
     float w[16], c[8], s[8];
     if constexpr (NORM) weights_of<T>(side.weight, p, w);
-    if constexpr (PAIR != kNoTurn) turn_of(a.inv_freq, p, a.positions != nullptr ? (double)a.positions[token] : (double)i, c, s);
+    if constexpr (PAIR != kNoTurn) turn_of<EXACT>(a.inv_freq, p, a.positions != nullptr ? (double)a.positions[token] : (double)i, c, s);
     const bool normed = NORM && side.weight != nullptr;
     for (int h0 = 0; h0 < count; h0 += U) {
 #pragma unroll
@@ -200,7 +221,7 @@ __global__ __launch_bounds__(256) void norm_rotate_kernel(NormRotateArgs a)
             unpack(in[u][0], x);
             unpack(in[u][1], x + 8);
             fetch(h0 + U + u, u);
-            if constexpr (NORM) norm<D>(x, w, a.eps, normed);
+            if constexpr (NORM) norm<D, EXACT>(x, w, a.eps, normed);
             if constexpr (PAIR != kNoTurn) rotate<PAIR>(x, c, s);
             if (h0 + u < count) {
                 uint8_t *row = dst + (long)(h0 + u) * a.n * D * T::bytes;
@@ -307,7 +328,7 @@ __device__ __forceinline__ void append_page(const PageAppendArgs &a, unsigned bi
     const bool normed = a.weight != nullptr, turns = a.rot > 0;
     if constexpr (!VALUES) {
         weights_of<T>(a.weight, p, w);
-        if (turns) turn_of(a.inv_freq, p, (double)pos, c, s);
+        if (turns) turn_of<false>(a.inv_freq, p, (double)pos, c, s);
     }
 
     // the keys and head dims of values that this thread stores: TURNS times 16 bytes of each of DIMS head dims
@@ -342,7 +363,7 @@ __device__ __forceinline__ void append_page(const PageAppendArgs &a, unsigned bi
         unpack(in[1], x + 8);
         fetch(min(g + 1, g_end - 1));
         if constexpr (!VALUES) {
-            if (normed) norm<D>(x, w, a.eps, true);
+            if (normed) norm<D, false>(x, w, a.eps, true);
             if (turns) {
                 if (a.interleaved) rotate<kNeighbours>(x, c, s);
                 else rotate<kHalves>(x, c, s);
