@@ -315,8 +315,8 @@ int dd_qk_norm_rope(const void *Q, int64_t q_batch, int64_t q_head, int64_t q_ro
  * nor below kv_lens[b] are left as they are.  A scale is positive, finite and normal (not subnormal) wherever the page holds
  * positions; rows for DD_FP8_E4M3 pages are finite (one that is not spoils its own page and head, no other).
  * The pages that a call writes must be distinct (else which rows and which scale win is unspecified); pages that are only read
- * later (a shared prefix) may be shared.  Kc and Vc overlap neither each other nor K or V (DD_ERR_SHAPE).  The caller owns
- * kv_lens: the call does not write it.
+ * later (a shared prefix) may be shared.  Kc and Vc, and with DD_FP8_E4M3 k_scale and v_scale, overlap neither each other nor K
+ * or V (DD_ERR_SHAPE).  The caller owns kv_lens: the call does not write it.
  * d in {64, 128}; B, Hkv, num_pages, max_pages >= 1; n >= 0 (0: a no-op); max_pages*page_size < 2^30, num_pages*Hkv*page_size*d
  * < 2^40, B*Hkv*n*d < 2^40, B*(n + 2 page_size)*d < 2^34.
  * Errors: DD_ERR_NULL (scales are required with DD_FP8_E4M3), DD_ERR_SHAPE, DD_ERR_DTYPE, DD_ERR_ALIGN, DD_ERR_LAUNCH.
@@ -336,8 +336,9 @@ int dd_paged_cache_append(void *Kc, void *Vc, float *k_scale, float *v_scale,
  * with K_j, V_j of kv head h*Hkv/H as the cache holds them; the block's own rows take part by being appended first.
  * kv_lens[b] is clamped to [0, max_pages*page_size]; positions whose page is not in [0, num_pages) take no part; a sequence
  * without a position that does gets zeros.  Slots that hold no position may hold anything, NaN included.
- *   Q, O [B,H,n,d] DD_BF16, dense;  O overlaps neither Q nor the cache (DD_ERR_SHAPE);  cache_dtype DD_BF16 or DD_FP8_E4M3 (then
- *   k_scale and v_scale are required; wherever a page holds positions they are positive, finite, normal and at most 2^119)
+ *   Q, O [B,H,n,d] DD_BF16, dense;  O overlaps neither Q nor the cache nor its scales (DD_ERR_SHAPE);  cache_dtype DD_BF16 or
+ *   DD_FP8_E4M3 (then k_scale and v_scale are required; wherever a page holds positions they are positive, finite, normal and at
+ *   most 2^119)
  * Arithmetic: matrix cores with fp32 accumulation, e4m3 codes decoded exactly to bf16, k_scale in the exponent's factor, fp32
  * online softmax, weights (times the significand of v_scale, in [1, 2)) rounded to bf16 before the PV product.
  * The key range is split over workgroups where those are few; the partial states live in `workspace`.  A capacity

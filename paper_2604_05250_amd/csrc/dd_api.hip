@@ -525,6 +525,14 @@ int dd_paged_cache_append(void *Kc, void *Vc, float *k_scale, float *v_scale,
     if (overlap(Kc, cache_bytes, Vc, cache_bytes) || overlap(Kc, cache_bytes, K, k_reach) || overlap(Kc, cache_bytes, V, v_reach) ||
         overlap(Vc, cache_bytes, K, k_reach) || overlap(Vc, cache_bytes, V, v_reach))
         return DD_ERR_SHAPE;
+    if (cache_dtype == DD_FP8_E4M3) {                        // each is read and written by one of a page's two workgroups, unordered with the other
+        const uintptr_t scale_bytes = (uintptr_t)num_pages * Hkv * sizeof(float);
+        if (overlap(k_scale, scale_bytes, v_scale, scale_bytes)) return DD_ERR_SHAPE;
+        for (const float *scale : {k_scale, v_scale})
+            if (overlap(scale, scale_bytes, Kc, cache_bytes) || overlap(scale, scale_bytes, Vc, cache_bytes) || overlap(scale, scale_bytes, K, k_reach) ||
+                overlap(scale, scale_bytes, V, v_reach))
+                return DD_ERR_SHAPE;
+    }
     dd::PageAppendArgs a;
     auto side = [&](dd::PageAppendSide &s, const void *x, void *cache, float *scale, const int64_t *st) {
         s.x = x; s.cache = cache; s.scale = cache_dtype == DD_FP8_E4M3 ? scale : nullptr;
@@ -572,6 +580,8 @@ int dd_paged_attention(const void *Q, const void *Kc, const void *Vc, const floa
     if (rc != DD_OK) return rc;
     const uintptr_t rows_bytes = (uintptr_t)B * H * n * d * 2, cache_bytes = (uintptr_t)num_pages * Hkv * page_size * d * (fp8 ? 1 : 2);
     if (overlap(O, rows_bytes, Q, rows_bytes) || overlap(O, rows_bytes, Kc, cache_bytes) || overlap(O, rows_bytes, Vc, cache_bytes)) return DD_ERR_SHAPE;
+    const uintptr_t scale_bytes = (uintptr_t)num_pages * Hkv * sizeof(float);
+    if (fp8 && (overlap(O, rows_bytes, k_scale, scale_bytes) || overlap(O, rows_bytes, v_scale, scale_bytes))) return DD_ERR_SHAPE;
     dd::PagedAttnArgs a;
     a.Q = Q; a.Kc = Kc; a.Vc = Vc; a.O = O;
     a.k_scale = fp8 ? k_scale : nullptr; a.v_scale = fp8 ? v_scale : nullptr;
