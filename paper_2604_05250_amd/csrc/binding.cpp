@@ -144,10 +144,17 @@ void one_byte(const at::Tensor &t, const char *what, const char *msg)
 // Shapes say how many elements the library reads and writes, dtype tags how large they are: a tensor that holds fewer bytes
 // than that never gets to a launch.
 int64_t tag_bytes(int tag) { return tag == DD_F32 ? 4 : tag == DD_BF16 ? 2 : tag == DD_FP8_E4M3 ? 1 : 0; }
+// A tensor of floating-point numbers has to be of the tag's kind (fp16 has bf16's width, e5m2 has e4m3's); integers are taken as the bits.
 void elements_of(const at::Tensor *t, int tag, const char *what)
 {
-    if (t == nullptr || tag_bytes(tag) == 0 || (int64_t)t->element_size() == tag_bytes(tag)) return;   // (no tag: the library refuses it)
-    PyErr_Format(PyExc_TypeError, "%s: elements of %lld bytes expected, has %s", what, (long long)tag_bytes(tag), c10::toString(t->scalar_type()));
+    if (t == nullptr || tag_bytes(tag) == 0) return;         // (no tag: the library refuses it)
+    const at::ScalarType kind = tag == DD_F32 ? at::kFloat : tag == DD_BF16 ? at::kBFloat16 : at::kFloat8_e4m3fn;
+    if ((int64_t)t->element_size() != tag_bytes(tag))
+        PyErr_Format(PyExc_TypeError, "%s: elements of %lld bytes expected, has %s", what, (long long)tag_bytes(tag), c10::toString(t->scalar_type()));
+    else if (t->scalar_type() != kind && !at::isIntegralType(t->scalar_type(), true))
+        PyErr_Format(PyExc_TypeError, "%s: %s expected, has %s", what, c10::toString(kind), c10::toString(t->scalar_type()));
+    else
+        return;
     throw Raised{};
 }
 void room_for(const at::Tensor *t, int64_t elements, int64_t bytes_each, const char *what)
