@@ -281,7 +281,8 @@ int dd_cache_insert_rows(void *Kc, void *Vc, const void *Krows, const void *Vrow
  *   K  the same with Hkv heads and its own strides; K == NULL (then Ko == NULL): queries only
  *   Qo [B,H,n,d], Ko [B,Hkv,n,d]  dense, dtype.  Qo may be Q (and Ko may be K) where that is dense itself; any other overlap of
  *      an output with Q or K, or of the two outputs, is DD_ERR_SHAPE
- *   q_weight, k_weight [d] dtype, 16-byte aligned; each may be NULL; with either, eps must be > 0 and finite
+ *   q_weight, k_weight [d] dtype, 16-byte aligned; each may be NULL; with either, eps must be > 0, finite and normal (not
+ *      subnormal), and the squares of a row add to less than 2^128
  *   inv_freq [rot_dim/2] f32; rot_dim a multiple of 16, at most d        positions [B*n] i32, any value
  * d in {64, 128}; B, H >= 1, Hkv >= 1 with K; n >= 0 (0: a no-op); B*n < 2^31, B*n*d < 2^36, B*H*n*d and
  * B*Hkv*n*d < 2^40.

@@ -432,7 +432,7 @@ static int check_rotation(const void *weight, float eps, const float *inv_freq, 
 {
     if (rot_dim < 0 || rot_dim > d || rot_dim % 16 != 0) return DD_ERR_SHAPE;
     if (rot_dim > 0 && !inv_freq) return DD_ERR_NULL;
-    if (weight && !(eps > 0.0f && eps <= 3.0e38f)) return DD_ERR_SHAPE;
+    if (weight && !(eps >= 1.17549435e-38f && eps <= 3.402823466e38f)) return DD_ERR_SHAPE;        // (normal: the reciprocal root takes others for 0)
     if (misaligned16(weight) || (reinterpret_cast<uintptr_t>(inv_freq) & 3u) != 0) return DD_ERR_ALIGN;
     return DD_OK;
 }
