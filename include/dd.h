@@ -342,8 +342,9 @@ int dd_paged_cache_append(void *Kc, void *Vc, float *k_scale, float *v_scale,
  *   most 2^119)
  * Arithmetic: matrix cores with fp32 accumulation, e4m3 codes decoded exactly to bf16, k_scale in the exponent's factor, fp32
  * online softmax, weights (times the significand of v_scale, in [1, 2)) rounded to bf16 before the PV product.
- * The key range is split over workgroups where those are few; the partial states live in `workspace`.  A capacity
- * max_pages*page_size far above the lengths costs workspace, not time: a sequence's own keys are shared out.
+ * The key range is split over workgroups where those are few; the partial states live in `workspace`.  Whether it is goes by the
+ * capacity max_pages*page_size, how a sequence's keys are shared out by its own length: a capacity far above the lengths costs
+ * workspace, and a few microseconds for the launch that merges partial states.
  * d in {64, 128}; H % Hkv == 0; B, H, Hkv, num_pages, max_pages >= 1; n >= 0 (0: a no-op); max_pages*page_size < 2^30,
  * num_pages*Hkv*page_size*d < 2^40, B*H*n < 2^30, B*Hkv*ceil(n*H/Hkv / 32) < 2^24.
  * Errors: as above, and DD_ERR_WORKSPACE.

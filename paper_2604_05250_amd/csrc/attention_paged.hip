@@ -42,7 +42,9 @@ constexpr float kNone = -1.0e30f;        // the reference of a row that has met 
 constexpr int kMaxSplits = 64;
 [[maybe_unused]] constexpr int kWaves = 4;           // per workgroup
 constexpr int kFewRows = 32;             // of a key/value head: one row block
-constexpr int kSplitTiles = 4, kSplitTilesMany = 8;        // tiles of 64 keys that a split has at least, with few rows and with more
+constexpr int kUnits = 256;              // compute units
+// tiles of 64 keys that a split has at least: with few rows, with more, and with more where workgroups share a compute unit
+constexpr int kSplitTiles = 4, kSplitTilesMany = 8, kSplitTilesShared = 32;
 
 __device__ __forceinline__ unsigned pack_bf16(float lo, float hi)
 {
@@ -82,15 +84,27 @@ struct PagedTail {
     float scale_log2;                    // log2(e) / sqrt(d)
 };
 #define DD_PAGED_HEAD const int32_t *table, const int32_t *kv_lens, const uint8_t *Kc, const uint8_t *Vc, int Hkv, int rows_total, int num_pages, \
-                      int max_pages, unsigned wgs, unsigned shape      // shape: row tiles, splits - 1 (6 bits), log2(page_size / 16) (2 bits)
+                      int max_pages, unsigned launched, unsigned shape // launched: workgroups, kLongSplits; shape: row tiles, splits - 1 (6
+                                                                       // bits), log2(page_size / 16) (2 bits)
 
-// How a sequence's tiles are shared out over the splits of a call: tiles per split and splits that have any.
+// How a sequence's tiles are shared out over the splits of a call: tiles per split and splits that have any.  The call's splits go by what
+// its table can hold, a sequence's by what it holds: with many rows and more workgroups than compute units (kLongSplits) only long ones
+// pay.  Workgroups that have none may not sit between the others (26.0 us where the first figure below is 20.8), so this is for calls whose
+// row blocks the eight XCDs share evenly.  us with this / with splits of half of the keys, and at a table that is no wider than that,
+// 64 rows, 32/8 heads:
+//     sequences x keys, table     e4m3                  bf16
+//     4 x 2048, 8192              20.8 / 23.4, 18.3     23.4 / 25.2, 21.1
+//     3 x 2048, 8192              19.0 / 20.3, 16.1     22.2 / 23.0, 19.1
+//     4 x 3008, 4096              26.0 / 26.8           30.2 / 31.8
+//     3 x 3008, 4096              24.6 / 24.7, 21.9     29.3 / 28.3, 26.3
+constexpr unsigned kLongSplits = 1u << 31;
 struct Share { int tiles, per_split, used, len; };
-__device__ __forceinline__ Share share_of(int len, int max_pages, int page_log2, int splits, int rows_total)
+__device__ __forceinline__ Share share_of(int len, int max_pages, int page_log2, int splits, int rows_total, unsigned launched)
 {
     Share s;
     s.len = min(max(len, 0), max_pages << page_log2);        // (less than 2^30)
     s.tiles = (int)(((unsigned)s.len + 63u) >> 6);
+    if (launched & kLongSplits) splits = min(splits, max(s.tiles / kSplitTilesShared, 1));
     s.per_split = max((s.tiles + splits - 1) / splits, rows_total <= kFewRows ? kSplitTiles : kSplitTilesMany);
     s.used = s.tiles == 0 ? 0 : (s.tiles + s.per_split - 1) / s.per_split;
     return s;
@@ -135,9 +149,13 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(DD_PAGED_HEAD, Paged
     const int P_log2 = 4 + (int)(shape & 3), splits = (int)(shape >> 2 & 63) + 1;
     unsigned bid = blockIdx.x;
     {                                                // workgroups that share keys: on one XCD
-        const unsigned per = wgs >> 3, rem = wgs & 7;
+        const unsigned wgs = launched & ~kLongSplits, per = wgs >> 3, rem = wgs & 7;
         const unsigned xcd = bid & 7, slot = bid >> 3;
         bid = xcd * per + min(xcd, rem) + slot;
+        if (launched & kLongSplits) {                // and there split after split, each of all of them: units get as much of each
+            const unsigned each = per / (unsigned)splits, s = slot / each, pair = xcd * each + (slot - s * each), tiles = shape >> 8;
+            bid = (pair / tiles * (unsigned)splits + s) * tiles + pair % tiles;
+        }
     }
     int rt, sp;
     place_of(bid, shape >> 8, rt);
@@ -160,7 +178,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(DD_PAGED_HEAD, Paged
         next = pages_of(stream + STREAMS);
         after = pages_of(stream + 2 * STREAMS);
     }
-    const Share sh = share_of(held, max_pages, P_log2, splits, rows_total);
+    const Share sh = share_of(held, max_pages, P_log2, splits, rows_total, launched);
     if (sp >= sh.used && sp > 0) return;
     const int v_first = (rt * RG + block) * 32;
     const size_t row_base = (size_t)head * rows_total;
@@ -657,7 +675,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(DD_PAGED_HEAD, Paged
 // with leading scalar arguments, as above).
 template <int D>
 __global__ __launch_bounds__(256) void paged_merge_kernel(const float *part_ml, const float *part_o, const int32_t *kv_lens, uint8_t *O, int Hkv, int rows_total,
-                                                          int max_pages, unsigned shape, int rows)
+                                                          int max_pages, unsigned shape, unsigned launched, int rows)
 {
     constexpr int LANES = D / 4;
     const int row = blockIdx.x * (256 / LANES) + threadIdx.x / LANES, d0 = (threadIdx.x % LANES) * 4;
@@ -678,7 +696,7 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(const float *part_ml, 
     };
     fetch(0);
     const unsigned b = (unsigned)row / (unsigned)rows_total / (unsigned)Hkv;
-    const int used = share_of(kv_lens[b], max_pages, 4 + (int)(shape & 3), splits, rows_total).used;
+    const int used = share_of(kv_lens[b], max_pages, 4 + (int)(shape & 3), splits, rows_total, launched).used;
     if (used <= 1) return;
     float M = kNone, L = 0;
     floatx4 x = {0, 0, 0, 0};
@@ -706,7 +724,7 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(const float *part_ml, 
     *reinterpret_cast<uint2 *>(O + ((size_t)row * D + d0) * 2) = make_uint2(pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv));
 }
 
-struct Plan { int rg, splits; long row_tiles, wgs; };        // splits: at most kMaxSplits, row tiles: less than 2^24
+struct Plan { int rg, splits; long row_tiles, wgs; bool long_splits; };      // splits: at most kMaxSplits, row tiles: less than 2^24
 Plan plan_of(int n, int B, int H, int Hkv, long capacity, bool fp8)
 {
     const long rows = (long)(H / Hkv) * n, heads = (long)B * Hkv, blocks = heads * ((rows + 31) / 32), tiles = capacity / 64;
@@ -730,23 +748,26 @@ Plan plan_of(int n, int B, int H, int Hkv, long capacity, bool fp8)
     // 2048 16.1 / 20.6 / 23.9 / - / -, 8192 46.6 / 42.9 / 41.1 / 46.0 / -; four 2048 16.3 / 22.8 / 26.1 / - / -, 8192 47.7 / 48.3 / 51.3 / 59.6 / -.
     // Calls a little past one or two workgroups per compute unit wait for the few that share one: 264 of 3937 positions 34.1 / 38.5 / 37.9 / - / -.
     auto up_to = [&](long want, long least) { return want < tiles / least ? want : tiles / least; };
-    long s = p.rg == 1 ? up_to(256 / base, kSplitTiles) : 1;
+    long s = p.rg == 1 ? up_to(kUnits / base, kSplitTiles) : 1;
     if (!few && p.rg < 4) {
-        const long twice = up_to(512 / base, 4 * kSplitTilesMany);
+        const long twice = up_to(2 * kUnits / base, kSplitTilesShared);
         s = s > twice ? s : twice;
     }
     if (capacity < (few ? 1024 : 1200)) s = 1;
     if (s > kMaxSplits) s = kMaxSplits;
     p.splits = s < 1 ? 1 : (int)s;
     p.wgs = base * p.splits;
+    p.long_splits = !few && p.wgs > kUnits && p.splits > 1 && base % 8 == 0;
     return p;
 }
+
+unsigned launched_of(const Plan &p) { return (unsigned)p.wgs | (p.long_splits ? kLongSplits : 0u); }       // (fewer than 2^24)
 
 template <int D, bool FP8, int NT, bool ONE> hipError_t attend(const PagedAttnArgs &a, const PagedTail &tail, const Plan &p, unsigned shape, hipStream_t stream)
 {
     auto run = [&](auto kernel) {
         return launch(kernel, dim3((unsigned)p.wgs), dim3(256), stream, a.table, a.kv_lens, static_cast<const uint8_t *>(a.Kc), static_cast<const uint8_t *>(a.Vc), a.Hkv,
-                      (a.H / a.Hkv) * a.n, a.num_pages, a.max_pages, (unsigned)p.wgs, shape, tail);
+                      (a.H / a.Hkv) * a.n, a.num_pages, a.max_pages, launched_of(p), shape, tail);
     };
     return p.rg == 1 ? run(attn_paged_kernel<D, FP8, NT, ONE, 1>) : p.rg == 2 ? run(attn_paged_kernel<D, FP8, NT, ONE, 2>) : run(attn_paged_kernel<D, FP8, NT, ONE, 4>);
 }
@@ -777,7 +798,10 @@ hipError_t launch_attention_paged(const PagedAttnArgs &a, hipStream_t stream)
     if (e != hipSuccess || p.splits <= 1) return e;
     const unsigned per_wg = 256 / (a.d / 4);
     const dim3 grid((unsigned)((rows + per_wg - 1) / per_wg));
-    auto merge = [&](auto kernel) { return launch(kernel, grid, dim3(256), stream, tail.part_ml, tail.part_o, a.kv_lens, tail.O, a.Hkv, (a.H / a.Hkv) * a.n, a.max_pages, shape, (int)rows); };
+    auto merge = [&](auto kernel) {
+        return launch(kernel, grid, dim3(256), stream, tail.part_ml, tail.part_o, a.kv_lens, tail.O, a.Hkv, (a.H / a.Hkv) * a.n, a.max_pages, shape,
+                      launched_of(p), (int)rows);
+    };
     return a.d == 128 ? merge(paged_merge_kernel<128>) : merge(paged_merge_kernel<64>);
 }
 
