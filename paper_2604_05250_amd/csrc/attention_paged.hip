@@ -18,7 +18,7 @@
 // the vector units have work at the same time; neither then idles for long, and the clock gives way to their load.  The states are
 // merged through LDS, the key range is split over workgroups where those are few, and the splits' states are merged by a second kernel.
 // e4m3 codes become bf16 exactly in registers.  k_scale goes into the factor of the exponent; of v_scale the power of two goes into the
-// decoding of V, which is exact (bf16 for its range: scales span 2^-126 .. 2^119), and the rest, 1 where this library made the scale,
+// decoding of V, which is exact (bf16 for its range: scales span 2^-126 .. 2^88), and the rest, 1 where this library made the scale,
 // into the exponent.  Weights are rounded to bf16 (2^-8 of each at most, as the result is), their sum is the one of the rounded ones.
 #include "attention_common.h"
 #include "dd_internal.h"
