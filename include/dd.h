@@ -339,7 +339,8 @@ int dd_paged_cache_append(void *Kc, void *Vc, float *k_scale, float *v_scale,
  * without a position that does gets zeros.  Slots that hold no position may hold anything, NaN included.
  *   Q, O [B,H,n,d] DD_BF16, dense;  O overlaps neither Q nor the cache nor its scales (DD_ERR_SHAPE);  cache_dtype DD_BF16 or
  *   DD_FP8_E4M3 (then k_scale and v_scale are required; wherever a page holds positions they are positive, finite, normal and at
- *   most 2^88; values on DD_BF16 pages are below 2^97: fp32 holds the sum of as many as a table can have)
+ *   most 2^88; values on DD_BF16 pages are below 2^97, scores below 2^96 in magnitude: fp32 holds the sums of as many as a table
+ *   can have)
  * Arithmetic: matrix cores with fp32 accumulation, e4m3 codes decoded exactly to bf16, k_scale in the exponent's factor, fp32
  * online softmax, weights (times the significand of v_scale, in [1, 2)) rounded to bf16 before the PV product.
  * The key range is split over workgroups where those are few; the partial states live in `workspace`.  Whether it is goes by the

@@ -10,10 +10,10 @@
 // the lanes lie side by side, and the second ones.  (Both of a lane side by side - every other piece of a row for each load and store -
 // made the pairing of neighbours slower: 4 x 2046 rows of 64 heads of 64, fp32, 122 us, 13 x 2613 of 32 heads of 128, bf16, 178.)
 // Angles: position * inv_freq in revolutions, in fp64, and its distance from the nearest whole one to fp32 (a product in fp32 is off by
-// 2^-24 of the angle: a hundredth of a radian at position 130000).  The hardware's sine and cosine take revolutions.  They are off by
-// 2^-23 (measured over [0, 1] against fp64) and the angle in fp32 by up to 2^-26 revolutions, 1.6 x 2^-24 rad: far below half a step of
-// bf16 and e4m3.  Where rows stay fp32, whose half step is 2^-24, sine and cosine are the exact functions of the fp32 angle, corrected by
-// what it leaves out, and the norm's root and reciprocal are the rounded ones.
+// 2^-24 of the angle: a hundredth of a radian at position 130000).  Where a result is bf16, the hardware's sine and cosine, which take
+// revolutions and are off by 2^-23 (measured over [0, 1] against fp64), and its reciprocal root: far below its half step of 2^-8.  Where
+// fp32 arithmetic shows - fp32 rows, and e4m3 pages, on which a key next to a border between two codes goes the other way as often as its
+// error is large - sine and cosine to a step of fp32, and the rounded root and reciprocal.
 #include "attention_common.h"
 #include "dd_internal.h"
 
@@ -115,10 +115,25 @@ template <int D> __device__ __forceinline__ Pairing pairing(int lane, int rot, b
 
 enum { kNoTurn = 0, kHalves = 1, kNeighbours = 2 };
 
-// cos and sin of the eight angles of a lane at a position; elements that stay as they are get 1 and 0.  EXACT: to fp32's last bits.
-// (fp32, us exact / with the hardware's functions: 4 x 2048 rows of 40 heads 62 / 75, neighbours paired 65 / 64; 16 x 64 rows 7.9 / 9.9,
-// neighbours 7.8 / 7.0.  Relative error of random rows against fp64, rms: 4.1e-8 / 9.3e-8.)
-template <bool EXACT> __device__ __forceinline__ void turn_of(const float *inv_freq, const Pairing &p, double position, float *c, float *s)
+// cos and sin of an angle within half a turn or so, off by little more than a step of fp32: the angle from the nearest quarter of a turn,
+// rounded once, and the power series of both functions over an eighth of a turn on either side; what they leave out is under 2^-28.
+__device__ __forceinline__ void cos_sin(double turns, float &c, float &s)
+{
+    const double quarters = 4.0 * turns, nearest = __builtin_rint(quarters);
+    const float x = (float)(1.5707963267948966 * (quarters - nearest)), xx = x * x;
+    const int q = (int)nearest;
+    const float sn = __builtin_fmaf(x * xx, __builtin_fmaf(xx, __builtin_fmaf(xx, __builtin_fmaf(xx, 1.0f / 362880, -1.0f / 5040), 1.0f / 120), -1.0f / 6), x);
+    const float cs = __builtin_fmaf(xx, __builtin_fmaf(xx, __builtin_fmaf(xx, __builtin_fmaf(xx, __builtin_fmaf(xx, -1.0f / 3628800, 1.0f / 40320), -1.0f / 720),
+                                                                       1.0f / 24), -0.5f), 1.0f);
+    c = as_float(__builtin_bit_cast(unsigned, (q & 1) ? sn : cs) ^ (unsigned)((q + 1) & 2) << 30);
+    s = as_float(__builtin_bit_cast(unsigned, (q & 1) ? cs : sn) ^ (unsigned)(q & 2) << 30);
+}
+// cos and sin of the eight angles of a lane at a position; elements that stay as they are get 1 and 0.  EXACT: to a step of fp32; FAR: at
+// positions past 2^30 too.  Relative error of fp32 rows against fp64, rms: 3.9e-8, with the hardware's functions 9.3e-8; codes that are not
+// the exact ones' of 33 million keys on e4m3 pages: 41 and 80 (plain fp32 arithmetic: 45).  us exact / hardware: 4 x 2048 fp32 rows of 40 heads
+// 62 / 75 (neighbours paired 64 / 64), 16 x 64 7.7 / 9.9 (7.6 / 7.0); append of 16 x 2048 rows of 8 heads to e4m3 pages 43.4 / 42.5, 16 x 64 6.0 /
+// 5.7, 1 x 512 4.3 / 3.9, 11 x 16 4.5 / 4.5.
+template <bool EXACT, bool FAR> __device__ __forceinline__ void turn_of(const float *inv_freq, const Pairing &p, double position, float *c, float *s)
 {
     constexpr double kTurn = 0.15915494309189535, kTurnRest = -9.839338337591243e-18;        // 1 / 2 pi, and what the first number lacks
     const double q = position * kTurn;
@@ -128,13 +143,15 @@ template <bool EXACT> __device__ __forceinline__ void turn_of(const float *inv_f
         const double f = (double)(i < 4 ? fa[i] : fb[i - 4]);
         float cs, sn;
         if constexpr (EXACT) {
-            const double a = position * f, turns = a * kTurn;                                // (a product has 55 bits)
-            const double r = (turns - __builtin_rint(turns)) + (__builtin_fma(a, kTurn, -turns) + __builtin_fma(__builtin_fma(position, f, -a), kTurn, a * kTurnRest));
-            const float near = (float)r, rest = 6.2831853f * (float)(r - (double)near);
-            float s0, c0;
-            sincospif(2.0f * near, &s0, &c0);
-            cs = __builtin_fmaf(-s0, rest, c0);
-            sn = __builtin_fmaf(c0, rest, s0);
+            double turns, rest = 0.0;
+            if constexpr (FAR) {
+                const double a = position * f;                                               // (the product has 55 bits)
+                turns = a * kTurn;
+                rest = __builtin_fma(a, kTurn, -turns) + __builtin_fma(__builtin_fma(position, f, -a), kTurn, a * kTurnRest);
+            } else {
+                turns = f * q;
+            }
+            cos_sin((turns - __builtin_rint(turns)) + rest, cs, sn);
         } else {
             const double turns = f * q;
             const float r = (float)(turns - __builtin_rint(turns));
@@ -212,7 +229,7 @@ __global__ __launch_bounds__(256) void norm_rotate_kernel(NormRotateArgs a)
 
     float w[16], c[8], s[8];
     if constexpr (NORM) weights_of<T>(side.weight, p, w);
-    if constexpr (PAIR != kNoTurn) turn_of<EXACT>(a.inv_freq, p, a.positions != nullptr ? (double)a.positions[token] : (double)i, c, s);
+    if constexpr (PAIR != kNoTurn) turn_of<EXACT, true>(a.inv_freq, p, a.positions != nullptr ? (double)a.positions[token] : (double)i, c, s);
     const bool normed = NORM && side.weight != nullptr;
     for (int h0 = 0; h0 < count; h0 += U) {
 #pragma unroll
@@ -283,7 +300,7 @@ struct Divide {                                              // x / s, by a prod
 // decided here without an atomic.  The rows stay in registers between the maximum over the page and their storage; the next head's are
 // on their way meanwhile, and its angles and weights are this one's.
 // Values are stored with the keys of one head dim side by side, and are turned over in LDS.
-// Bound by memory: 16 x 2048 rows of 8 heads to e4m3 pages of 64 42 us, 4.8 TB/s read and written.
+// Bound by memory: 16 x 2048 rows of 8 heads to e4m3 pages of 64 43 us, 4.7 TB/s read and written.
 template <typename T, int D, int PAGE, int ROWS, bool FP8, bool VALUES>
 __device__ __forceinline__ void append_page(const PageAppendArgs &a, unsigned bid, unsigned *turned, float *wave_max)
 {
@@ -328,7 +345,7 @@ __device__ __forceinline__ void append_page(const PageAppendArgs &a, unsigned bi
     const bool normed = a.weight != nullptr, turns = a.rot > 0;
     if constexpr (!VALUES) {
         weights_of<T>(a.weight, p, w);
-        if (turns) turn_of<false>(a.inv_freq, p, (double)pos, c, s);
+        if (turns) turn_of<FP8, false>(a.inv_freq, p, (double)pos, c, s);
     }
 
     // the keys and head dims of values that this thread stores: TURNS times 16 bytes of each of DIMS head dims
@@ -363,7 +380,7 @@ __device__ __forceinline__ void append_page(const PageAppendArgs &a, unsigned bi
         unpack(in[1], x + 8);
         fetch(min(g + 1, g_end - 1));
         if constexpr (!VALUES) {
-            if (normed) norm<D, false>(x, w, a.eps, true);
+            if (normed) norm<D, FP8>(x, w, a.eps, true);
             if (turns) {
                 if (a.interleaved) rotate<kNeighbours>(x, c, s);
                 else rotate<kHalves>(x, c, s);
@@ -540,7 +557,7 @@ hipError_t launch_page_append(PageAppendArgs a, int d, bool rows_bf16, bool fp8,
     a.pages_per_seq = (int)((a.n + page - 2) / page + 1);    // that n rows can touch, wherever they begin
     // Heads per workgroup: as many as leave two thousand threads per compute unit, what fits there; more workgroups make the angles and
     // look up the page once more each.  us at one head / all heads / this: 16 x 2048 rows, 8 heads, e4m3 67 / 42 / 42, 4096 rows, 32 heads,
-    // bf16 pages of 16 32 / 33 / 31; short calls have one head each.
+    // bf16 pages of 16 32 / 33 / 31 (with the hardware's sine); short calls have one head each.
     const long threads = 2L * a.B * a.pages_per_seq * a.Hkv * (rows_of(a.n, (int)page) * d / 16), per = threads / (256 * 2048);
     a.per_wg = per < 1 ? 1 : per > a.Hkv ? a.Hkv : (int)per;
     a.head_groups = (a.Hkv + a.per_wg - 1) / a.per_wg;

@@ -1,4 +1,4 @@
-"""How exact the rotation of fp32 rows is: to its last bits, as fp32 rows are taken for that."""
+"""How exact the rotation is where that shows: fp32 rows to their last bits, keys on e4m3 pages next to a border between two codes."""
 import numpy as np
 import pytest
 
@@ -11,9 +11,10 @@ pytestmark = pytest.mark.gpu
 @pytest.mark.parametrize("interleaved", [False, True])
 @pytest.mark.parametrize("far", [200, 200000, 2**31 - 1])
 def test_fp32_rotation(far, interleaved):
-    # Sine and cosine are off by at most one step, 2^-24 (they are below 1), and their correction by what the fp32 angle leaves out rounds
-    # once more: 1.5 x 2^-24 each, for a pair of length r sqrt 2 x 1.5 x 2^-24 r < 2.13; two products of lengths that add to r at most,
-    # 2^-24 r; their sum, 2^-24 r: 4.13 x 2^-24 r in all, and second-order terms far below the rest of 4.25.
+    # In units of 2^-24, for a pair of length r.  The angle from the nearest quarter of a turn, at most pi / 4, is rounded once: 0.5.  The sine:
+    # x^3 P is at most 0.081 and carries three roundings, 0.25, the last sum 0.5, what the series leaves out 0.03; the cosine: x^2 R is at
+    # most 0.29 and carries one, R's own is 0.25 times x^2 = 0.62, with later terms 0.5 in all, the last difference 0.5: 1 each, sqrt 2 r
+    # together.  Two products of lengths that add to r at most, 1 r; their sum, 1 r: under 4 r.
     import torch
     rng = np.random.default_rng(far % 1000 + interleaved)
     d, n = 128, 4096
@@ -28,3 +29,44 @@ def test_fp32_rotation(far, interleaved):
     r = np.hypot(u, v)
     worst = max((np.abs(gu - (u * c - v * s)) / r).max(), (np.abs(gv - (v * c + u * s)) / r).max())
     assert worst <= 4.25 * 2.0 ** -24, f"{worst * 2.0 ** 24:.2f} x 2^-24"
+
+
+@pytest.mark.parametrize("seed", [1, 2])
+def test_codes_of_rotated_keys(seed):
+    # A key next to a border between two codes goes the other way with an error of fp32 arithmetic, and as often as that error is large.
+    # The plain form in fp32, sines and cosines rounded from 64 bits, has a half step of 2^-24 each of two factors, two products and a sum;
+    # the kernel has one of the angle more: its codes may differ from the exact ones' some tenths more often.  1.5 times leaves three
+    # standard deviations of the counts, some ninety; functions off by 2^-23 are at more than twice.
+    import torch
+    B, Hkv, n, d, P = 16, 16, 2048, 128, 64
+    half = d // 2
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    K = (1.5 * torch.randn((B, Hkv, n, d), generator=g, device="cuda")).bfloat16()
+    f = (500000.0 ** (-torch.arange(half, device="cuda", dtype=torch.float64) / half)).float()
+    start = torch.randint(0, 130000, (B,), generator=g, device="cuda") // P * P
+    per = (int(start.max()) + n) // P
+    pages = B * n // P
+    table = torch.zeros((B, per), dtype=torch.int32, device="cuda")
+    for b in range(B):
+        table[b, int(start[b]) // P:int(start[b]) // P + n // P] = torch.arange(b * (n // P), (b + 1) * (n // P), device="cuda")
+    Kc, Vc = (torch.zeros(s, dtype=torch.float8_e4m3fn, device="cuda") for s in ((pages, Hkv, P, d), (pages, Hkv, d, P)))
+    ks, vs = torch.ones((pages, Hkv), device="cuda"), torch.ones((pages, Hkv), device="cuda")
+    dd.dd_paged_cache_append(Kc, Vc, K, K, table, start.int(), k_scale=ks, v_scale=vs, inv_freq=f)
+
+    def codes(x):                                            # of rows [Hkv, n, d] in the scales that their pages have
+        x = x.reshape(Hkv, n // P, P, d) / scale.to(x.dtype)[:, :, None, None]
+        return x.to(torch.float64)
+    off = {"plain": 0, "kernel": 0}
+    for b in range(B):
+        scale = ks[b * (n // P):(b + 1) * (n // P)].t()
+        a = (start[b] + torch.arange(n, device="cuda")).double()[:, None] * f.double()
+        turned = {}
+        for t in (torch.float64, torch.float32):
+            c, s, u, v = a.cos().to(t), a.sin().to(t), K[b, ..., :half].to(t), K[b, ..., half:].to(t)
+            turned[t] = codes(torch.cat([u * c - v * s, v * c + u * s], -1))
+        rounded = {t: torch.round(x / step) * step for t, x in turned.items()
+                   for step in [torch.exp2(torch.floor(torch.log2(x.abs().clamp(min=2.0 ** -6))) - 3)]}
+        own = Kc[b * (n // P):(b + 1) * (n // P)].transpose(0, 1).double()
+        off["plain"] += int((rounded[torch.float32] != rounded[torch.float64]).sum())
+        off["kernel"] += int((own != rounded[torch.float64]).sum())
+    assert 20 < off["plain"] and off["kernel"] <= 1.5 * off["plain"], off
