@@ -112,6 +112,17 @@ template <typename T> __device__ __forceinline__ T uniform_load(const T *p)
     return *(__attribute__((address_space(4))) const T *)(unsigned long long)p;
 }
 
+// two bf16 numbers, to nearest even, in one word
+__device__ __forceinline__ unsigned pack_bf16(float lo, float hi)
+{
+    typedef float two_f32 __attribute__((ext_vector_type(2)));
+    typedef __bf16 two_bf16 __attribute__((ext_vector_type(2)));
+    const two_f32 f = {lo, hi};
+    return __builtin_bit_cast(unsigned, __builtin_convertvector(f, two_bf16));
+}
+// (by value: a bit cast of a vector's element in place takes element 0)
+__device__ __forceinline__ float as_float(unsigned w) { return __builtin_bit_cast(float, w); }
+
 constexpr int kAttnThreads = 256;
 
 struct AttnArgs;

@@ -29,9 +29,7 @@ namespace dd {
 namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
-typedef float floatx2 __attribute__((ext_vector_type(2)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef short short4v __attribute__((ext_vector_type(4)));
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
@@ -46,11 +44,6 @@ constexpr int kUnits = 256;              // compute units
 // tiles of 64 keys that a split has at least: with few rows, with more, and with more where workgroups share a compute unit
 constexpr int kSplitTiles = 4, kSplitTilesMany = 8, kSplitTilesShared = 32;
 
-__device__ __forceinline__ unsigned pack_bf16(float lo, float hi)
-{
-    floatx2 f = {lo, hi};
-    return __builtin_bit_cast(unsigned, __builtin_convertvector(f, bf16x2));
-}
 // eight e4m3 codes times the power of two in `scale` (the instruction takes no more of it), exactly
 __device__ __forceinline__ bf16x8 decode8(unsigned w0, unsigned w1, float scale)
 {
@@ -67,7 +60,6 @@ template <bool FP8> __device__ __forceinline__ bf16x8 fragment(const u32x4 *raw,
     else return __builtin_bit_cast(bf16x8, raw[f]);
 }
 // across the two halves of a wave
-__device__ __forceinline__ float as_float(unsigned w) { return __builtin_bit_cast(float, w); }       // (by value: in place it takes a vector's element 0)
 __device__ __forceinline__ float halves_max(float x)
 {
     const u32x2 r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
