@@ -13,7 +13,7 @@
 // 2^-24 of the angle: a hundredth of a radian at position 130000).  Where a result is bf16, the hardware's sine and cosine, which take
 // revolutions and are off by 2^-23 (measured over [0, 1] against fp64), and its reciprocal root: far below its half step of 2^-8.  Where
 // fp32 arithmetic shows - fp32 rows, and e4m3 pages, on which a key next to a border between two codes goes the other way as often as its
-// error is large - sine and cosine to a step of fp32, and the rounded root and reciprocal.
+// error is large - sine and cosine to a step of fp32, and the reciprocal root to half of one.
 #include "attention_common.h"
 #include "dd_internal.h"
 
@@ -122,9 +122,9 @@ __device__ __forceinline__ void cos_sin(double turns, float &c, float &s)
 }
 // cos and sin of the eight angles of a lane at a position; elements that stay as they are get 1 and 0.  EXACT: to a step of fp32; FAR: at
 // positions past 2^30 too.  Relative error of fp32 rows against fp64, rms: 3.9e-8, with the hardware's functions 9.3e-8; codes that are not
-// the exact ones' of 33 million keys on e4m3 pages: 41 and 80 (plain fp32 arithmetic: 45).  us exact / hardware: 4 x 2048 fp32 rows of 40 heads
-// 62 / 75 (neighbours paired 64 / 64), 16 x 64 7.7 / 9.9 (7.6 / 7.0); append of 16 x 2048 rows of 8 heads to e4m3 pages 43.4 / 42.5, 16 x 64 6.0 /
-// 5.7, 1 x 512 4.3 / 3.9, 11 x 16 4.5 / 4.5.
+// the exact ones' of 33 million normed keys on e4m3 pages: 32 and 80 (plain fp32 arithmetic: 45).  us exact / hardware: 4 x 2048 fp32 rows of
+// 40 heads 62 / 75 (neighbours paired 64 / 64), 16 x 64 7.7 / 9.9 (7.6 / 7.0); append of 16 x 2048 rows of 8 heads to e4m3 pages 43.2 / 42.5,
+// 16 x 64 5.9 / 5.7, 1 x 512 4.2 / 3.9, 11 x 16 4.5 / 4.5.
 template <bool EXACT, bool FAR> __device__ __forceinline__ void turn_of(const float *inv_freq, const Pairing &p, double position, float *c, float *s)
 {
     constexpr double kTurn = 0.15915494309189535, kTurnRest = -9.839338337591243e-18;        // 1 / 2 pi, and what the first number lacks
@@ -176,14 +176,34 @@ template <typename T> __device__ __forceinline__ void weights_of(const void *wei
     unpack(load_chunk<T>(static_cast<const uint8_t *>(weight), p.a), w);
     unpack(load_chunk<T>(static_cast<const uint8_t *>(weight), p.b), w + 8);
 }
-template <int D, bool EXACT> __device__ __forceinline__ void norm(float *x, const float *w, float eps, bool normed)
+// EXACT: the root to half a step of fp32 or so, by a correction of the hardware's, and what the elements are to be multiplied by after their
+// rotation, which leaves out a rounding of each (bf16 rows times bf16 weights are exact); else they are normed when it returns.
+template <int D, bool EXACT> __device__ __forceinline__ float norm(float *x, const float *w, float eps, bool normed)
 {
+    if constexpr (EXACT) {
+        float q[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q[i] = __builtin_fmaf(x[2 * i + 1], x[2 * i + 1], x[2 * i] * x[2 * i]);
+        const float m = __builtin_fmaf(row_sum<D / 16>(((q[0] + q[1]) + (q[2] + q[3])) + ((q[4] + q[5]) + (q[6] + q[7]))), 1.0f / D, eps);
+        const float r = __builtin_amdgcn_rsqf(m), p = m * r, e = __builtin_fmaf(-p, r, 1.0f) - __builtin_fmaf(m, r, -p) * r;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] *= w[i];
+        return normed ? __builtin_fmaf(0.5f * r, e, r) : 1.0f;
+    }
     float q = 0;
 #pragma unroll
     for (int i = 0; i < 16; ++i) q += x[i] * x[i];
-    const float mean = row_sum<D / 16>(q) * (1.0f / D) + eps, root = EXACT ? 1.0f / sqrtf(mean) : __builtin_amdgcn_rsqf(mean), r = normed ? root : 1.0f;
+    const float root = __builtin_amdgcn_rsqf(row_sum<D / 16>(q) * (1.0f / D) + eps), r = normed ? root : 1.0f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) x[i] = x[i] * r * w[i];
+    return 1.0f;
+}
+template <bool EXACT> __device__ __forceinline__ void times(float *x, float r)
+{
+    if constexpr (EXACT) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] *= r;
+    }
 }
 
 // ---------------------------------------------------------------- queries and keys for dense attention
@@ -230,8 +250,10 @@ __global__ __launch_bounds__(256) void norm_rotate_kernel(NormRotateArgs a)
             unpack(in[u][0], x);
             unpack(in[u][1], x + 8);
             fetch(h0 + U + u, u);
-            if constexpr (NORM) norm<D, EXACT>(x, w, a.eps, normed);
+            float root = 1.0f;
+            if constexpr (NORM) root = norm<D, EXACT>(x, w, a.eps, normed);
             if constexpr (PAIR != kNoTurn) rotate<PAIR>(x, c, s);
+            if constexpr (NORM) times<EXACT>(x, root);
             if (h0 + u < count) {
                 uint8_t *row = dst + (long)(h0 + u) * a.n * D * T::bytes;
                 store_chunk<T, true>(row, p.a, x);
@@ -372,11 +394,12 @@ __device__ __forceinline__ void append_page(const PageAppendArgs &a, unsigned bi
         unpack(in[1], x + 8);
         fetch(min(g + 1, g_end - 1));
         if constexpr (!VALUES) {
-            if (normed) norm<D, FP8>(x, w, a.eps, true);
+            const float root = normed ? norm<D, FP8>(x, w, a.eps, true) : 1.0f;
             if (turns) {
                 if (a.interleaved) rotate<kNeighbours>(x, c, s);
                 else rotate<kHalves>(x, c, s);
             }
+            if (normed) times<FP8>(x, root);
         }
         float by = 1.0f;                                     // kept codes: their old scale over the new one
         if constexpr (FP8) {

@@ -70,3 +70,21 @@ def test_codes_of_rotated_keys(seed):
         off["plain"] += int((rounded[torch.float32] != rounded[torch.float64]).sum())
         off["kernel"] += int((own != rounded[torch.float64]).sum())
     assert 20 < off["plain"] and off["kernel"] <= 1.5 * off["plain"], off
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_fp32_norm(d):
+    # In units of 2^-24, relative: the sum of squares goes through two roundings of products, three sums of a lane's and three across lanes at
+    # most, 8, of which the root has half, 4; 1/d is exact, the sum with eps 1, halved 0.5; the root's own 1 (half a step, and its correction);
+    # times the weight 1, times the root 1: 7.5.  A row of zeros stays zeros, one beside eps is a matter of the sum with it alone.
+    import torch
+    rng = np.random.default_rng(d)
+    x = (rng.standard_normal((1, 2, 4096, d)) * 2.0 ** rng.integers(-30, 30, (1, 2, 4096, 1))).astype(np.float32)
+    x[0, 0, :7] = 0
+    w = (1 + 0.2 * rng.standard_normal(d)).astype(np.float32)
+    for eps in (1e-6, 1.2e-38):
+        got, _ = dd.dd_qk_norm_rope(dev(x), q_weight=dev(w), eps=eps)
+        y = x.astype(np.float64)
+        want = y / np.sqrt((y * y).mean(-1, keepdims=True) + float(np.float32(eps))) * w.astype(np.float64)
+        off = np.abs(host(got) - want) - 7.5 * 2.0 ** -24 * np.abs(want)
+        assert (off <= 1e-45).all(), f"eps {eps}: {(np.abs(host(got) - want) / np.maximum(np.abs(want), 1e-30)).max() * 2 ** 24:.2f} x 2^-24"
