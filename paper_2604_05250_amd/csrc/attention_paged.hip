@@ -724,21 +724,30 @@ Plan plan_of(int n, int B, int H, int Hkv, long capacity, bool fp8)
     const bool few = rows <= kFewRows;               // no two workgroups read the same keys: memory bounds them
     Plan p;
     // Two or four row blocks per workgroup read the cache once for all, but the workgroups are fewer and their waves wait for each other.
-    // 256 compute units hold two workgroups each, so that up to 512 of one block run at once; bf16 pages wait for memory sooner.  us with
-    // one / two / four row blocks, unsplit.  e4m3: 128 blocks, 2048 positions 15.5 / 25.2 / -; 512, 2048 25.0 / 27.1 / 46.1; 1024, 2048 45.5 / 40.0 /
-    // 46.6; 1536, 2048 73.9 / 62.2 / 65.6; 1920, 2048 91.5 / 78.2 / 75.5; 8192, 2048 335 / 290 / 272.  bf16: 256 blocks, 1024 positions 14.6 / 19.3 /
-    // -; 320, 2048 28.8 / 32.0 / -; 512, 4096 75.5 / 68.0 / 104; 1024, 2048 76.3 / 50.7 / 57.3; 1152, 2048 89.5 / 74.5 / 71.0; 2048, 1024 80.0 / 56.5 /
-    // 50.0.  Where a workgroup's last rows are missing, their work is not: 320 rows of 128 heads, 700 positions 35.3 / 32.6 / 34.7.
+    // 256 compute units hold two workgroups each, so that up to 512 of one block run at once; bf16 pages wait for memory sooner.
+    // us with one / two / four row blocks, unsplit, by blocks x positions:
+    //     e4m3    128 x 2048    15.5 / 25.2 / -           bf16    256 x 1024    14.6 / 19.3 / -
+    //             512 x 2048    25.0 / 27.1 / 46.1                320 x 2048    28.8 / 32.0 / -
+    //            1024 x 2048    45.5 / 40.0 / 46.6                512 x 4096    75.5 / 68.0 / 104
+    //            1536 x 2048    73.9 / 62.2 / 65.6               1024 x 2048    76.3 / 50.7 / 57.3
+    //            1920 x 2048    91.5 / 78.2 / 75.5               1152 x 2048    89.5 / 74.5 / 71.0
+    //            8192 x 2048     335 /  290 /  272               2048 x 1024    80.0 / 56.5 / 50.0
+    // Where a workgroup's last rows are missing, their work is not: 320 rows of 128 heads, 700 positions 35.3 / 32.6 / 34.7.
     const bool full = (rows + 127) / 128 * 128 * 8 <= rows * 9;
     p.rg = few || blocks <= (fp8 ? 512 : 256) ? 1 : full && blocks > (fp8 ? 1792 : 1024) ? 4 : 2;
     p.row_tiles = (rows + 32 * p.rg - 1) / (32 * p.rg);
     const long base = heads * p.row_tiles;
     // Splits: the merge's launch costs some 1.5 us and each split a state per row, written and read again, for 32 rows as many bytes as a
-    // tile of 64 keys; so up to one workgroup per compute unit, and up to two where arithmetic bounds them and the splits stay long.  us with
-    // 1 / 2 / 4 / 8 / 16 splits, 32/8 heads, e4m3.  One token: one sequence, 512 positions 6.1 / 7.4 / 7.4 / - / -, 1024 8.6 / 8.6 / 7.4 / - / -,
-    // 4096 22.2 / 15.6 / 11.0 / 8.8 / 8.4; four 4096 25.1 / 17.5 / 12.7 / 11.3 / 13.1; 24 4096 35.2 / 40.9 / 39.5 / 42.3 / -.  64 tokens: one sequence
-    // 1024 9.9 / 10.7 / 10.8 / - / -, 1500 12.5 / 12.3 / 11.8 / - / -, 2048 14.8 / 13.1 / 12.0 / - / -, 16384 83.2 / 47.6 / 29.1 / 28.9 / 33.8; three
-    // 2048 16.1 / 20.6 / 23.9 / - / -, 8192 46.6 / 42.9 / 41.1 / 46.0 / -; four 2048 16.3 / 22.8 / 26.1 / - / -, 8192 47.7 / 48.3 / 51.3 / 59.6 / -.
+    // tile of 64 keys; so up to one workgroup per compute unit, and up to two where arithmetic bounds them and the splits stay long.
+    // us with 1 / 2 / 4 / 8 / 16 splits, 32/8 heads, e4m3, by sequences x positions:
+    //     one token    1 x 512      6.1 /  7.4 /  7.4 / - / -         64 tokens    1 x 1024     9.9 / 10.7 / 10.8 / - / -
+    //                  1 x 1024     8.6 /  8.6 /  7.4 / - / -                      1 x 1500    12.5 / 12.3 / 11.8 / - / -
+    //                  1 x 4096    22.2 / 15.6 / 11.0 / 8.8 / 8.4                  1 x 2048    14.8 / 13.1 / 12.0 / - / -
+    //                  4 x 4096    25.1 / 17.5 / 12.7 / 11.3 / 13.1                1 x 16384   83.2 / 47.6 / 29.1 / 28.9 / 33.8
+    //                 24 x 4096    35.2 / 40.9 / 39.5 / 42.3 / -                   3 x 2048    16.1 / 20.6 / 23.9 / - / -
+    //                                                                              3 x 8192    46.6 / 42.9 / 41.1 / 46.0 / -
+    //                                                                              4 x 2048    16.3 / 22.8 / 26.1 / - / -
+    //                                                                              4 x 8192    47.7 / 48.3 / 51.3 / 59.6 / -
     // Calls a little past one or two workgroups per compute unit wait for the few that share one: 264 of 3937 positions 34.1 / 38.5 / 37.9 / - / -.
     auto up_to = [&](long want, long least) { return want < tiles / least ? want : tiles / least; };
     long s = p.rg == 1 ? up_to(kUnits / base, kSplitTiles) : 1;
