@@ -361,7 +361,8 @@ def _plain_verify(st, case):
     turned = accepted < count                                             # a draft was turned down: from what p has more than q
     again = accepted.clamp(max=n - 1)
     minus = q[which, again] if q is not None else torch.zeros_like(r).scatter_(1, x[which, again], math.inf)
-    r = torch.where(turned.unsqueeze(1), (r - minus).clamp(min=0), r)
+    left = (r - minus).clamp(min=0)
+    r = torch.where((turned & (left.sum(-1) > 0)).unsqueeze(1), left, r)
     c = r.cumsum(-1)
     token = (c <= u[:, n:] * c[:, -1:]).sum(-1).clamp(max=V - 1)
     if not case["bonus"]:
@@ -507,7 +508,8 @@ def _exact_verify(st, case):
                 out[b, k] = x
                 i += 1
             elif weights is None:
-                weights = (p - q).clamp(min=0)
+                left = (p - q).clamp(min=0)
+                weights = left if float(left.sum()) > 0 else p
         accepted[b] = i
         if weights is None and case["bonus"]:
             weights = probabilities(st["logits_v"][b, i], temps[b])
