@@ -480,6 +480,37 @@ int dd_verify_scores(const void *logits_d, const void *logits_v,
                      int P, int V, dd_dtype logit_dtype, void *workspace, size_t workspace_bytes, void *stream);
 size_t dd_verify_scores_workspace_bytes(int P, int V, dd_dtype logit_dtype);
 
+/*
+ * Verification of drafted tokens by given random numbers: what is kept and what is drawn instead is distributed as the verifier's
+ * own draws.  Sequence b has drafts x_i = tokens[b*n + i], i < n_b (n_draft[b] clamped to [0, n]; n_draft == NULL: n), made with
+ * the drafter's probabilities q_i = softmax(logits_d[b,i,:] / T_b), and the verifier's p_i = softmax(logits_v[b,i,:] / T_b).
+ *     draft i stands iff  u_i q_i(x_i) < p_i(x_i),   u_i = uniforms[b*(n+1) + i]
+ *     a = number of drafts before the first that does not stand (n_b where all do)
+ *     a < n_b:  the token behind them is drawn with weights w = max(p_a - q_a, 0), or w = p_a where that is 0 everywhere
+ *     a == n_b: with `bonus`, it is drawn with w = p_{n_b} (row n_b of logits_v); without, there is none
+ *     drawn: the lowest x with  sum_{y <= x} w(y) > u sum_y w(y),   u = uniforms[b*(n+1) + n]
+ * T_b <= 1e-6 (temperature 0; NaN too): all of the probability on the lowest of the largest logits.  logits_d == NULL: the drafter
+ * was sure of its tokens, q_i(x_i) = 1.  A draft that is no token of the vocabulary has p = q = 0 (q = 1 with logits_d == NULL).
+ * A call on [B*n,1,V] views with bonus = 0 decides every position on its own (the marginals of a masked diffusion model).
+ *
+ *   logits_v [B,n+1,V] with bonus, else [B,n,V];  logits_d [B,n,V] or NULL;  logit_dtype DD_F32 or DD_BF16
+ *   tokens [B,n] i32;  n_draft [B] i32 or NULL;  uniforms [B,n+1] f32 in [0, 1);  temperature [B] f32 or NULL (1 each)
+ *   out_tokens [B,n+1] i32: x_0 .. x_{a-1}, the drawn token, then -1        out_accepted [B] i32 = a
+ *   out_chances [B,n] f32 = min(1, p_i(x_i) / q_i(x_i)) of every draft i < n_b, 0 behind (1 where only q_i(x_i) is 0)
+ * Logits are finite or -inf (probability 0), below 2^30 T in magnitude; a row has a finite one.  For any other values, of
+ * uniforms, tokens and temperatures too, no access leaves the tensors and tokens are in [-1, V) or drafts.  Rows behind the last that
+ * a sequence needs are not read.
+ * Arithmetic: fp64 throughout, exponentials to 1.1e-12, so that which token is drawn does not hang on roundings.
+ * V * sizeof(element) a multiple of 16; logits 16-byte aligned; no output overlaps an input or another output (DD_ERR_SHAPE); B >= 0
+ * (0: a no-op), n >= 0, n >= 1 without bonus; workspace from the query; workgroups of one launch (rows, and parts of long rows)
+ * fewer than 2^24, else DD_ERR_SHAPE.
+ */
+int dd_verify_draft(const void *logits_v, const void *logits_d, const int32_t *tokens, const int32_t *n_draft,
+                    const float *uniforms, const float *temperature,
+                    int32_t *out_tokens, int32_t *out_accepted, float *out_chances,
+                    int B, int n, int bonus, int V, dd_dtype logit_dtype, void *workspace, size_t workspace_bytes, void *stream);
+size_t dd_verify_draft_workspace_bytes(int B, int n, int bonus, int V, int with_drafter, dd_dtype logit_dtype);
+
 #ifdef __cplusplus
 }
 #endif

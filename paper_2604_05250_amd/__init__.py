@@ -101,6 +101,10 @@ def lib():
     L.dd_paged_attention.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i, i, i, i, i, i, i, i, i, vp, sz, vp]
     L.dd_paged_attention_workspace_bytes.restype = sz
     L.dd_paged_attention_workspace_bytes.argtypes = [i, i, i, i, i, i, i, i]
+    L.dd_verify_draft.restype = i
+    L.dd_verify_draft.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, i, i, i, i, i, vp, sz, vp]
+    L.dd_verify_draft_workspace_bytes.restype = sz
+    L.dd_verify_draft_workspace_bytes.argtypes = [i, i, i, i, i, i]
     _lib = L
     return L
 
@@ -114,7 +118,7 @@ EXPORTS = ("dd_strerror", "dd_version", "dd_bidir_attention", "dd_bidir_attentio
            "dd_block_attention_batched", "dd_block_attention_batched_workspace_bytes",
            "dd_bidir_attention_fp8v", "dd_block_attention_cached_fp8v", "dd_block_attention_cached_fp8v_workspace_bytes",
            "dd_bidir_attention_mx", "dd_qk_norm_rope", "dd_paged_cache_append", "dd_paged_attention",
-           "dd_paged_attention_workspace_bytes")
+           "dd_paged_attention_workspace_bytes", "dd_verify_draft", "dd_verify_draft_workspace_bytes")
 
 
 # ---------------------------------------------------------------- marshalling (csrc/binding.cpp)
@@ -311,3 +315,17 @@ def dd_verify_scores(logits_d, logits_v, drafter: bool = True, logit_dtype: Opti
     """Divergence, both confidences and both argmax tokens of every row in one pass.  logits_d, logits_v [P, V].
     Returns (kl f32, conf_v f32, tok_v i32, conf_d f32 | None, tok_d i32 | None)."""
     return native().verify_scores(logits_d, logits_v, drafter, logit_dtype)
+
+
+def dd_verify_draft_workspace_bytes(B, n, bonus, V, with_drafter, logit_dtype) -> int:
+    return lib().dd_verify_draft_workspace_bytes(B, n, bonus, V, with_drafter, logit_dtype)
+
+
+def dd_verify_draft(logits_v, logits_d, tokens, uniforms, temperature=None, n_draft=None, out_tokens=None, out_accepted=None,
+                    out_chances=None, logit_dtype: Optional[int] = None):
+    """Drafted tokens [B,n] i32 against the verifier's probabilities, by given random numbers: uniforms [B,n+1] f32 (the last one
+    draws the token behind the drafts that stand).  logits_v [B,n+1,V], or [B,n,V] for no token behind a draft that stands whole;
+    logits_d [B,n,V], or None where the drafter was sure of its tokens; temperature [B] f32 (0: the largest logit; default 1);
+    n_draft [B] i32 (default n).  Returns (tokens [B,n+1] i32: kept drafts, the drawn token, then -1; accepted [B] i32; chances
+    [B,n] f32: the probability with which each draft stands)."""
+    return native().verify_draft(logits_v, logits_d, tokens, uniforms, temperature, n_draft, out_tokens, out_accepted, out_chances, logit_dtype)

@@ -768,6 +768,42 @@ PyObject *paged_attention(PyObject *const *a, Py_ssize_t n)
     return THPVariable_Wrap(out);
 }
 
+// (logits_v, logits_d, tokens, uniforms, temperature, n_draft, out_tokens, out_accepted, out_chances, logit_dtype) -> the three outputs
+PyObject *verify_draft(PyObject *const *a, Py_ssize_t n)
+{
+    want(n, 10);
+    const at::Tensor &L = tensor(a[0], "logits_v"), &x = tensor(a[2], "tokens"), &u = tensor(a[3], "uniforms");
+    const at::Tensor *D = opt_tensor(a[1], "logits_d"), *t = opt_tensor(a[4], "temperature"), *count = opt_tensor(a[5], "n_draft");
+    const at::Tensor *ot = opt_tensor(a[6], "out_tokens"), *oa = opt_tensor(a[7], "out_accepted"), *oc = opt_tensor(a[8], "out_chances");
+    if (L.dim() != 3 || x.dim() != 2) value_error("", "logits_v must have three dimensions, tokens two");
+    const int64_t B = x.size(0), drafts = x.size(1), rows = L.size(1), V = L.size(2);
+    fits_int({B, drafts, rows, V});
+    if (L.size(0) != B || (rows != drafts && rows != drafts + 1)) value_error("", "logits_v shape must be [B,n,V] or, with a row behind the last draft, [B,n+1,V]");
+    if (D && !has_shape(*D, {B, drafts, V})) value_error("", "logits_d shape must be [B,n,V]");
+    const int bonus = rows == drafts + 1;
+    const dd_dtype dt = (dd_dtype)tag_or(a[9], L, "logits_v");
+    elements_of(&L, dt, "logits_v"); elements_of(D, dt, "logits_d");
+    check_vec(&x, B * drafts, at::kInt, "tokens");
+    check_vec(&u, B * (drafts + 1), at::kFloat, "uniforms");
+    check_vec(t, B, at::kFloat, "temperature");
+    check_vec(count, B, at::kInt, "n_draft");
+    check_vec(ot, B * (drafts + 1), at::kInt, "out_tokens");
+    check_vec(oa, B, at::kInt, "out_accepted");
+    check_vec(oc, B * drafts, at::kFloat, "out_chances");
+    const OneDevice dev(L);
+    void *const lv = dev(L, "logits_v"), *const ld = dev(D, "logits_d"), *const px = dev(x, "tokens"), *const pu = dev(u, "uniforms");
+    void *const pt = dev(t, "temperature"), *const pn = dev(count, "n_draft");
+    const c10::hip::HIPGuard guard(L.device().index());
+    const at::Tensor rt = ot ? *ot : empty_like_type({B, drafts + 1}, at::kInt, L);
+    const at::Tensor ra = oa ? *oa : empty_like_type({B}, at::kInt, L);
+    const at::Tensor rc = oc ? *oc : empty_like_type({B, drafts}, at::kFloat, L);
+    void *const wt = dev(rt, "out_tokens"), *const wa = dev(ra, "out_accepted"), *const wc = dev(rc, "out_chances");
+    const Call c(dd_verify_draft_workspace_bytes(B, drafts, bonus, V, D != nullptr, dt), L);
+    check(c.run([&] { return dd_verify_draft(lv, ld, (const int32_t *)px, (const int32_t *)pn, (const float *)pu, (const float *)pt, (int32_t *)wt, (int32_t *)wa,
+                                             (float *)wc, B, drafts, bonus, V, dt, c.ptr(), c.bytes(), c.stream); }), "dd_verify_draft");
+    return triple(rt, ra, rc);
+}
+
 // (DDError) -> None
 PyObject *set_error_class(PyObject *const *a, Py_ssize_t n)
 {
@@ -816,7 +852,7 @@ PyObject *entry(PyObject *, PyObject *const *a, Py_ssize_t n)
 #define DD_METHOD(name) {#name, (PyCFunction)(void (*)(void))entry<name>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {DD_METHOD(bidir), DD_METHOD(block), DD_METHOD(bidir_fp8v), DD_METHOD(bidir_mx), DD_METHOD(block_fp8v),
                          DD_METHOD(cache_insert), DD_METHOD(verify_remask), DD_METHOD(unmask), DD_METHOD(verify_scores),
-                         DD_METHOD(qk_norm_rope), DD_METHOD(paged_append), DD_METHOD(paged_attention),
+                         DD_METHOD(qk_norm_rope), DD_METHOD(paged_append), DD_METHOD(paged_attention), DD_METHOD(verify_draft),
                          DD_METHOD(set_error_class), DD_METHOD(set_fixed_workspace), DD_METHOD(reset_workspace_peak),
                          DD_METHOD(workspace_peak), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", "argument marshalling of paper_2604_05250_amd", -1, methods, nullptr, nullptr, nullptr, nullptr};

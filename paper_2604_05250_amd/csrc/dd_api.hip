@@ -746,4 +746,59 @@ int dd_verify_scores(const void *logits_d, const void *logits_v,
     return e == hipSuccess ? DD_OK : DD_ERR_LAUNCH;
 }
 
+static bool draft_sizes(int B, int n, int bonus, int V, int with_drafter, dd_dtype t)
+{
+    const int nv = n + (bonus ? 1 : 0);
+    if (B < 1 || n < 0 || n == 0x7fffffff || nv < 1 || V < 1) return false;
+    if ((double)B * (n + 1.0) >= 1073741824.0) return false;
+    return dd::verify_draft_workgroups(B, n, nv, V, t == DD_BF16, with_drafter != 0) < 16777216.0;
+}
+
+size_t dd_verify_draft_workspace_bytes(int B, int n, int bonus, int V, int with_drafter, dd_dtype logit_dtype)
+{
+    if (logit_dtype != DD_F32 && logit_dtype != DD_BF16) return 0;
+    if (!draft_sizes(B, n, bonus, V, with_drafter, logit_dtype)) return 0;
+    return dd::verify_draft_workspace_bytes(B, n, n + (bonus ? 1 : 0), V, logit_dtype == DD_BF16, with_drafter != 0);
+}
+
+int dd_verify_draft(const void *logits_v, const void *logits_d, const int32_t *tokens, const int32_t *n_draft,
+                    const float *uniforms, const float *temperature,
+                    int32_t *out_tokens, int32_t *out_accepted, float *out_chances,
+                    int B, int n, int bonus, int V, dd_dtype logit_dtype, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (logit_dtype != DD_F32 && logit_dtype != DD_BF16) return DD_ERR_DTYPE;
+    if (B < 0 || n < 0 || V < 1) return DD_ERR_SHAPE;
+    const int eb = logit_dtype == DD_BF16 ? 2 : 4, nv = n + (bonus ? 1 : 0);
+    if (((long)V * eb) % 16 != 0) return DD_ERR_ALIGN;
+    if (B == 0) return DD_OK;
+    if (!draft_sizes(B, n, bonus, V, logits_d != nullptr, logit_dtype)) return DD_ERR_SHAPE;
+    if (!logits_v || !uniforms || !out_tokens || !out_accepted || (n > 0 && (!tokens || !out_chances))) return DD_ERR_NULL;
+    uintptr_t words = 0;
+    for (const void *p : {(const void *)tokens, (const void *)n_draft, (const void *)uniforms, (const void *)temperature, (const void *)out_tokens,
+                          (const void *)out_accepted, (const void *)out_chances})
+        words |= reinterpret_cast<uintptr_t>(p);
+    if (misaligned16(logits_v) || misaligned16(logits_d) || (words & 3u) != 0) return DD_ERR_ALIGN;
+    const int rc = check_workspace(workspace, workspace_bytes, dd::verify_draft_workspace_bytes(B, n, nv, V, logit_dtype == DD_BF16, logits_d != nullptr));
+    if (rc != DD_OK) return rc;
+    // (a sequence's inputs are read by some workgroups while others write outputs)
+    struct Range { const void *at; uintptr_t bytes; };
+    const uintptr_t seqs = (uintptr_t)B * 4, drafts = (uintptr_t)B * n * 4, both = seqs + drafts;
+    const Range outs[3] = {{out_tokens, both}, {out_accepted, seqs}, {out_chances, drafts}};
+    const Range ins[6] = {{logits_v, (uintptr_t)B * nv * V * eb}, {logits_d, (uintptr_t)B * n * V * eb}, {tokens, drafts}, {n_draft, seqs}, {uniforms, both},
+                          {temperature, seqs}};
+    for (int o = 0; o < 3; ++o) {
+        for (int i = 0; i < 6; ++i)
+            if (ins[i].at && outs[o].bytes && ins[i].bytes && overlap(outs[o].at, outs[o].bytes, ins[i].at, ins[i].bytes)) return DD_ERR_SHAPE;
+        for (int i = 0; i < o; ++i)
+            if (outs[o].bytes && outs[i].bytes && overlap(outs[o].at, outs[o].bytes, outs[i].at, outs[i].bytes)) return DD_ERR_SHAPE;
+    }
+    dd::DraftArgs a;
+    a.logits_v = logits_v; a.logits_d = n > 0 ? logits_d : nullptr; a.tokens = tokens; a.n_draft = n_draft; a.uniforms = uniforms; a.temperature = temperature;
+    a.out_tokens = out_tokens; a.out_accepted = out_accepted; a.out_chances = out_chances;
+    a.B = B; a.n = n; a.nv = nv; a.V = V; a.bonus = bonus != 0; a.bf16 = logit_dtype == DD_BF16;
+    a.workspace = workspace;
+    const hipError_t e = dd::launch_verify_draft(a, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? DD_OK : DD_ERR_LAUNCH;
+}
+
 }  // extern "C"

@@ -70,6 +70,21 @@ hipError_t launch_verify(const void *logits_d, const void *logits_v, const uint8
                          int B, int G, int V, int logit_is_bf16, void *workspace, size_t workspace_bytes, hipStream_t stream,
                          int32_t *x_tokens = nullptr, const VerifyExtra *extra = nullptr);
 
+// ---- verification of drafted tokens (draft.hip) -----------------------------------
+struct DraftArgs {
+    const void *logits_v = nullptr, *logits_d = nullptr;     // [B, nv, V], [B, n, V] or nullptr: the drafter was sure of its tokens
+    const int32_t *tokens = nullptr, *n_draft = nullptr;     // [B, n], [B] or nullptr: n each
+    const float *uniforms = nullptr, *temperature = nullptr; // [B, n + 1], [B] or nullptr: 1
+    int32_t *out_tokens = nullptr, *out_accepted = nullptr;  // [B, n + 1], [B]
+    float *out_chances = nullptr;                            // [B, n]
+    int B = 0, n = 0, nv = 0, V = 0;                         // nv: n + 1 with `bonus`, else n
+    bool bonus = false, bf16 = false;
+    void *workspace = nullptr;
+};
+size_t verify_draft_workspace_bytes(int B, int n, int nv, int V, bool bf16, bool drafter);
+double verify_draft_workgroups(int B, int n, int nv, int V, bool bf16, bool drafter);      // of the largest launch
+hipError_t launch_verify_draft(const DraftArgs &a, hipStream_t stream);
+
 // ---- attention (attention_mfma.hip, attention_f32.hip) -------------------------
 // One description serves the verifier's full attention and the drafter's block attention:
 // for every (batch, kv head) the `group * Nq` query rows of the heads sharing that kv head
