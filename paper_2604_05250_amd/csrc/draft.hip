@@ -3,13 +3,18 @@
 //     draft i stands iff  u_i q_i(x_i) < p_i(x_i);   a = drafts that stand before the first that does not
 //     the token behind them is the lowest x with  sum_{y <= x} w(y) > u_n sum_y w(y),   w = max(p_a - q_a, 0) where a draft was turned
 //     down, p_a where none was
-// so that every token is distributed as the verifier's.  A decision is a comparison with a border that is one of V, some 10^-5 apart and
-// closer: exponentials and sums are held in 64 bits, and no order of addition or rounding of an exponential decides (fp32 sums would
-// move a border by 10^-3 of a token's width and more).  An fp64 instruction takes a wave as long here as an fp32 one.
+// so that every token is distributed as the verifier's.  A decision is a comparison with a border, and a draw one with borders that are
+// V, some 10^-5 apart and closer: no rounding may decide them (fp32 sums would move a border by 10^-3 of a token's width and more).
 // Three launches, as every step needs all of the one before:
-//   draft_sums_kernel   every logit once: reference and sum of 2^((l - ref) c), c = log2(e) / T, of every part of a row
-//   draft_decide_kernel the drafts' fate, and the weights' sums over the parts of the row that a token is drawn from
-//   draft_pick_kernel   the part in which the sum passes its mark, and there the token
+//   draft_sums_kernel   every logit once: reference and sum of 2^((l - ref) c), c = log2(e) / T, of every part of a row; fp32
+//                       exponentials, whose sums are good to kNear: memory bounds it
+//   draft_decide_kernel the drafts' fate; a draft nearer to its border than kNear is decided again on fp64 sums of its rows (one in some
+//                       ten thousand).  Then, of the one row that a token is drawn from, in fp64 by parts: sums of p's and q's
+//                       exponentials, all and where p is the larger.  Which of the two is the larger goes by the fp32 sums: where that is
+//                       wrong they agree to kNear, for kNear of the tokens, and a part's weight is off by kNear^2 of it at most
+//   draft_pick_kernel   the part in which the running sum passes its mark, and there the token
+// An fp64 instruction takes a wave as long here as an fp32 one (2.2 and 1.9 ns), a power of two 18 of them; with fp64 sums in the
+// first kernel too, that one took 100 us for 64 sequences of 8 drafts, 126464 bf16 logits, which are 44 us from memory.
 #include "dd_internal.h"
 
 #include <type_traits>
@@ -21,18 +26,23 @@ typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
-constexpr int kLoads = 4;                    // vectors of 16 bytes of a lane on their way
+constexpr int kWaves = kThreads / 64;
+[[maybe_unused]] constexpr int kLoads = 4;                    // vectors of 16 bytes of a lane on their way
 constexpr int kMostSplits = 64;              // of a row: a lane of a wave for each
-constexpr int kMostParts = kThreads;         // of the row that is drawn from: a thread of a workgroup for each
+constexpr int kMostParts = 64;               // workgroups of the row that is drawn from: a thread of a workgroup for each of their waves
 [[maybe_unused]] constexpr float kCold = 1.0e-6f;             // temperatures up to here: all of the probability on the largest logit
 [[maybe_unused]] constexpr double kLog2e = 1.4426950408889634;
-[[maybe_unused]] constexpr float kRaise = 500.0f;             // log2 units: a reference may be exceeded by as much, 2^kRaise sums fit fp64
+[[maybe_unused]] constexpr float kRaise = 16.0f;              // log2 units by which logits may exceed a reference
 [[maybe_unused]] constexpr double kFloor = -1020.0;           // below that a power of two is none
+// What a quotient of two of the first kernel's sums and of two probabilities may be off by: per exponential the roundings of l - ref and
+// of its product with c, as rounded, 2^-24 each of an exponent of 40 and less (what is below adds nothing), ln 2 of that, its own
+// of 2^-23, and three additions: 5.5e-6 per sum.
+[[maybe_unused]] constexpr double kNear = 2.0e-5;
 
 struct State { float ref; int first; double sum; };      // reference, its first index (temperature 0), sum
-struct Sums { double w, p; };                            // of a part of the row that is drawn from: of the weights, and of p alone
-enum { kDone = 0, kDraw = 1, kDrawP = 2 };
-struct Verdict { int kind, at; float ref_p, ref_q; double inv_p, inv_q, c; };      // how the token at `at` is drawn
+struct Sums { double p, q, above_p, above_q; };          // of exponentials, of a part of the row that is drawn from: all, and where p > q
+enum { kDone = 0, kDraw = 1 };
+struct Verdict { int kind, at; float ref_p, ref_q; double c; };      // how the token at `at` is drawn
 
 struct DraftKernelArgs {
     const uint8_t *lv, *ld;
@@ -41,10 +51,10 @@ struct DraftKernelArgs {
     int32_t *out_tokens, *out_accepted;
     float *out_chances;
     State *states;                           // [B nv + B n][splits]
-    Sums *sums;                              // [B][parts]
+    Sums *sums;                              // [B][parts][kWaves]
     Verdict *verdicts;                       // [B]
     int B, n, nv, bonus, vecs;               // nv: verifier rows of a sequence; vecs: 16-byte vectors of a row
-    int splits, per_split, parts, per_part;  // vectors per split and part
+    int splits, per_split, parts, per_part;  // vectors per split and part (of a part, a quarter per wave)
 };
 
 // 2^t for t <= 1000, 0 below -1020: the nearest integer by a number so large that fractions fall off, the rest on [-1/2, 1/2] by a
@@ -89,31 +99,32 @@ template <bool BF16> __device__ __forceinline__ float logit(const uint8_t *row, 
     else return reinterpret_cast<const float *>(row)[x];
 }
 
-// ---- across a wave and a workgroup, every lane with the result, always in the same order
-__device__ __forceinline__ double other(double v, int mask)
+// ---- across a wave, every lane with the result (the same bits: the two that meet are added in either order): neighbours, pairs of two,
+// halves of eight and of sixteen lanes, then the halves of 32 and of 64
+template <int STEP> __device__ __forceinline__ u32x2 meet(unsigned v)
 {
-    u32x2 r = __builtin_bit_cast(u32x2, v);
-    r.x = __shfl_xor((int)r.x, mask);
-    r.y = __shfl_xor((int)r.y, mask);
-    return __builtin_bit_cast(double, r);
+    if constexpr (STEP < 4) {
+        constexpr int CTRL = STEP == 0 ? 0xB1 : STEP == 1 ? 0x4E : STEP == 2 ? 0x141 : 0x140;
+        return u32x2{v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true)};
+    } else if constexpr (STEP == 4) {
+        return __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(v, v, false, false));
+    } else {
+        return __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(v, v, false, false));
+    }
 }
-__device__ __forceinline__ double wave_sum(double v)
+template <int STEP = 0> __device__ __forceinline__ double wave_sum(double v)
 {
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) v += other(v, m);
-    return v;
+    const u32x2 r = __builtin_bit_cast(u32x2, v), lo = meet<STEP>(r.x), hi = meet<STEP>(r.y);
+    v = __builtin_bit_cast(double, u32x2{lo.x, hi.x}) + __builtin_bit_cast(double, u32x2{lo.y, hi.y});
+    if constexpr (STEP < 5) return wave_sum<STEP + 1>(v);
+    else return v;
 }
-__device__ __forceinline__ float wave_max(float v)
+template <int STEP = 0> __device__ __forceinline__ float wave_max(float v)
 {
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) v = fmaxf(v, __shfl_xor(v, m));
-    return v;
-}
-__device__ __forceinline__ int wave_min(int v)
-{
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) v = min(v, __shfl_xor(v, m));
-    return v;
+    const u32x2 r = meet<STEP>(__builtin_bit_cast(unsigned, v));
+    v = fmaxf(__builtin_bit_cast(float, (unsigned)r.x), __builtin_bit_cast(float, (unsigned)r.y));
+    if constexpr (STEP < 5) return wave_max<STEP + 1>(v);
+    else return v;
 }
 __device__ __forceinline__ void merge_first(float &ref, int &first, float r, int f)
 {
@@ -128,7 +139,7 @@ __device__ __forceinline__ double factor_of(const DraftKernelArgs &a, int b)
     return t > kCold ? kLog2e / (double)fminf(t, 3.0e38f) : 0.0;
 }
 
-// One part of one row.  A lane's reference is set by its first vectors and raised only where one passes it by 2^kRaise.
+// One part of one row.  A lane's reference is set by its first vectors and raised only where one passes it by kRaise.
 template <bool BF16> __global__ __launch_bounds__(kThreads) void draft_sums_kernel(DraftKernelArgs a)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -156,37 +167,34 @@ template <bool BF16> __global__ __launch_bounds__(kThreads) void draft_sums_kern
                 if (x[e] > ref || first == 0x7fffffff) { ref = x[e]; first = (begin + v) * E + e; }
         }
     } else {
-        const float margin = (float)(kRaise / c);
-        double at = -(double)ref * c, s[2] = {0, 0};
+        const float by = (float)c, margin = (float)(kRaise / c);
         for (int v = tid; v < count; v += kThreads * kLoads) {
             u32x4 w[kLoads];
 #pragma unroll
-            for (int u = 0; u < kLoads; ++u) {
-                const int j = v + u * kThreads;
-                w[u] = p[min(j, count - 1)];
-            }
+            for (int u = 0; u < kLoads; ++u) w[u] = __builtin_nontemporal_load(p + min(v + u * kThreads, count - 1));
 #pragma unroll
             for (int u = 0; u < kLoads; ++u) {
-                if (v + u * kThreads >= count) break;
                 float x[E], top;
                 unpack<BF16>(w[u], x);
                 top = x[0];
 #pragma unroll
                 for (int e = 1; e < E; ++e) top = fmaxf(top, x[e]);
                 if (top - ref > margin) {                    // (the first vectors too)
-                    const double by = power(((double)ref - (double)top) * c);
-                    s[0] *= by;
-                    s[1] *= by;
+                    sum *= power(((double)ref - (double)top) * c);
                     ref = top;
-                    at = -(double)ref * c;
                 }
+                float s[E];
 #pragma unroll
-                for (int e = 0; e < E; ++e) s[e & 1] += power(__builtin_fma((double)x[e], c, at));
+                for (int e = 0; e < E; ++e) s[e] = __builtin_amdgcn_exp2f((x[e] - ref) * by);
+#pragma unroll
+                for (int k = 1; k < E; k *= 2)
+#pragma unroll
+                    for (int e = 0; e + k < E; e += 2 * k) s[e] += s[e + k];
+                sum += v + u * kThreads < count ? (double)s[0] : 0.0;
             }
         }
-        sum = s[0] + s[1];
     }
-    __shared__ State of_wave[kThreads / 64];
+    __shared__ State of_wave[kWaves];
     if (c == 0) {
 #pragma unroll
         for (int m = 1; m < 64; m <<= 1) merge_first(ref, first, __shfl_xor(ref, m), __shfl_xor(first, m));
@@ -199,7 +207,7 @@ template <bool BF16> __global__ __launch_bounds__(kThreads) void draft_sums_kern
     __syncthreads();
     if (tid == 0) {
         State r = of_wave[0];
-        for (int w = 1; w < kThreads / 64; ++w) {
+        for (int w = 1; w < kWaves; ++w) {
             const State o = of_wave[w];
             if (c == 0) merge_first(r.ref, r.first, o.ref, o.first);
             else {
@@ -230,49 +238,95 @@ __device__ __forceinline__ State row_state(const DraftKernelArgs &a, size_t row,
     return r;
 }
 
+// The sum of a whole row's exponentials in fp64, by a workgroup.
+template <bool BF16> __device__ double exact_sum(const uint8_t *row, int vecs, double c, float ref)
+{
+    constexpr int E = BF16 ? 8 : 4;
+    const u32x4 *const p = reinterpret_cast<const u32x4 *>(row);
+    const double at = -(double)ref * c;
+    double s = 0;
+    for (int v = threadIdx.x; v < vecs; v += kThreads) {
+        float x[E];
+        unpack<BF16>(p[v], x);
+#pragma unroll
+        for (int e = 0; e < E; ++e) s += weight_of(x[e], c, at);
+    }
+    s = wave_sum(s);
+    __shared__ double of_wave[kWaves];
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) of_wave[threadIdx.x >> 6] = s;
+    __syncthreads();
+    s = of_wave[0];
+    for (int w = 1; w < kWaves; ++w) s += of_wave[w];
+    return s;
+}
+
 // The drafts' fate, by every workgroup of a sequence for itself; the first one of them writes it.
 template <bool BF16> __global__ __launch_bounds__(kThreads) void draft_decide_kernel(DraftKernelArgs a)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     constexpr int E = BF16 ? 8 : 4;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int b = (int)(blockIdx.x / (unsigned)a.parts), part = (int)(blockIdx.x - (unsigned)b * (unsigned)a.parts);
     const int drafts = drafts_of(a, b), V = a.vecs * E;
     const double c = factor_of(a, b);
-    const size_t v_row = (size_t)b * a.nv, d_row = (size_t)a.B * a.nv + (size_t)b * a.n;
-    const size_t row_bytes = (size_t)a.vecs * 16;
-    __shared__ int turned;
-    if (tid == 0) turned = drafts;
-    __syncthreads();
-    for (int i = wave; i < a.n; i += kThreads / 64) {
-        float chance = 0;
-        if (i < drafts) {
-            const int x = a.tokens[(size_t)b * a.n + i];
-            const bool known = x >= 0 && x < V;
-            const State sp = row_state(a, v_row + i, c);
-            double px, qx = 1;
-            if (c == 0) px = sp.first == x ? 1 : 0;
-            else px = known && sp.sum > 0 ? weight_of(logit<BF16>(a.lv + (v_row + i) * row_bytes, x), c, -(double)sp.ref * c) / sp.sum : 0;
-            if (a.ld) {
-                const State sq = row_state(a, d_row + i, c);
-                if (c == 0) qx = sq.first == x ? 1 : 0;
-                else qx = known && sq.sum > 0 ? weight_of(logit<BF16>(a.ld + ((size_t)b * a.n + i) * row_bytes, x), c, -(double)sq.ref * c) / sq.sum : 0;
+    const size_t v_row = (size_t)b * a.nv, d_row = (size_t)a.B * a.nv + (size_t)b * a.n, row_bytes = (size_t)a.vecs * 16;
+    auto row_v = [&](int i) { return a.lv + (v_row + i) * row_bytes; };
+    auto row_d = [&](int i) { return a.ld + ((size_t)b * a.n + i) * row_bytes; };
+    // an exponential at a token, 0 at one that is none
+    auto weight_at = [&](const uint8_t *row, int x, float ref) { return x >= 0 && x < V ? weight_of(logit<BF16>(row, x), c, -(double)ref * c) : 0.0; };
+    auto over = [](double w, double sum) { return sum > 0 ? w / sum : 0.0; };
+    auto chance_of = [](double px, double qx) { return qx > px ? (float)(px / qx) : px > 0 ? 1.0f : 0.0f; };
+    __shared__ int stop;                     // the first draft that does not stand for sure: twice its place, and 1 where it falls for sure
+    int at = 0;
+    for (int from = 0;;) {
+        if (tid == 0) stop = 2 * drafts;
+        __syncthreads();
+        for (int i = from + wave; i < a.n; i += kWaves) {
+            float chance = 0;
+            if (i < drafts) {
+                const int x = a.tokens[(size_t)b * a.n + i];
+                const double u = a.uniforms[(size_t)b * (a.n + 1) + i];
+                const State sp = row_state(a, v_row + i, c);
+                const double px = c == 0 ? (sp.first == x ? 1 : 0) : over(weight_at(row_v(i), x, sp.ref), sp.sum);
+                double qx = 1;
+                if (a.ld) {
+                    const State sq = row_state(a, d_row + i, c);
+                    qx = c == 0 ? (sq.first == x ? 1 : 0) : over(weight_at(row_d(i), x, sq.ref), sq.sum);
+                }
+                const double uq = u * qx;
+                const bool near = c != 0 && px > 0 && uq > 0 && __builtin_fabs(uq - px) <= kNear * px;
+                if (lane == 0 && (near || !(uq < px))) atomicMin(&stop, 2 * i + (near ? 0 : 1));
+                chance = chance_of(px, qx);
             }
-            const double u = a.uniforms[(size_t)b * (a.n + 1) + i];
-            if (lane == 0 && !(u * qx < px)) atomicMin(&turned, i);
-            chance = qx > px ? (float)(px / qx) : px > 0 ? 1.0f : 0.0f;
+            if (part == 0 && lane == 0) a.out_chances[(size_t)b * a.n + i] = chance;
         }
-        if (part == 0 && lane == 0) a.out_chances[(size_t)b * a.n + i] = chance;
+        __syncthreads();
+        const int s = stop;
+        at = s >> 1;
+        if (at >= drafts || (s & 1)) break;
+        // as near to the border as that: again, on sums in fp64
+        const int x = a.tokens[(size_t)b * a.n + at];
+        const double u = a.uniforms[(size_t)b * (a.n + 1) + at];
+        const float ref = row_state(a, v_row + at, c).ref;
+        const double px = over(weight_at(row_v(at), x, ref), exact_sum<BF16>(row_v(at), a.vecs, c, ref));
+        double qx = 1;
+        if (a.ld) {
+            const float rd = row_state(a, d_row + at, c).ref;
+            qx = over(weight_at(row_d(at), x, rd), exact_sum<BF16>(row_d(at), a.vecs, c, rd));
+        }
+        if (part == 0 && tid == 0) a.out_chances[(size_t)b * a.n + at] = chance_of(px, qx);
+        if (!(u * qx < px)) break;
+        from = at + 1;
+        __syncthreads();                                     // (`stop` has been read by all)
     }
-    __syncthreads();
-    const int at = turned;
     const bool down = at < drafts, draws = down || a.bonus;
     if (part == 0) {
         for (int j = tid; j <= a.n; j += kThreads)
             if (j != at || !draws) a.out_tokens[(size_t)b * (a.n + 1) + j] = j < at ? a.tokens[(size_t)b * a.n + j] : -1;
         if (tid == 0) a.out_accepted[b] = at;
     }
-    Verdict verdict{kDone, at, 0, 0, 0, 0, c};
+    Verdict verdict{kDone, at, 0, 0, c};
     State p{}, q{};
     const bool minus = down && a.ld != nullptr;
     const int without = down && a.ld == nullptr ? a.tokens[(size_t)b * a.n + at] : -1;       // a drafter without probabilities was sure of this one
@@ -284,41 +338,51 @@ template <bool BF16> __global__ __launch_bounds__(kThreads) void draft_decide_ke
             if (part == 0 && tid == 0) a.out_tokens[(size_t)b * (a.n + 1) + at] = p.first < V ? p.first : -1;
         } else {
             if (minus) q = row_state(a, d_row + at, c);
-            verdict = Verdict{kDraw, at, p.ref, q.ref, p.sum > 0 ? 1.0 / p.sum : 0.0, q.sum > 0 ? 1.0 / q.sum : 0.0, c};
+            verdict = Verdict{kDraw, at, p.ref, q.ref, c};
         }
     }
     if (part == 0 && tid == 0) a.verdicts[b] = verdict;
     if (verdict.kind == kDone) return;
-    // ---- this part of the row that the token is drawn from
-    const int begin = part * a.per_part, count = min(a.per_part, a.vecs - begin);
-    const u32x4 *const pv = reinterpret_cast<const u32x4 *>(a.lv + (v_row + at) * row_bytes) + begin;
-    const u32x4 *const pd = minus ? reinterpret_cast<const u32x4 *>(a.ld + ((size_t)b * a.n + at) * row_bytes) + begin : pv;
+    // ---- this wave's part of the row that the token is drawn from
+    const int per_wave = a.per_part / kWaves, begin = part * a.per_part + wave * per_wave, end = min(begin + per_wave, a.vecs);
+    const u32x4 *const pv = reinterpret_cast<const u32x4 *>(row_v(at));
     const double at_p = -(double)p.ref * c, at_q = -(double)q.ref * c;
-    double sw = 0, sp = 0;
-    for (int v = tid; v < count; v += kThreads) {
-        float x[E], y[E];
-        unpack<BF16>(pv[v], x);
-        unpack<BF16>(pd[v], y);
+    Sums s{0, 0, 0, 0};
+    if (minus) {
+        const u32x4 *const pd = reinterpret_cast<const u32x4 *>(row_d(at));
+        // p > q as e_p > e_q S_p / S_q; a row without any probability is below whatever there is
+        const double even = q.sum > 0 ? p.sum / q.sum : 0;
+        for (int v = begin + lane; v < end; v += 64) {
+            float x[E], y[E];
+            unpack<BF16>(pv[v], x);
+            unpack<BF16>(pd[v], y);
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const double px = weight_of(x[e], c, at_p) * verdict.inv_p;
-            double w = px;
-            if (minus) w = __builtin_fmax(px - weight_of(y[e], c, at_q) * verdict.inv_q, 0.0);
-            if ((begin + v) * E + e == without) w = 0;
-            sw += w;
-            sp += px;
+            for (int e = 0; e < E; ++e) {
+                const double ep = weight_of(x[e], c, at_p), eq = weight_of(y[e], c, at_q);
+                const bool above = ep > eq * even;
+                s.p += ep;
+                s.q += eq;
+                s.above_p += above ? ep : 0;
+                s.above_q += above ? eq : 0;
+            }
+        }
+        s.q = wave_sum(s.q);
+        s.above_q = wave_sum(s.above_q);
+    } else {
+        for (int v = begin + lane; v < end; v += 64) {
+            float x[E];
+            unpack<BF16>(pv[v], x);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const double ep = weight_of(x[e], c, at_p);
+                s.p += ep;
+                s.above_p += v * E + e != without ? ep : 0;
+            }
         }
     }
-    sw = wave_sum(sw);
-    sp = wave_sum(sp);
-    __shared__ Sums of_wave[kThreads / 64];
-    if (lane == 0) of_wave[wave] = Sums{sw, sp};
-    __syncthreads();
-    if (tid == 0) {
-        Sums s = of_wave[0];
-        for (int w = 1; w < kThreads / 64; ++w) { s.w += of_wave[w].w; s.p += of_wave[w].p; }
-        a.sums[(size_t)b * a.parts + part] = s;
-    }
+    s.p = wave_sum(s.p);
+    s.above_p = wave_sum(s.above_p);
+    if (lane == 0) a.sums[((size_t)b * a.parts + part) * kWaves + wave] = s;
 #endif
 }
 
@@ -342,90 +406,113 @@ __device__ __forceinline__ double before(double v, double *of_wave, double &all)
     __syncthreads();
     double pre = 0;
     all = 0;
-    for (int w = 0; w < kThreads / 64; ++w) {
+    for (int w = 0; w < kWaves; ++w) {
         if (w == wave) pre = all;
         all += of_wave[w];
     }
     return pre + (lane == 0 ? 0.0 : __builtin_bit_cast(double, r));
 }
 
+// in a wave, the sum of a lane's value and all before it
+__device__ __forceinline__ double up_to(double v)
+{
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        u32x2 r = __builtin_bit_cast(u32x2, v);
+        r.x = __shfl_up((int)r.x, m);
+        r.y = __shfl_up((int)r.y, m);
+        if (lane >= m) v += __builtin_bit_cast(double, r);
+    }
+    return v;
+}
+
 template <bool BF16> __global__ __launch_bounds__(kThreads) void draft_pick_kernel(DraftKernelArgs a)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     constexpr int E = BF16 ? 8 : 4;
-    const int tid = threadIdx.x, b = blockIdx.x;
+    const int tid = threadIdx.x, lane = tid & 63, b = blockIdx.x;
     const Verdict verdict = a.verdicts[b];
     if (verdict.kind == kDone) return;
-    const int at = verdict.at;
-    __shared__ double of_wave[kThreads / 64];
-    __shared__ int found, last;
-    __shared__ double start;
-    const Sums s = tid < a.parts ? a.sums[(size_t)b * a.parts + tid] : Sums{0, 0};
-    // what is left of p without q; where p is nowhere above q, p itself
-    double all_w, all_p;
-    const double pre_w = before(s.w, of_wave, all_w), pre_p = before(s.p, of_wave, all_p);
-    const bool left = all_w > 0;
-    const double mine = left ? s.w : s.p, pre = left ? pre_w : pre_p;
-    const double mark = __builtin_fmax((double)a.uniforms[(size_t)b * (a.n + 1) + a.n], 0.0) * (left ? all_w : all_p);
-    if (tid == 0) { found = a.parts; last = -1; }
-    __syncthreads();
-    if (tid < a.parts && mine > 0) {
-        if (pre + mine > mark) atomicMin(&found, tid);
-        atomicMax(&last, tid);
-    }
-    __syncthreads();
-    const int part = found < a.parts ? found : last;
-    if (part < 0) {                                          // no probability anywhere
-        if (tid == 0) a.out_tokens[(size_t)b * (a.n + 1) + at] = -1;
-        return;
-    }
-    if (tid == part) start = pre;
-    __syncthreads();
-    if (tid == 0) { found = 0x7fffffff; last = -1; }
-    // ---- within the part, neighbouring vectors per thread
+    const int at = verdict.at, pieces = a.parts * kWaves, per_piece = a.per_part / kWaves;
+    __shared__ double of_wave[kWaves], start;
+    __shared__ int found, last, token;
     const int drafts = drafts_of(a, b);
-    const bool down = at < drafts, minus = left && down && a.ld != nullptr;
-    const int without = left && down && a.ld == nullptr ? a.tokens[(size_t)b * a.n + at] : -1;
+    const bool down = at < drafts, minus = down && a.ld != nullptr;
+    const int without = down && a.ld == nullptr ? a.tokens[(size_t)b * a.n + at] : -1;
     const size_t row_bytes = (size_t)a.vecs * 16;
-    const int begin = part * a.per_part, count = min(a.per_part, a.vecs - begin), each = (count + kThreads - 1) / kThreads;
-    const u32x4 *const pv = reinterpret_cast<const u32x4 *>(a.lv + ((size_t)b * a.nv + at) * row_bytes) + begin;
-    const u32x4 *const pd = minus ? reinterpret_cast<const u32x4 *>(a.ld + ((size_t)b * a.n + at) * row_bytes) + begin : pv;
+    const uint8_t *const row_v = a.lv + ((size_t)b * a.nv + at) * row_bytes, *const row_d = minus ? a.ld + ((size_t)b * a.n + at) * row_bytes : row_v;
     const double c = verdict.c, at_p = -(double)verdict.ref_p * c, at_q = -(double)verdict.ref_q * c;
-    auto weights = [&](int v, double *w) __attribute__((always_inline)) {
-        float x[E], y[E];
-        unpack<BF16>(pv[v], x);
-        unpack<BF16>(pd[v], y);
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            w[e] = weight_of(x[e], c, at_p) * verdict.inv_p;
-            if (minus) w[e] = __builtin_fmax(w[e] - weight_of(y[e], c, at_q) * verdict.inv_q, 0.0);
-            if ((begin + v) * E + e == without) w[e] = 0;
+    const double u = __builtin_fmax((double)a.uniforms[(size_t)b * (a.n + 1) + a.n], 0.0);
+    Sums s{0, 0, 0, 0};
+    if (tid < pieces) s = a.sums[(size_t)b * pieces + tid];
+    double all_p, all_q = 0;
+    (void)before(s.p, of_wave, all_p);
+    if (minus) (void)before(s.q, of_wave, all_q);
+    const double inv_p = all_p > 0 ? 1.0 / all_p : 0.0, inv_q = all_q > 0 ? 1.0 / all_q : 0.0;
+    // what is left of p without q; where p is nowhere above q, p itself
+    for (int left = 1; left >= 0; --left) {
+        const double mine = left ? s.above_p * inv_p - s.above_q * inv_q : s.p * inv_p;
+        double all;
+        const double pre = before(mine, of_wave, all), mark = u * all;
+        if (tid == 0) { found = pieces; last = -1; token = -1; }
+        __syncthreads();
+        if (mine > 0) {
+            if (pre + mine > mark) atomicMin(&found, tid);
+            atomicMax(&last, tid);
         }
-    };
-    double sum = 0;
-    for (int v = tid * each; v < min((tid + 1) * each, count); ++v) {
-        double w[E];
-        weights(v, w);
+        __syncthreads();
+        const int piece = found < pieces ? found : last;
+        if (tid == piece) start = pre;
+        __syncthreads();
+        if (piece < 0) continue;
+        // ---- within the piece, neighbouring vectors per thread
+        const int begin = piece * per_piece, end = min(begin + per_piece, a.vecs), each = (end - begin + kThreads - 1) / kThreads;
+        auto weight = [&](float x, float y, int e) __attribute__((always_inline)) {
+            double w = weight_of(x, c, at_p) * inv_p;
+            if (left && minus) w = __builtin_fmax(w - weight_of(y, c, at_q) * inv_q, 0.0);
+            return left && e == without ? 0.0 : w;
+        };
+        double sum = 0;
+        const int mine_from = begin + tid * each;
+        for (int v = mine_from; v < min(mine_from + each, end); ++v) {
+            float x[E], y[E];
+            unpack<BF16>(reinterpret_cast<const u32x4 *>(row_v)[v], x);
+            unpack<BF16>(reinterpret_cast<const u32x4 *>(row_d)[v], y);
 #pragma unroll
-        for (int e = 0; e < E; ++e) sum += w[e];
-    }
-    double all;
-    double so_far = start + before(sum, of_wave, all);
-    // (threads that begin behind the mark have nothing to look for, but that rounding may have taken the mark past the part's end)
-    for (int v = tid * each; v < min((tid + 1) * each, count); ++v) {
-        double w[E];
-        weights(v, w);
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            so_far += w[e];
-            if (w[e] > 0) {
-                if (so_far > mark) atomicMin(&found, (begin + v) * E + e);
-                atomicMax(&last, (begin + v) * E + e);
+            for (int e = 0; e < E; ++e) sum += weight(x[e], y[e], v * E + e);
+        }
+        double whole;
+        const double so_far = start + before(sum, of_wave, whole);
+        if (tid == 0) { found = kThreads; last = -1; }
+        __syncthreads();
+        if (sum > 0) {
+            if (so_far + sum > mark) atomicMin(&found, tid);
+            atomicMax(&last, tid);
+        }
+        __syncthreads();
+        const int who = found < kThreads ? found : last;
+        if (tid == who) start = so_far;
+        __syncthreads();
+        // ---- within that thread's vectors, an element per lane (of every wave the same)
+        if (who >= 0) {
+            const int from = (begin + who * each) * E, to = min(begin + (who + 1) * each, end) * E;
+            double done = start;
+            int hit = -1, fallback = -1;
+            for (int e0 = from; e0 < to && hit < 0; e0 += 64) {
+                const int e = e0 + lane;
+                const double w = e < to ? weight(logit<BF16>(row_v, e), logit<BF16>(row_d, e), e) : 0.0, upto = up_to(w);
+                const unsigned long long passed = __ballot(w > 0 && done + upto > mark), any = __ballot(w > 0);
+                if (passed) hit = e0 + __builtin_ctzll(passed);
+                if (any) fallback = e0 + 63 - __builtin_clzll(any);
+                done += __shfl(upto, 63);
             }
+            if (tid == 0) token = hit >= 0 ? hit : fallback;
         }
+        __syncthreads();
+        if (token >= 0) break;
     }
-    __syncthreads();
-    if (tid == 0) a.out_tokens[(size_t)b * (a.n + 1) + at] = found != 0x7fffffff ? found : last;
+    if (tid == 0) a.out_tokens[(size_t)b * (a.n + 1) + at] = token;      // (-1: no probability anywhere)
 #endif
 }
 
@@ -439,14 +526,14 @@ Plan plan_of(int B, int n, int nv, int V, bool bf16, bool drafter)
         long v = (long)p.vecs * rows / want;                 // vectors per workgroup
         const long least = ((long)p.vecs + most - 1) / most;
         v = v > least ? v : least;
-        v = (v + kThreads - 1) / kThreads * kThreads;
+        v = (v + kThreads - 1) / kThreads * kThreads;        // (a quarter of it per wave: whole waves too)
         per = (int)(v < 0x7fffff00 ? v : 0x7fffff00);
         count = (int)(((long)p.vecs + per - 1) / per);
     };
     divide(rows, 8192, kMostSplits, p.per_split, p.splits);
     divide(B, 1024, kMostParts, p.per_part, p.parts);
     p.states = ((size_t)rows * p.splits * sizeof(State) + 255) / 256 * 256;
-    p.sums = ((size_t)B * p.parts * sizeof(Sums) + 255) / 256 * 256;
+    p.sums = ((size_t)B * p.parts * kWaves * sizeof(Sums) + 255) / 256 * 256;
     p.bytes = p.states + p.sums + (size_t)B * sizeof(Verdict);
     return p;
 }
