@@ -358,6 +358,28 @@ size_t dd_paged_attention_workspace_bytes(int n, int B, int H, int Hkv, int d, i
                                           dd_dtype cache_dtype);
 
 /*
+ * The same for a batch whose sequences share prefixes (several answers to one prompt): sequences group_starts[g] <= b <
+ * group_starts[g+1] have the positions of prefix g before their own,
+ *     O[b,h,i,:] = sum_j softmax_j( Q[b,h,i,:] . K_j / sqrt(d) ) V_j   over the prefix's positions j < prefix_lens[g], on the pages of
+ *     prefix_table[g,:], and the sequence's own positions j < kv_lens[b], on those of block_table[b,:]
+ * as dd_paged_attention computes it on a table that has both, but with a prefix's keys and values read once for all of its sequences
+ * and not once for each.  A prefix may end within a page: the sequence's own positions begin on a page of their own.
+ *   prefix_table [G,max_prefix_pages] i32, prefix_lens [G] i32;  group_starts [G+1] i32, not descending, in [0, B]: sequences below
+ *   group_starts[0] and from group_starts[G] on have no prefix, and a group may have no sequence
+ *   everything else (lengths, pages that are none, empty rows, dtypes, ranges, arithmetic) as for dd_paged_attention
+ * For starts that descend, the outputs of the sequences concerned are unspecified; no access leaves the tensors.  The states of a row's
+ * parts live in `workspace`; how many there are goes by sizes and capacities alone.
+ * G, max_prefix_pages >= 1, max_prefix_pages*page_size < 2^30, (B*(ceil(n*H/Hkv / 32) + 1) + G)*Hkv < 2^24; O overlaps none of its inputs.
+ */
+int dd_paged_attention_shared(const void *Q, const void *Kc, const void *Vc, const float *k_scale, const float *v_scale,
+                              const int32_t *prefix_table, const int32_t *prefix_lens, const int32_t *group_starts,
+                              const int32_t *block_table, const int32_t *kv_lens, void *O,
+                              int n, int B, int H, int Hkv, int d, int num_pages, int page_size, int G, int max_prefix_pages,
+                              int max_pages, dd_dtype cache_dtype, void *workspace, size_t workspace_bytes, void *stream);
+size_t dd_paged_attention_shared_workspace_bytes(int n, int B, int H, int Hkv, int d, int page_size, int G, int max_prefix_pages,
+                                                 int max_pages, dd_dtype cache_dtype);
+
+/*
  * Verification rule of Sec. 3.2 for P = B*G positions (G verified positions per sequence),
  * softmax at temperature 1 over the whole vocabulary, natural logarithm:
  *     c_V,i  = max_x p_V(x | i)                     (Eq. 7)      t_V,i = lowest x attaining it

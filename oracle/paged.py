@@ -124,3 +124,30 @@ def paged_attention(Q, Kc, Vc, k_scale, v_scale, table, kv_lens):
             w /= w.sum(-1, keepdims=True)
             O[b, h], A[b, h] = w @ v, w @ np.abs(v)
     return O, A
+
+
+def paged_attention_shared(Q, Kc, Vc, k_scale, v_scale, prefix_table, prefix_lens, group_starts, table, kv_lens):
+    """-> (O, A) as paged_attention: each sequence on a table of its own that has its prefix's positions and then its own, one page a
+    position."""
+    B, P = np.shape(Q)[0], np.shape(Kc)[2]
+    O, A = np.zeros(np.shape(Q)), np.zeros(np.shape(Q))
+    for b in range(B):
+        slots = []
+        for g in range(len(prefix_lens)):
+            if group_starts[g] <= b < group_starts[g + 1]:
+                held = min(max(int(prefix_lens[g]), 0), len(prefix_table[g]) * P)
+                slots += [(int(prefix_table[g][p // P]), p % P) for p in range(held)]
+        held = min(max(int(kv_lens[b]), 0), len(table[b]) * P)
+        slots += [(int(table[b][p // P]), p % P) for p in range(held)]
+        slots = [(page, at) for page, at in slots if 0 <= page < len(Kc)]
+        if not slots:
+            continue
+        page, at = np.array([s[0] for s in slots]), np.array([s[1] for s in slots])
+        # the cache's rows at those slots, as a cache with pages of one position
+        one_k = np.asarray(Kc, np.float64)[page, :, at][:, :, None, :]
+        one_v = np.asarray(Vc, np.float64)[page, :, :, at][:, :, :, None]
+        ks = None if k_scale is None else np.asarray(k_scale)[page]
+        vs = None if v_scale is None else np.asarray(v_scale)[page]
+        o, a = paged_attention(Q[b:b + 1], one_k, one_v, ks, vs, [list(range(len(slots)))], [len(slots)])
+        O[b], A[b] = o[0], a[0]
+    return O, A

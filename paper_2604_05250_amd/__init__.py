@@ -101,6 +101,10 @@ def lib():
     L.dd_paged_attention.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i, i, i, i, i, i, i, i, i, vp, sz, vp]
     L.dd_paged_attention_workspace_bytes.restype = sz
     L.dd_paged_attention_workspace_bytes.argtypes = [i, i, i, i, i, i, i, i]
+    L.dd_paged_attention_shared.restype = i
+    L.dd_paged_attention_shared.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i, i, i, i, i, i, i, i, i, i, i, vp, sz, vp]
+    L.dd_paged_attention_shared_workspace_bytes.restype = sz
+    L.dd_paged_attention_shared_workspace_bytes.argtypes = [i, i, i, i, i, i, i, i, i, i]
     L.dd_verify_draft.restype = i
     L.dd_verify_draft.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, i, i, i, i, i, vp, sz, vp]
     L.dd_verify_draft_workspace_bytes.restype = sz
@@ -118,7 +122,8 @@ EXPORTS = ("dd_strerror", "dd_version", "dd_bidir_attention", "dd_bidir_attentio
            "dd_block_attention_batched", "dd_block_attention_batched_workspace_bytes",
            "dd_bidir_attention_fp8v", "dd_block_attention_cached_fp8v", "dd_block_attention_cached_fp8v_workspace_bytes",
            "dd_bidir_attention_mx", "dd_qk_norm_rope", "dd_paged_cache_append", "dd_paged_attention",
-           "dd_paged_attention_workspace_bytes", "dd_verify_draft", "dd_verify_draft_workspace_bytes")
+           "dd_paged_attention_workspace_bytes", "dd_verify_draft", "dd_verify_draft_workspace_bytes",
+           "dd_paged_attention_shared", "dd_paged_attention_shared_workspace_bytes")
 
 
 # ---------------------------------------------------------------- marshalling (csrc/binding.cpp)
@@ -274,6 +279,18 @@ def dd_paged_attention(Q, Kc, Vc, block_table, kv_lens, k_scale=None, v_scale=No
     """Attention of Q [B,H,n,d] (bf16) over the kv_lens[b] positions that each sequence holds in a paged cache (shapes as for
     dd_paged_cache_append) -> O [B,H,n,d] bf16; a sequence that holds none gets zeros."""
     return native().paged_attention(Q, Kc, Vc, block_table, kv_lens, k_scale, v_scale, O, cache_dtype)
+
+
+def dd_paged_attention_shared_workspace_bytes(n, B, H, Hkv, d, page_size, G, max_prefix_pages, max_pages, cache_dtype) -> int:
+    return lib().dd_paged_attention_shared_workspace_bytes(n, B, H, Hkv, d, page_size, G, max_prefix_pages, max_pages, cache_dtype)
+
+
+def dd_paged_attention_shared(Q, Kc, Vc, prefix_table, prefix_lens, group_starts, block_table, kv_lens, k_scale=None, v_scale=None, O=None,
+                              cache_dtype: Optional[int] = None):
+    """dd_paged_attention for sequences that share prefixes: sequences group_starts[g] .. group_starts[g+1] - 1 attend the
+    prefix_lens[g] positions on the pages prefix_table[g] and then their own kv_lens[b] on block_table[b]; a prefix is read once for all
+    of them.  prefix_table [G,max_prefix_pages], prefix_lens [G], group_starts [G+1], not descending: i32, on the device."""
+    return native().paged_attention_shared(Q, Kc, Vc, prefix_table, prefix_lens, group_starts, block_table, kv_lens, k_scale, v_scale, O, cache_dtype)
 
 
 def dd_verify_remask_workspace_bytes(B, G, V, logit_dtype) -> int:

@@ -1,0 +1,163 @@
+// Attention over a paged cache of a batch whose sequences share prefixes (the answers to one prompt): a row's keys are those of its group's
+// prefix and its sequence's own.  A softmax can be taken in parts: with the states (m, l, o) of two sets of keys, reference, sum of weights
+// and weighted sum of values, that of both is  M = max(m, m'),  2^(m-M) l + 2^(m'-M) l',  2^(m-M) o + 2^(m'-M) o'.  So the rows of all
+// sequences of a group meet the prefix together, as the rows of one very long block, and its keys are read once for all of them; the own
+// keys are met sequence by sequence; a second kernel merges the states.  The workgroups are those of attention_paged.h, of either kind in
+// one launch where both take one row block, as neither fills the card in a serving batch's step.
+#include "attention_paged.h"
+
+namespace dd {
+namespace {
+
+// Every state of a row, merged by D / 4 lanes: the prefix's splits, then those of the own keys.
+template <int D>
+__global__ __launch_bounds__(256) void shared_merge_kernel(const float *part_ml, const float *part_o, const int32_t *kv_lens, uint8_t *O, int Hkv, int rows_total, int rows,
+                                                           int max_pages, int page_log2, int own_splits, int own_least, int prefix_least, SharedTail a)
+{
+    constexpr int LANES = D / 4;
+    const int row = blockIdx.x * (256 / LANES) + threadIdx.x / LANES, d0 = (threadIdx.x % LANES) * 4;
+    if (row >= rows) return;
+    const int b = (int)((unsigned)row / (unsigned)rows_total / (unsigned)Hkv);
+    const int own = shared_share_of(kv_lens[b], max_pages, page_log2, own_splits, own_least).used;
+    int lo = 0, hi = a.groups;                       // the last group that begins at b or before
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (a.group_starts[mid] <= b) lo = mid;
+        else hi = mid;
+    }
+    const bool member = a.group_starts[lo] <= b && b < a.group_starts[lo + 1];
+    const int shared = member ? shared_share_of(a.prefix_lens[lo], a.max_prefix_pages, page_log2, a.prefix_splits, prefix_least).used : 0;
+    const float2 *ml = reinterpret_cast<const float2 *>(part_ml) + (size_t)row * a.slots;
+    const floatx4 *po = reinterpret_cast<const floatx4 *>(part_o + (size_t)row * a.slots * D + d0);
+    const int count = shared + own;
+    constexpr int U = 8;                             // states on their way
+    float M = kNone, L = 0;
+    floatx4 x = {0, 0, 0, 0};
+    for (int s0 = 0; s0 < count; s0 += U) {
+        float2 st[U];
+        floatx4 v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int k = min(s0 + u, count - 1), s = k < shared ? k : a.prefix_splits + k - shared;
+            st[u] = ml[s];
+            v[u] = po[(size_t)s * (D / 4)];
+        }
+        float top = M;
+#pragma unroll
+        for (int u = 0; u < U; ++u) top = fmaxf(top, s0 + u < count ? st[u].x : M);
+        const float by = __builtin_amdgcn_exp2f(M - top);
+        M = top;
+        L *= by;
+        x *= by;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (s0 + u < count) {
+                const float f = __builtin_amdgcn_exp2f(st[u].x - M);
+                L += f * st[u].y;
+                x += f * v[u];
+            }
+        }
+    }
+    const float inv = L > 0 ? 1.0f / L : 0.0f;       // no key at all: zeros
+    *reinterpret_cast<uint2 *>(O + ((size_t)row * D + d0) * 2) = make_uint2(pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv));
+}
+
+// One kind of workgroup: 32-row blocks each takes, splits of the keys, least tiles of 64 keys of a split, row tiles, workgroups.
+struct Kind { int rg, splits, least; long row_tiles, wgs; };
+struct Plan { Kind prefix, own; int slots; };
+Plan plan_of(const SharedAttnShape &s)
+{
+    const long rows = (long)(s.H / s.Hkv) * s.n, all = rows * s.B;
+    auto blocks_of = [](long r) { return (r + 31) / 32; };
+    auto group_rows = [&](long blocks, bool few, bool full) { return few || blocks <= (s.fp8 ? 512 : 256) ? 1 : full && blocks > (s.fp8 ? 1792 : 1024) ? 4 : 2; };
+    auto is_full = [](long r) { return (r + 127) / 128 * 128 * 8 <= r * 9; };
+    auto splits_of = [](long room, long base, long tiles, int least) {
+        long n = room / base < tiles / least ? room / base : tiles / least;
+        return (int)(n < 1 ? 1 : n > kMaxSplits ? kMaxSplits : n);
+    };
+    Plan p;
+    p.own.rg = group_rows(s.B * (long)s.Hkv * blocks_of(rows), rows <= kFewRows, is_full(rows));
+    p.own.row_tiles = (rows + 32 * p.own.rg - 1) / (32 * p.own.rg);
+    const long own_base = (long)s.B * s.Hkv * p.own.row_tiles;
+    p.own.least = kSplitTiles;
+    p.own.splits = splits_of(kUnits, own_base, ((long)s.max_pages << s.page_log2) / 64, p.own.least);
+    p.own.wgs = own_base * p.own.splits;
+    p.prefix.rg = group_rows((long)s.Hkv * blocks_of(all), all <= kFewRows, is_full(all));
+    p.prefix.row_tiles = all / (32 * p.prefix.rg) + s.G;      // (every group may end within a tile)
+    if (s.G == 1) p.prefix.row_tiles = (all + 32 * p.prefix.rg - 1) / (32 * p.prefix.rg);
+    const long base = (long)s.Hkv * p.prefix.row_tiles;
+    p.prefix.least = kSplitTiles;
+    p.prefix.splits = splits_of(2 * kUnits, base, ((long)s.max_prefix_pages << s.page_log2) / 64, p.prefix.least);
+    p.prefix.wgs = base * p.prefix.splits;
+    p.slots = p.prefix.splits + p.own.splits;
+    return p;
+}
+
+unsigned eights(long wgs) { return (unsigned)((wgs + 7) / 8 * 8); }
+
+template <int D, bool FP8, int NT, bool ONE> hipError_t attend(const SharedAttnArgs &a, const SharedTail &tail, int rg, unsigned grid, unsigned launched, unsigned shape, hipStream_t stream)
+{
+    auto run = [&](auto kernel) {
+        return launch(kernel, dim3(grid), dim3(256), stream, a.table, a.kv_lens, static_cast<const uint8_t *>(a.Kc), static_cast<const uint8_t *>(a.Vc), a.s.Hkv,
+                      (a.s.H / a.s.Hkv) * a.s.n, a.num_pages, a.s.max_pages, launched, shape, tail);
+    };
+    return rg == 1 ? run(attn_paged_kernel<D, FP8, NT, ONE, 1, SharedTail>)
+         : rg == 2 ? run(attn_paged_kernel<D, FP8, NT, ONE, 2, SharedTail>) : run(attn_paged_kernel<D, FP8, NT, ONE, 4, SharedTail>);
+}
+template <int D, bool FP8> hipError_t attend(const SharedAttnArgs &a, const SharedTail &tail, int rg, unsigned grid, unsigned launched, unsigned shape, hipStream_t stream)
+{
+    constexpr int NT = FP8 ? 2 : 1;
+    return (1 << a.s.page_log2) >= 32 * NT ? attend<D, FP8, NT, true>(a, tail, rg, grid, launched, shape, stream)
+                                           : attend<D, FP8, NT, false>(a, tail, rg, grid, launched, shape, stream);
+}
+
+}  // namespace
+
+bool shared_attention_fits(const SharedAttnShape &s)
+{
+    const double rows = (double)(s.H / s.Hkv) * s.n;
+    // (splits are for calls of few workgroups: with or without them a launch of either kind has fewer than 2^24, and all of them 2^25)
+    return rows * s.B * s.Hkv < 1073741824.0 && ((__builtin_ceil(rows / 32) + 1) * s.B + s.G) * s.Hkv < 16777216.0;
+}
+
+size_t shared_attention_workspace_bytes(const SharedAttnShape &s)
+{
+    return (size_t)s.B * s.H * s.n * (size_t)plan_of(s).slots * (size_t)(s.d + 2) * sizeof(float);
+}
+
+hipError_t launch_attention_shared(const SharedAttnArgs &a, hipStream_t stream)
+{
+    const SharedAttnShape &s = a.s;
+    const Plan p = plan_of(s);
+    const size_t rows = (size_t)s.B * s.H * s.n;
+    SharedTail tail;
+    static_cast<PagedTail &>(tail) = PagedTail{static_cast<const uint8_t *>(a.Q), a.k_scale, a.v_scale, static_cast<uint8_t *>(a.O), static_cast<float *>(a.workspace),
+                                               static_cast<float *>(a.workspace) + rows * p.slots * s.d, (float)(1.4426950408889634 / __builtin_sqrt((double)s.d))};
+    tail.prefix_table = a.prefix_table; tail.prefix_lens = a.prefix_lens; tail.group_starts = a.group_starts;
+    tail.groups = s.G; tail.max_prefix_pages = s.max_prefix_pages; tail.B = s.B;
+    tail.prefix_tiles = (unsigned)p.prefix.row_tiles; tail.prefix_splits = p.prefix.splits; tail.slots = p.slots;
+    const unsigned shape = (unsigned)p.own.row_tiles << 8 | (unsigned)(p.own.splits - 1) << 2 | (unsigned)(s.page_log2 - 4);
+    auto part = [&](int rg, long prefix_wgs, long own_wgs, int least) {
+        tail.prefix_wgs = eights(prefix_wgs); tail.own_wgs = (unsigned)own_wgs; tail.least = least;
+        const unsigned grid = tail.prefix_wgs + eights(own_wgs);
+        return s.d == 128 ? (s.fp8 ? attend<128, true>(a, tail, rg, grid, (unsigned)prefix_wgs, shape, stream) : attend<128, false>(a, tail, rg, grid, (unsigned)prefix_wgs, shape, stream))
+                          : (s.fp8 ? attend<64, true>(a, tail, rg, grid, (unsigned)prefix_wgs, shape, stream) : attend<64, false>(a, tail, rg, grid, (unsigned)prefix_wgs, shape, stream));
+    };
+    hipError_t e;
+    if (p.prefix.rg == p.own.rg && p.prefix.least == p.own.least) {
+        e = part(p.own.rg, p.prefix.wgs, p.own.wgs, p.own.least);
+    } else {
+        e = part(p.prefix.rg, p.prefix.wgs, 0, p.prefix.least);
+        if (e == hipSuccess) e = part(p.own.rg, 0, p.own.wgs, p.own.least);
+    }
+    if (e != hipSuccess) return e;
+    const unsigned per_wg = 256 / (s.d / 4);
+    const dim3 grid((unsigned)((rows + per_wg - 1) / per_wg));
+    auto merge = [&](auto kernel) {
+        return launch(kernel, grid, dim3(256), stream, tail.part_ml, tail.part_o, a.kv_lens, tail.O, s.Hkv, (s.H / s.Hkv) * s.n, (int)rows, s.max_pages, s.page_log2,
+                      p.own.splits, p.own.least, p.prefix.least, tail);
+    };
+    return s.d == 128 ? merge(shared_merge_kernel<128>) : merge(shared_merge_kernel<64>);
+}
+
+}  // namespace dd

@@ -768,6 +768,36 @@ PyObject *paged_attention(PyObject *const *a, Py_ssize_t n)
     return THPVariable_Wrap(out);
 }
 
+// (Q, Kc, Vc, prefix_table, prefix_lens, group_starts, block_table, kv_lens, k_scale, v_scale, O, cache_dtype) -> O
+PyObject *paged_attention_shared(PyObject *const *a, Py_ssize_t n)
+{
+    want(n, 12);
+    const at::Tensor &Q = tensor(a[0], "Q"), &Kc = tensor(a[1], "Kc"), &Vc = tensor(a[2], "Vc"), &prefix = tensor(a[3], "prefix_table");
+    const at::Tensor &plens = tensor(a[4], "prefix_lens"), &starts = tensor(a[5], "group_starts"), &table = tensor(a[6], "block_table"), &lens = tensor(a[7], "kv_lens");
+    const at::Tensor *ks = opt_tensor(a[8], "k_scale"), *vs = opt_tensor(a[9], "v_scale"), *O = opt_tensor(a[10], "O");
+    const Pages p = pages_of(Kc, Vc, table, ks, vs, a[11]);
+    if (prefix.dim() != 2 || prefix.scalar_type() != at::kInt) value_error("", "prefix_table must be int32 with two dimensions");
+    const int64_t G = prefix.size(0), most = prefix.size(1);
+    if (Q.dim() != 4 || Q.size(0) != p.B || Q.size(3) != p.d) value_error("", "Q shape must be [B,H,n,d] matching the cache and block_table");
+    const int64_t H = Q.size(1), rows = Q.size(2);
+    fits_int({H, rows, G, most});
+    elements_of(&Q, DD_BF16, "Q"); elements_of(O, DD_BF16, "O");
+    ints_of(&lens, p.B, "kv_lens"); ints_of(&plens, G, "prefix_lens"); ints_of(&starts, G + 1, "group_starts");
+    room_for(O, p.B * H * rows * p.d, 2, "O");
+    const OneDevice dev(Q);
+    void *const q = dev(Q, "Q"), *const kc = dev(Kc, "Kc"), *const vc = dev(Vc, "Vc"), *const pt = dev(prefix, "prefix_table"), *const pl = dev(plens, "prefix_lens");
+    void *const gs = dev(starts, "group_starts"), *const t = dev(table, "block_table"), *const ln = dev(lens, "kv_lens");
+    void *const sk = dev(ks, "k_scale"), *const sv = dev(vs, "v_scale");
+    const c10::hip::HIPGuard guard(Q.device().index());
+    const at::Tensor out = O ? *O : empty_like_type({p.B, H, rows, p.d}, Q.scalar_type(), Q);
+    void *const o = dev(out, "O");
+    const Call c(dd_paged_attention_shared_workspace_bytes(rows, p.B, H, p.Hkv, p.d, p.size, G, most, p.max, (dd_dtype)p.tag), Q);
+    check(c.run([&] { return dd_paged_attention_shared(q, kc, vc, (const float *)sk, (const float *)sv, (const int32_t *)pt, (const int32_t *)pl, (const int32_t *)gs,
+                                                          (const int32_t *)t, (const int32_t *)ln, o, rows, p.B, H, p.Hkv, p.d, p.num, p.size, G, most, p.max,
+                                                          (dd_dtype)p.tag, c.ptr(), c.bytes(), c.stream); }), "dd_paged_attention_shared");
+    return THPVariable_Wrap(out);
+}
+
 // (logits_v, logits_d, tokens, uniforms, temperature, n_draft, out_tokens, out_accepted, out_chances, logit_dtype) -> the three outputs
 PyObject *verify_draft(PyObject *const *a, Py_ssize_t n)
 {
@@ -853,6 +883,7 @@ PyObject *entry(PyObject *, PyObject *const *a, Py_ssize_t n)
 PyMethodDef methods[] = {DD_METHOD(bidir), DD_METHOD(block), DD_METHOD(bidir_fp8v), DD_METHOD(bidir_mx), DD_METHOD(block_fp8v),
                          DD_METHOD(cache_insert), DD_METHOD(verify_remask), DD_METHOD(unmask), DD_METHOD(verify_scores),
                          DD_METHOD(qk_norm_rope), DD_METHOD(paged_append), DD_METHOD(paged_attention), DD_METHOD(verify_draft),
+                         DD_METHOD(paged_attention_shared),
                          DD_METHOD(set_error_class), DD_METHOD(set_fixed_workspace), DD_METHOD(reset_workspace_peak),
                          DD_METHOD(workspace_peak), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", "argument marshalling of paper_2604_05250_amd", -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -592,6 +592,60 @@ int dd_paged_attention(const void *Q, const void *Kc, const void *Vc, const floa
     return e == hipSuccess ? DD_OK : DD_ERR_LAUNCH;
 }
 
+static dd::SharedAttnShape shared_shape(int n, int B, int H, int Hkv, int d, int page_size, int G, int max_prefix_pages, int max_pages, dd_dtype t)
+{
+    dd::SharedAttnShape s;
+    s.n = n; s.B = B; s.H = H; s.Hkv = Hkv; s.d = d; s.G = G; s.max_prefix_pages = max_prefix_pages; s.max_pages = max_pages;
+    s.page_log2 = page_log2_of(page_size); s.fp8 = t == DD_FP8_E4M3;
+    return s;
+}
+
+size_t dd_paged_attention_shared_workspace_bytes(int n, int B, int H, int Hkv, int d, int page_size, int G, int max_prefix_pages, int max_pages,
+                                                 dd_dtype cache_dtype)
+{
+    if (n < 1 || B < 1 || H < 1 || Hkv < 1 || H % Hkv != 0 || (d != 64 && d != 128) || G < 1 || max_prefix_pages < 1 || max_pages < 1) return 0;
+    if (page_log2_of(page_size) < 0 || (cache_dtype != DD_BF16 && cache_dtype != DD_FP8_E4M3)) return 0;
+    if ((double)max_pages * page_size >= 1073741824.0 || (double)max_prefix_pages * page_size >= 1073741824.0) return 0;
+    const dd::SharedAttnShape s = shared_shape(n, B, H, Hkv, d, page_size, G, max_prefix_pages, max_pages, cache_dtype);
+    return dd::shared_attention_fits(s) ? dd::shared_attention_workspace_bytes(s) : 0;
+}
+
+int dd_paged_attention_shared(const void *Q, const void *Kc, const void *Vc, const float *k_scale, const float *v_scale,
+                              const int32_t *prefix_table, const int32_t *prefix_lens, const int32_t *group_starts,
+                              const int32_t *block_table, const int32_t *kv_lens, void *O,
+                              int n, int B, int H, int Hkv, int d, int num_pages, int page_size, int G, int max_prefix_pages,
+                              int max_pages, dd_dtype cache_dtype, void *workspace, size_t workspace_bytes, void *stream)
+{
+    int rc = check_pages(Kc, Vc, k_scale, v_scale, block_table, kv_lens, n, B, Hkv, d, num_pages, page_size, max_pages, cache_dtype);
+    if (rc != DD_OK) return rc;
+    if (!prefix_table || !prefix_lens || !group_starts) return DD_ERR_NULL;
+    if (H < 1 || H % Hkv != 0 || G < 1 || max_prefix_pages < 1 || (double)max_prefix_pages * page_size >= 1073741824.0) return DD_ERR_SHAPE;
+    if (((reinterpret_cast<uintptr_t>(prefix_table) | reinterpret_cast<uintptr_t>(prefix_lens) | reinterpret_cast<uintptr_t>(group_starts)) & 3u) != 0) return DD_ERR_ALIGN;
+    if (n == 0) return DD_OK;
+    if (!Q || !O) return DD_ERR_NULL;
+    const dd::SharedAttnShape s = shared_shape(n, B, H, Hkv, d, page_size, G, max_prefix_pages, max_pages, cache_dtype);
+    if (!dd::shared_attention_fits(s)) return DD_ERR_SHAPE;
+    if (misaligned16(Q) || misaligned16(O)) return DD_ERR_ALIGN;
+    rc = check_workspace(workspace, workspace_bytes, dd::shared_attention_workspace_bytes(s));
+    if (rc != DD_OK) return rc;
+    const uintptr_t rows_bytes = (uintptr_t)B * H * n * d * 2, cache_bytes = (uintptr_t)num_pages * Hkv * page_size * d * (s.fp8 ? 1 : 2);
+    const uintptr_t scale_bytes = (uintptr_t)num_pages * Hkv * sizeof(float);
+    if (overlap(O, rows_bytes, Q, rows_bytes) || overlap(O, rows_bytes, Kc, cache_bytes) || overlap(O, rows_bytes, Vc, cache_bytes)) return DD_ERR_SHAPE;
+    if (s.fp8 && (overlap(O, rows_bytes, k_scale, scale_bytes) || overlap(O, rows_bytes, v_scale, scale_bytes))) return DD_ERR_SHAPE;
+    if (overlap(O, rows_bytes, prefix_table, (uintptr_t)G * max_prefix_pages * 4) || overlap(O, rows_bytes, prefix_lens, (uintptr_t)G * 4) ||
+        overlap(O, rows_bytes, group_starts, ((uintptr_t)G + 1) * 4) || overlap(O, rows_bytes, block_table, (uintptr_t)B * max_pages * 4) ||
+        overlap(O, rows_bytes, kv_lens, (uintptr_t)B * 4))
+        return DD_ERR_SHAPE;
+    dd::SharedAttnArgs a;
+    a.s = s;
+    a.Q = Q; a.Kc = Kc; a.Vc = Vc; a.O = O;
+    a.k_scale = s.fp8 ? k_scale : nullptr; a.v_scale = s.fp8 ? v_scale : nullptr;
+    a.prefix_table = prefix_table; a.prefix_lens = prefix_lens; a.group_starts = group_starts; a.table = block_table; a.kv_lens = kv_lens;
+    a.num_pages = num_pages; a.workspace = workspace;
+    const hipError_t e = dd::launch_attention_shared(a, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? DD_OK : DD_ERR_LAUNCH;
+}
+
 size_t dd_verify_remask_workspace_bytes(int B, int G, int V, dd_dtype logit_dtype)
 {
     if (B < 0 || G < 0 || V < 1 || (logit_dtype != DD_F32 && logit_dtype != DD_BF16)) return 0;

@@ -213,6 +213,21 @@ struct PagedAttnArgs {
 size_t paged_attention_workspace_bytes(int n, int B, int H, int Hkv, int d, long capacity, bool fp8);     // capacity: keys of a table row
 hipError_t launch_attention_paged(const PagedAttnArgs &a, hipStream_t stream);
 
+// ---- ... of sequences that share prefixes (attention_shared.hip)
+struct SharedAttnShape { int n = 0, B = 0, H = 0, Hkv = 0, d = 0, G = 0, max_prefix_pages = 0, max_pages = 0, page_log2 = 0; bool fp8 = false; };
+struct SharedAttnArgs {
+    SharedAttnShape s;
+    const void *Q = nullptr, *Kc = nullptr, *Vc = nullptr;
+    const float *k_scale = nullptr, *v_scale = nullptr;      // [pages, Hkv]: e4m3 pages
+    const int32_t *prefix_table = nullptr, *prefix_lens = nullptr, *group_starts = nullptr, *table = nullptr, *kv_lens = nullptr;
+    void *O = nullptr;
+    int num_pages = 0;
+    void *workspace = nullptr;
+};
+bool shared_attention_fits(const SharedAttnShape &s);        // whether launches have few enough workgroups
+size_t shared_attention_workspace_bytes(const SharedAttnShape &s);
+hipError_t launch_attention_shared(const SharedAttnArgs &a, hipStream_t stream);
+
 // merge of the partial states (a.splits > 1), carrying the cache refresh on extra workgroups when one is asked for
 hipError_t launch_attention_combine(const AttnArgs &a, hipStream_t stream);
 // what every attention launcher ends with: the merge if the key range was split (`splits_used` > 1),
