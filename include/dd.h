@@ -331,6 +331,32 @@ int dd_paged_cache_append(void *Kc, void *Vc, float *k_scale, float *v_scale,
                           dd_dtype row_dtype, dd_dtype cache_dtype, void *stream);
 
 /*
+ * Pages for sequences that grow, shrink and end, from their lengths: sequence b, of lens[b] positions on the first
+ * have = ceil(lens[b] / page_size) pages of block_table[b,:], shall have new_lens[b] on need = ceil(new_lens[b] / page_size).
+ *     need < have: entries need .. have - 1 go back to the pool and become -1
+ *     need > have: entries have .. need - 1 are set to free pages.  In the order of b, a sequence gets them if the pages that it and the
+ *         sequences before it ask for (those that get none included) are no more than are free once all pages have come back
+ * free_pages [capacity] i32 is the pool's stack, its first *num_free entries are free.  With F entries and R pages given back, the i-th of
+ * them (in the order of sequences, then entries) goes to place F + R - 1 - i, the t-th page taken comes from place F + R - 1 - t, and
+ * *num_free becomes F + R less the pages taken: a call and its opposite leave the tables and the stack as they were.
+ *   out_lens [B] i32 = new_lens[b] (0 below 0), or lens[b] where the pages were not there or new_lens[b] > max_pages*page_size: then
+ *       the sequence is left as it is.  May be lens or new_lens
+ *   positions, slots [B,n] i32 for row r < n that follows the lens[b] positions (both or neither; n may be 0): positions = lens[b] + r, and
+ *       slots = page * page_size + position % page_size where lens[b] + r < out_lens[b], else -1 (a page that is none: -1 too)
+ * With the positions for dd_qk_norm_rope, the rows go into the pages with starts = lens, n_rows = out_lens - lens.  Sequences that share a
+ * prefix have its pages in a table of its own (dd_paged_attention_shared), so no page is in two rows of these tables.
+ * lens are clamped to [0, max_pages*page_size], *num_free to [0, capacity]; whatever the arrays hold, no access leaves them; a stack
+ * with too little room for the pages that come back loses some.
+ * num_pages (= capacity) * page_size < 2^31, max_pages*page_size < 2^30, B*max_pages < 2^31, n < 2^30, B*n < 2^31; B >= 0 (0: a no-op);
+ * page_size 16, 32, 64 or 128.  No two arrays overlap, but for out_lens as above (DD_ERR_SHAPE).  Calls with few sequences and rows need no
+ * workspace.
+ */
+int dd_paged_resize(int32_t *block_table, int32_t *free_pages, int32_t *num_free, const int32_t *lens, const int32_t *new_lens,
+                    int32_t *out_lens, int32_t *positions, int32_t *slots,
+                    int n, int B, int num_pages, int page_size, int max_pages, void *workspace, size_t workspace_bytes, void *stream);
+size_t dd_paged_resize_workspace_bytes(int n, int B, int page_size, int max_pages);
+
+/*
  * Drafter attention over a paged cache, from single tokens (n = 1) to blocks and prompts: the formula of
  * dd_block_attention_cached (no causal mask) over the positions j < kv_lens[b] that sequence b holds,
  *     O[b,h,i,:] = sum_j softmax_j( Q[b,h,i,:] . K_j / sqrt(d) ) V_j

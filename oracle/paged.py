@@ -151,3 +151,37 @@ def paged_attention_shared(Q, Kc, Vc, k_scale, v_scale, prefix_table, prefix_len
         o, a = paged_attention(Q[b:b + 1], one_k, one_v, ks, vs, [list(range(len(slots)))], [len(slots)])
         O[b], A[b] = o[0], a[0]
     return O, A
+
+
+def paged_resize(table, free_pages, num_free, lens, new_lens, page_size, n):
+    """-> (table, free_pages, num_free, out_lens, positions, slots), one sequence after the other with the stack as a list."""
+    table = [list(map(int, row)) for row in table]
+    stack, width = list(map(int, free_pages)), len(table[0])
+    free = stack[:min(max(int(num_free), 0), len(stack))]
+    pages = lambda x: -(-x // page_size)
+    lens = [min(max(int(x), 0), width * page_size) for x in lens]
+    want = [max(int(x), 0) for x in new_lens]
+    back = []
+    for row, a, w in zip(table, lens, want):
+        if pages(w) < pages(a):
+            back += row[pages(w):pages(a)]
+            row[pages(w):pages(a)] = [-1] * (pages(a) - pages(w))
+    free += back[::-1]
+    stack[:len(free)] = free
+    there, asked, out, positions, slots = len(free), 0, [], [], []
+    for row, a, w in zip(table, lens, want):
+        more = pages(w) - pages(a)
+        if w > width * page_size:
+            w = a
+        elif more > 0:
+            asked += more
+            if asked > there:
+                w = a
+            else:
+                row[pages(a):pages(w)] = [free.pop() for _ in range(more)]
+        out.append(w)
+        positions.append([a + r for r in range(n)])
+        at = [row[p // page_size] if p < w else -1 for p in positions[-1]]
+        slots.append([page * page_size + p % page_size if page >= 0 else -1 for page, p in zip(at, positions[-1])])
+    as_ints = lambda x: np.array(x, np.int64)
+    return as_ints(table), as_ints(stack), len(free), as_ints(out), as_ints(positions).reshape(len(lens), n), as_ints(slots).reshape(len(lens), n)

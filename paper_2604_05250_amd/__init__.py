@@ -101,6 +101,10 @@ def lib():
     L.dd_paged_attention.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i, i, i, i, i, i, i, i, i, vp, sz, vp]
     L.dd_paged_attention_workspace_bytes.restype = sz
     L.dd_paged_attention_workspace_bytes.argtypes = [i, i, i, i, i, i, i, i]
+    L.dd_paged_resize.restype = i
+    L.dd_paged_resize.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i, i, i, i, i, vp, sz, vp]
+    L.dd_paged_resize_workspace_bytes.restype = sz
+    L.dd_paged_resize_workspace_bytes.argtypes = [i, i, i, i]
     L.dd_paged_attention_shared.restype = i
     L.dd_paged_attention_shared.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i, i, i, i, i, i, i, i, i, i, i, vp, sz, vp]
     L.dd_paged_attention_shared_workspace_bytes.restype = sz
@@ -123,7 +127,8 @@ EXPORTS = ("dd_strerror", "dd_version", "dd_bidir_attention", "dd_bidir_attentio
            "dd_bidir_attention_fp8v", "dd_block_attention_cached_fp8v", "dd_block_attention_cached_fp8v_workspace_bytes",
            "dd_bidir_attention_mx", "dd_qk_norm_rope", "dd_paged_cache_append", "dd_paged_attention",
            "dd_paged_attention_workspace_bytes", "dd_verify_draft", "dd_verify_draft_workspace_bytes",
-           "dd_paged_attention_shared", "dd_paged_attention_shared_workspace_bytes")
+           "dd_paged_attention_shared", "dd_paged_attention_shared_workspace_bytes",
+           "dd_paged_resize", "dd_paged_resize_workspace_bytes")
 
 
 # ---------------------------------------------------------------- marshalling (csrc/binding.cpp)
@@ -269,6 +274,18 @@ def dd_paged_cache_append(Kc, Vc, K, V, block_table, starts, kv_lens=None, n_row
     call; default: starts), n_rows (default: n) [B]: i32, on the device.  In place; returns None."""
     native().paged_append(Kc, Vc, K, V, block_table, starts, kv_lens, n_rows, k_scale, v_scale, k_weight, eps, inv_freq, interleaved,
                           row_dtype, cache_dtype)
+
+
+def dd_paged_resize_workspace_bytes(n, B, page_size, max_pages) -> int:
+    return lib().dd_paged_resize_workspace_bytes(n, B, page_size, max_pages)
+
+
+def dd_paged_resize(block_table, free_pages, num_free, lens, new_lens, page_size: int, n: int = 0, out_lens=None, positions=None, slots=None):
+    """Sequences of lens [B] positions grow or shrink to new_lens [B]: pages that are over go back from block_table [B,max_pages] to
+    the stack free_pages [pages] (its first num_free [1] entries are free), what is missing is taken from there, in place; a
+    sequence whose pages are not there stays as it is.  All int32 on the device.  Returns (out_lens [B]: the lengths now; positions
+    [B,n] and slots [B,n] of the n rows behind lens: page * page_size + offset, -1 where the sequence has none; None each for n == 0)."""
+    return native().paged_resize(block_table, free_pages, num_free, lens, new_lens, page_size, n, out_lens, positions, slots)
 
 
 def dd_paged_attention_workspace_bytes(n, B, H, Hkv, d, page_size, max_pages, cache_dtype) -> int:

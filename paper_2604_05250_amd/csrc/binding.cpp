@@ -798,6 +798,52 @@ PyObject *paged_attention_shared(PyObject *const *a, Py_ssize_t n)
     return THPVariable_Wrap(out);
 }
 
+// (block_table, free_pages, num_free, lens, new_lens, page_size, n, out_lens, positions, slots) -> (out_lens, positions | None, slots | None)
+PyObject *paged_resize(PyObject *const *a, Py_ssize_t n)
+{
+    want(n, 10);
+    const at::Tensor &table = tensor(a[0], "block_table"), &stack = tensor(a[1], "free_pages"), &count = tensor(a[2], "num_free");
+    const at::Tensor &lens = tensor(a[3], "lens"), &new_lens = tensor(a[4], "new_lens");
+    const at::Tensor *ol = opt_tensor(a[7], "out_lens"), *op = opt_tensor(a[8], "positions"), *os = opt_tensor(a[9], "slots");
+    int64_t sizes[2];
+    for (int i = 0; i < 2; ++i) {
+        PyObject *v = exact_integer(a[5 + i], i == 0 ? "page_size" : "n");
+        int over = 0;
+        sizes[i] = PyLong_AsLongLongAndOverflow(v, &over);
+        Py_DECREF(v);
+        if (over != 0 || sizes[i] < 0) value_error(i == 0 ? "page_size" : "n", "is out of range");
+    }
+    const int64_t page = sizes[0], rows = sizes[1];
+    if (table.dim() != 2 || table.scalar_type() != at::kInt) value_error("", "block_table must be int32 with two dimensions");
+    const int64_t B = table.size(0), most = table.size(1), pages = stack.numel();
+    fits_int({B, most, pages, page, rows});
+    ints_of(&stack, pages, "free_pages"); ints_of(&count, 1, "num_free"); ints_of(&lens, B, "lens"); ints_of(&new_lens, B, "new_lens");
+    ints_of(ol, B, "out_lens"); ints_of(op, B * rows, "positions"); ints_of(os, B * rows, "slots");
+    const OneDevice dev(table);
+    void *const t = dev(table, "block_table"), *const st = dev(stack, "free_pages"), *const nf = dev(count, "num_free"), *const ln = dev(lens, "lens");
+    void *const nl = dev(new_lens, "new_lens");
+    const c10::hip::HIPGuard guard(table.device().index());
+    const at::Tensor rl = ol ? *ol : empty_like_type({B}, at::kInt, table);
+    const at::Tensor rp = op ? *op : rows > 0 ? empty_like_type({B, rows}, at::kInt, table) : at::Tensor();
+    const at::Tensor rs = os ? *os : rows > 0 ? empty_like_type({B, rows}, at::kInt, table) : at::Tensor();
+    void *const wl = dev(rl, "out_lens"), *const wp = dev(rp.defined() ? &rp : nullptr, "positions"), *const wsl = dev(rs.defined() ? &rs : nullptr, "slots");
+    const Call c(dd_paged_resize_workspace_bytes(rows, B, page, most), table);
+    check(c.run([&] { return dd_paged_resize((int32_t *)t, (int32_t *)st, (int32_t *)nf, (const int32_t *)ln, (const int32_t *)nl, (int32_t *)wl, (int32_t *)wp,
+                                             (int32_t *)wsl, rows, B, pages, page, most, c.ptr(), c.bytes(), c.stream); }), "dd_paged_resize");
+    PyObject *out = PyTuple_New(3);
+    if (out == nullptr) throw Raised{};
+    PyTuple_SET_ITEM(out, 0, THPVariable_Wrap(rl));
+    int i = 1;
+    for (const at::Tensor *r : {&rp, &rs}) {
+        if (r->defined()) {
+            PyTuple_SET_ITEM(out, i++, THPVariable_Wrap(*r));
+        } else {
+            Py_INCREF(Py_None); PyTuple_SET_ITEM(out, i++, Py_None);
+        }
+    }
+    return out;
+}
+
 // (logits_v, logits_d, tokens, uniforms, temperature, n_draft, out_tokens, out_accepted, out_chances, logit_dtype) -> the three outputs
 PyObject *verify_draft(PyObject *const *a, Py_ssize_t n)
 {
@@ -883,7 +929,7 @@ PyObject *entry(PyObject *, PyObject *const *a, Py_ssize_t n)
 PyMethodDef methods[] = {DD_METHOD(bidir), DD_METHOD(block), DD_METHOD(bidir_fp8v), DD_METHOD(bidir_mx), DD_METHOD(block_fp8v),
                          DD_METHOD(cache_insert), DD_METHOD(verify_remask), DD_METHOD(unmask), DD_METHOD(verify_scores),
                          DD_METHOD(qk_norm_rope), DD_METHOD(paged_append), DD_METHOD(paged_attention), DD_METHOD(verify_draft),
-                         DD_METHOD(paged_attention_shared),
+                         DD_METHOD(paged_attention_shared), DD_METHOD(paged_resize),
                          DD_METHOD(set_error_class), DD_METHOD(set_fixed_workspace), DD_METHOD(reset_workspace_peak),
                          DD_METHOD(workspace_peak), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", "argument marshalling of paper_2604_05250_amd", -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -592,6 +592,43 @@ int dd_paged_attention(const void *Q, const void *Kc, const void *Vc, const floa
     return e == hipSuccess ? DD_OK : DD_ERR_LAUNCH;
 }
 
+static bool resize_sizes(int n, int B, int page_size, int max_pages)
+{
+    if (n < 0 || B < 1 || max_pages < 1 || page_log2_of(page_size) < 0) return false;
+    if ((double)max_pages * page_size >= 1073741824.0 || (double)B * max_pages >= 2147483648.0 || n >= 1073741824 || (double)B * n >= 2147483648.0) return false;
+    return dd::paged_resize_workgroups(n, B, max_pages) < 16777216.0;
+}
+
+size_t dd_paged_resize_workspace_bytes(int n, int B, int page_size, int max_pages)
+{
+    return resize_sizes(n, B, page_size, max_pages) ? dd::paged_resize_workspace_bytes(n, B, max_pages) : 0;
+}
+
+int dd_paged_resize(int32_t *block_table, int32_t *free_pages, int32_t *num_free, const int32_t *lens, const int32_t *new_lens,
+                    int32_t *out_lens, int32_t *positions, int32_t *slots,
+                    int n, int B, int num_pages, int page_size, int max_pages, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (B == 0 && n >= 0 && num_pages >= 1 && max_pages >= 1 && page_log2_of(page_size) >= 0) return DD_OK;
+    if (!resize_sizes(n, B, page_size, max_pages) || num_pages < 1 || (double)num_pages * page_size >= 2147483648.0) return DD_ERR_SHAPE;
+    if (!block_table || !free_pages || !num_free || !lens || !new_lens || !out_lens || (n > 0 && (!positions || !slots))) return DD_ERR_NULL;
+    struct Range { const void *at; uintptr_t bytes; };
+    const uintptr_t seqs = (uintptr_t)B * 4, rows = (uintptr_t)B * n * 4;
+    const Range all[8] = {{block_table, (uintptr_t)B * max_pages * 4}, {free_pages, (uintptr_t)num_pages * 4}, {num_free, 4}, {out_lens, seqs},
+                          {positions, rows}, {slots, rows}, {lens, seqs}, {new_lens, seqs}};
+    for (const Range &r : all)
+        if ((reinterpret_cast<uintptr_t>(r.at) & 3u) != 0) return DD_ERR_ALIGN;
+    const int rc = check_workspace(workspace, workspace_bytes, dd::paged_resize_workspace_bytes(n, B, max_pages));
+    if (rc != DD_OK) return rc;
+    for (int i = 0; i < 6; ++i)                              // (what is written, against everything)
+        for (int j = i + 1; j < 8; ++j)
+            if (all[i].bytes && all[j].bytes && !(i == 3 && j >= 6 && all[i].at == all[j].at) && overlap(all[i].at, all[i].bytes, all[j].at, all[j].bytes)) return DD_ERR_SHAPE;
+    dd::TableArgs a;
+    a.table = block_table; a.stack = free_pages; a.num_free = num_free; a.lens = lens; a.new_lens = new_lens; a.out_lens = out_lens; a.positions = positions; a.slots = slots;
+    a.n = n; a.B = B; a.page_log2 = page_log2_of(page_size); a.max_pages = max_pages; a.capacity = num_pages; a.workspace = workspace;
+    const hipError_t e = dd::launch_paged_resize(a, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? DD_OK : DD_ERR_LAUNCH;
+}
+
 static dd::SharedAttnShape shared_shape(int n, int B, int H, int Hkv, int d, int page_size, int G, int max_prefix_pages, int max_pages, dd_dtype t)
 {
     dd::SharedAttnShape s;

@@ -201,6 +201,18 @@ struct PageAppendArgs {
 };
 hipError_t launch_page_append(PageAppendArgs a, int d, bool rows_bf16, bool fp8, hipStream_t stream);
 
+// ---- block tables from lengths (tables.hip) -------------------------------------------
+struct TableArgs {
+    int32_t *table = nullptr, *stack = nullptr, *num_free = nullptr;      // [B, max_pages], [capacity], [1]
+    const int32_t *lens = nullptr, *new_lens = nullptr;
+    int32_t *out_lens = nullptr, *positions = nullptr, *slots = nullptr;  // [B], [B, n] twice
+    int n = 0, B = 0, page_log2 = 0, max_pages = 0, capacity = 0;
+    void *workspace = nullptr;
+};
+double paged_resize_workgroups(int n, int B, int max_pages);
+size_t paged_resize_workspace_bytes(int n, int B, int max_pages);
+hipError_t launch_paged_resize(const TableArgs &a, hipStream_t stream);
+
 // ---- attention over a paged cache (attention_paged.hip) ----------------------------
 struct PagedAttnArgs {
     const void *Q = nullptr, *Kc = nullptr, *Vc = nullptr;

@@ -1,0 +1,153 @@
+"""GPU parity of dd_paged_resize against the oracle: whole numbers, equal."""
+import numpy as np
+import pytest
+
+import paper_2604_05250_amd as dd
+from oracle import paged
+from paper_2604_05250_amd.step import capture_step
+from _paged import ints
+from test_gpu_guard_bands import Guarded
+
+pytestmark = pytest.mark.gpu
+
+
+def _state(rng, lens, P, width, free):
+    """tables of those lengths on pages in random order, and a pool with `free` more"""
+    B = len(lens)
+    held = [min(-(-max(x, 0) // P), width) for x in lens]
+    order = rng.permutation(sum(held) + free)
+    table, at = np.full((B, width), -1, np.int32), 0
+    for b, k in enumerate(held):
+        table[b, :k] = order[at:at + k]
+        at += k
+    stack = np.full(max(1, sum(held) + free), -9, np.int32)
+    stack[:free] = order[at:]
+    return table, stack
+
+
+def _check(table, stack, free, lens, new, P, n, guard=False, in_place=None):
+    import torch
+    g = Guarded()
+    put = (lambda x: g.like(np.ascontiguousarray(x, np.int32))) if guard else ints
+    t, s, f, a, w = put(table), put(stack), put([free]), put(lens), put(new)
+    kw = dict(out_lens={"lens": a, "new": w}[in_place]) if in_place else {}
+    if guard:
+        B = len(lens)
+        kw.update(out_lens=g.empty((B,), torch.int32), positions=g.empty((B, n), torch.int32), slots=g.empty((B, n), torch.int32))
+        need = dd.dd_paged_resize_workspace_bytes(n, B, P, table.shape[1])
+        with dd.fixed_workspace(g.empty((max(need, 256),), torch.uint8)):
+            got = dd.dd_paged_resize(t, s, f, a, w, P, n, **kw)
+        g.check("resize")
+        assert a.tolist() == list(lens) and w.tolist() == list(new)
+    else:
+        got = dd.dd_paged_resize(t, s, f, a, w, P, n, **kw)
+    want = paged.paged_resize(table, stack, free, lens, new, P, n)
+    mine = [t, s, f] + [x if x is not None else torch.empty((len(lens), 0)) for x in got]
+    for name, x, y in zip(("table", "stack", "num_free", "out_lens", "positions", "slots"), mine, want):
+        assert np.array_equal(x.cpu().numpy().reshape(np.shape(y)), y), (name, x.cpu().numpy(), y)
+    return t, s, f, got
+
+
+def _lengths(rng, B, most):
+    lens = rng.integers(0, most + 1, B)
+    new = np.where(rng.random(B) < 0.3, rng.integers(0, most + 1, B), np.clip(lens + rng.integers(-40, 41, B), 0, most))
+    new[rng.random(B) < 0.1] = 0
+    return lens.astype(int), new.astype(int)
+
+
+@pytest.mark.parametrize("P", [16, 32, 64, 128])
+@pytest.mark.parametrize("B,width,n", [(1, 1, 1), (1, 40, 700), (3, 5, 0), (17, 9, 16), (64, 33, 1), (1000, 3, 2), (1024, 2, 8), (1025, 4, 3), (2500, 7, 1), (5, 30, 3000),
+                                       (300, 400, 0)])
+def test_parity(P, B, width, n):
+    rng = np.random.default_rng(B + P)
+    lens, new = _lengths(rng, B, width * P)
+    grown = sum(max(0, -(-w // P) - -(-a // P)) for a, w in zip(lens, new))
+    for free in (grown, grown // 3, 0):                      # pages for all, for some, none but those that come back
+        table, stack = _state(rng, lens, P, width, free)
+        _check(table, stack, free, lens, new, P, n)
+
+
+@pytest.mark.parametrize("B,width,n", [(9, 6, 5), (1200, 6, 5), (40, 2000, 3)])
+@pytest.mark.parametrize("scarce", [False, True])
+def test_nothing_else_is_written(B, width, n, scarce):
+    rng = np.random.default_rng(B)
+    lens, new = _lengths(rng, B, width * 16)
+    free = 3 if scarce else B * width
+    table, stack = _state(rng, lens, 16, width, free)
+    _check(table, stack, free, lens, new, 16, n, guard=True)
+
+
+@pytest.mark.parametrize("B", [7, 1300])
+def test_a_call_and_its_opposite_leave_the_pool_as_it_was(B):
+    import torch
+    rng = np.random.default_rng(B)
+    P, width = 16, 12
+    lens, new = _lengths(rng, B, width * P)
+    free = B * width
+    table, stack = _state(rng, lens, P, width, free)
+    t, s, f, got = _check(table, stack, free, lens, new, P, 0)
+    back = dd.dd_paged_resize(t, s, f, got[0], ints(lens), P)[0]
+    assert back.tolist() == list(lens) and int(f) == free and np.array_equal(t.cpu().numpy(), table) and np.array_equal(s.cpu().numpy()[:free], stack[:free])
+
+
+@pytest.mark.parametrize("B", [5, 1100])
+@pytest.mark.parametrize("where", ["lens", "new"])
+def test_lengths_in_place(B, where):
+    rng = np.random.default_rng(B)
+    lens, new = _lengths(rng, B, 160)
+    table, stack = _state(rng, lens, 16, 10, 100)
+    _check(table, stack, 100, lens, new, 16, 9, in_place=where)
+
+
+def test_lengths_that_do_not_fit():
+    rng = np.random.default_rng(1)
+    lens = [0, 30, 64, 10 ** 9, -5, 17, 2 ** 31 - 1, -2 ** 31]
+    new = [65, 64, 10 ** 9, 64, 20, -3, 5, 2 ** 31 - 1]      # 64 positions fit
+    table, stack = _state(rng, lens, 16, 4, 20)
+    _, _, _, got = _check(table, stack, 20, lens, new, 16, 3, guard=True)
+    assert got[0].tolist() == [0, 64, 64, 64, 20, 0, 5, 0]
+
+
+@pytest.mark.parametrize("B,width", [(6, 4), (1500, 4), (20, 4000)])
+def test_arrays_that_hold_anything_stay_inside(B, width):
+    import torch
+    rng = np.random.default_rng(B)
+    for free in (-2 ** 31, -1, 0, 5, 10 ** 6, 2 ** 31 - 1):
+        g = Guarded()
+        wild = lambda *s: rng.integers(-2 ** 31, 2 ** 31, s, dtype=np.int64).astype(np.int32)
+        t, s, f, a, w = (g.like(x) for x in (wild(B, width), wild(50), np.array([free], np.int32), wild(B), wild(B)))
+        a[::2] = ints(rng.integers(0, width * 16 + 1, B)[::2])
+        w[1::2] = ints(rng.integers(0, width * 16 + 1, B)[1::2])
+        out = [g.empty((B,), torch.int32), g.empty((B, 7), torch.int32), g.empty((B, 7), torch.int32)]
+        with dd.fixed_workspace(g.empty((max(256, dd.dd_paged_resize_workspace_bytes(7, B, 16, width)),), torch.uint8)):
+            dd.dd_paged_resize(t, s, f, a, w, 16, 7, out_lens=out[0], positions=out[1], slots=out[2])
+        g.check(f"num_free {free}")
+        assert 0 <= int(f) <= 50 and bool((out[0] >= 0).all()) and bool((out[0] <= width * 16).all()) and bool((out[2] >= -1).all())
+
+
+def test_graph_replays_match_eager_calls():
+    import torch
+    rng = np.random.default_rng(0)
+    for B, width, n in ((9, 6, 8), (1300, 6, 8)):
+        lens, _ = _lengths(rng, B, width * 16)
+        table, stack = _state(rng, lens, 16, width, 4 * B)
+        state = [ints(table), ints(stack), ints([4 * B]), ints(lens)]
+        want_lens = ints(lens)
+        positions, slots = torch.zeros((B, n), dtype=torch.int32, device="cuda"), torch.zeros((B, n), dtype=torch.int32, device="cuda")
+
+        def step():                                          # the lengths go on in place
+            dd.dd_paged_resize(state[0], state[1], state[2], state[3], want_lens, 16, n, out_lens=state[3], positions=positions, slots=slots)
+
+        graph = capture_step(step)
+        for rep in range(5):
+            want_lens.copy_(ints(np.clip(lens + rng.integers(-60, 61, B), 0, width * 16)))
+            kept = [t.clone() for t in state]
+            step()
+            torch.cuda.synchronize()
+            want = [t.clone() for t in (*state, positions, slots)]
+            for t, k in zip(state, kept):
+                t.copy_(k)
+            positions.zero_(), slots.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(x, y) for x, y in zip(want, (*state, positions, slots))), f"B {B} replay {rep}"
