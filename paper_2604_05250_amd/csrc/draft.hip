@@ -42,7 +42,7 @@ constexpr int kMostParts = 64;               // workgroups of the row that is dr
 struct State { float ref; int first; double sum; };      // reference, its first index (temperature 0), sum
 struct Sums { double p, q, above_p, above_q; };          // of exponentials, of a part of the row that is drawn from: all, and where p > q
 enum { kDone = 0, kDraw = 1 };
-struct Verdict { int kind, at; float ref_p, ref_q; double c; };      // how the token at `at` is drawn
+struct Verdict { int kind, at, minus, without; float ref_p, ref_q; double c; };      // how the token at `at` is drawn
 
 struct DraftKernelArgs {
     const uint8_t *lv, *ld;
@@ -326,7 +326,7 @@ template <bool BF16> __global__ __launch_bounds__(kThreads) void draft_decide_ke
             if (j != at || !draws) a.out_tokens[(size_t)b * (a.n + 1) + j] = j < at ? a.tokens[(size_t)b * a.n + j] : -1;
         if (tid == 0) a.out_accepted[b] = at;
     }
-    Verdict verdict{kDone, at, 0, 0, c};
+    Verdict verdict{kDone, at, 0, -1, 0, 0, c};
     State p{}, q{};
     const bool minus = down && a.ld != nullptr;
     const int without = down && a.ld == nullptr ? a.tokens[(size_t)b * a.n + at] : -1;       // a drafter without probabilities was sure of this one
@@ -338,179 +338,187 @@ template <bool BF16> __global__ __launch_bounds__(kThreads) void draft_decide_ke
             if (part == 0 && tid == 0) a.out_tokens[(size_t)b * (a.n + 1) + at] = p.first < V ? p.first : -1;
         } else {
             if (minus) q = row_state(a, d_row + at, c);
-            verdict = Verdict{kDraw, at, p.ref, q.ref, c};
+            verdict = Verdict{kDraw, at, minus, without, p.ref, q.ref, c};
         }
     }
     if (part == 0 && tid == 0) a.verdicts[b] = verdict;
     if (verdict.kind == kDone) return;
     // ---- this wave's part of the row that the token is drawn from
     const int per_wave = a.per_part / kWaves, begin = part * a.per_part + wave * per_wave, end = min(begin + per_wave, a.vecs);
-    const u32x4 *const pv = reinterpret_cast<const u32x4 *>(row_v(at));
+    const u32x4 *const pv = reinterpret_cast<const u32x4 *>(row_v(at)), *const pd = minus ? reinterpret_cast<const u32x4 *>(row_d(at)) : pv;
     const double at_p = -(double)p.ref * c, at_q = -(double)q.ref * c;
+    // p > q as e_p > e_q S_p / S_q; a row without any probability is below whatever there is
+    const double even = minus && q.sum > 0 ? p.sum / q.sum : 0;
     Sums s{0, 0, 0, 0};
-    if (minus) {
-        const u32x4 *const pd = reinterpret_cast<const u32x4 *>(row_d(at));
-        // p > q as e_p > e_q S_p / S_q; a row without any probability is below whatever there is
-        const double even = q.sum > 0 ? p.sum / q.sum : 0;
+    if (begin < end) {
+        u32x4 wv = pv[min(begin + lane, end - 1)], wd = pd[min(begin + lane, end - 1)];
         for (int v = begin + lane; v < end; v += 64) {
             float x[E], y[E];
-            unpack<BF16>(pv[v], x);
-            unpack<BF16>(pd[v], y);
+            unpack<BF16>(wv, x);
+            unpack<BF16>(wd, y);
+            wv = pv[min(v + 64, end - 1)];                   // (the next ones, on their way meanwhile)
+            wd = pd[min(v + 64, end - 1)];
+            if (minus) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const double ep = weight_of(x[e], c, at_p), eq = weight_of(y[e], c, at_q);
-                const bool above = ep > eq * even;
-                s.p += ep;
-                s.q += eq;
-                s.above_p += above ? ep : 0;
-                s.above_q += above ? eq : 0;
-            }
-        }
-        s.q = wave_sum(s.q);
-        s.above_q = wave_sum(s.above_q);
-    } else {
-        for (int v = begin + lane; v < end; v += 64) {
-            float x[E];
-            unpack<BF16>(pv[v], x);
+                for (int e = 0; e < E; ++e) {
+                    const double ep = weight_of(x[e], c, at_p), eq = weight_of(y[e], c, at_q);
+                    const bool above = ep > eq * even;
+                    s.p += ep;
+                    s.q += eq;
+                    s.above_p += above ? ep : 0;
+                    s.above_q += above ? eq : 0;
+                }
+            } else {
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const double ep = weight_of(x[e], c, at_p);
-                s.p += ep;
-                s.above_p += v * E + e != without ? ep : 0;
+                for (int e = 0; e < E; ++e) {
+                    const double ep = weight_of(x[e], c, at_p);
+                    s.p += ep;
+                    s.above_p += v * E + e != without ? ep : 0;
+                }
             }
         }
     }
+    s.q = wave_sum(s.q);
+    s.above_q = wave_sum(s.above_q);
     s.p = wave_sum(s.p);
     s.above_p = wave_sum(s.above_p);
     if (lane == 0) a.sums[((size_t)b * a.parts + part) * kWaves + wave] = s;
 #endif
 }
 
-// Sums of the threads before, in the threads' order, and the sum of all.
-__device__ __forceinline__ double before(double v, double *of_wave, double &all)
+// in a wave, the sum of a lane's value and all before it: within rows of sixteen lanes, then the rows' last lanes to the rows behind them
+template <int CTRL, int ROWS> __device__ __forceinline__ double moved(double v)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    double s = v;
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) {
-        u32x2 r = __builtin_bit_cast(u32x2, s);
-        r.x = __shfl_up((int)r.x, m);
-        r.y = __shfl_up((int)r.y, m);
-        if (lane >= m) s += __builtin_bit_cast(double, r);
-    }
-    u32x2 r = __builtin_bit_cast(u32x2, s);
-    r.x = __shfl_up((int)r.x, 1);
-    r.y = __shfl_up((int)r.y, 1);
-    __syncthreads();
-    if (lane == 63) of_wave[wave] = s;
-    __syncthreads();
-    double pre = 0;
-    all = 0;
-    for (int w = 0; w < kWaves; ++w) {
-        if (w == wave) pre = all;
-        all += of_wave[w];
-    }
-    return pre + (lane == 0 ? 0.0 : __builtin_bit_cast(double, r));
+    const u32x2 r = __builtin_bit_cast(u32x2, v);
+    return __builtin_bit_cast(double, u32x2{(unsigned)__builtin_amdgcn_update_dpp(0, (int)r.x, CTRL, ROWS, 0xF, false),
+                                            (unsigned)__builtin_amdgcn_update_dpp(0, (int)r.y, CTRL, ROWS, 0xF, false)});
 }
-
-// in a wave, the sum of a lane's value and all before it
 __device__ __forceinline__ double up_to(double v)
 {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) {
-        u32x2 r = __builtin_bit_cast(u32x2, v);
-        r.x = __shfl_up((int)r.x, m);
-        r.y = __shfl_up((int)r.y, m);
-        if (lane >= m) v += __builtin_bit_cast(double, r);
-    }
+    v += moved<0x111, 0xF>(v);                               // row_shr by 1, 2, 4, 8
+    v += moved<0x112, 0xF>(v);
+    v += moved<0x114, 0xF>(v);
+    v += moved<0x118, 0xF>(v);
+    v += moved<0x142, 0xA>(v);                               // row_bcast:15 to the second and fourth row
+    v += moved<0x143, 0xC>(v);                               // row_bcast:31 to the upper half
     return v;
+}
+__device__ __forceinline__ double from_lane(double v, int lane)
+{
+    const u32x2 r = __builtin_bit_cast(u32x2, v);
+    return __builtin_bit_cast(double, u32x2{(unsigned)__builtin_amdgcn_readlane((int)r.x, lane), (unsigned)__builtin_amdgcn_readlane((int)r.y, lane)});
+}
+
+// Of the threads' values v >= 0 in the threads' order, the first at which the running sum, begun at `base`, passes base + u * (their sum)
+// or, if it is given, `mark`: which thread, and the sum before it.  Where rounding or u >= 1 leaves none, the last v > 0; -1 where
+// there is none of those either.
+struct Spot { int thread; double before, mark; };
+__device__ __forceinline__ Spot spot_of(double v, double base, bool given, double mark, double u, double (*of_wave)[4])
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const double upto = up_to(v), last = from_lane(upto, 63);
+    if (lane == 0) of_wave[0][wave] = last;
+    __syncthreads();
+    double all = 0, pre = base;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        const double x = of_wave[0][w];
+        pre += w < wave ? x : 0;
+        all += x;
+    }
+    if (!given) mark = base + u * all;
+    const unsigned long long passed = __ballot(v > 0 && pre + upto > mark), some = __ballot(v > 0);
+    const int first = passed ? __builtin_ctzll(passed) : -1, end = some ? 63 - __builtin_clzll(some) : -1;
+    // per wave: the place, and what was before it
+    const int at = first >= 0 ? first : end;
+    const double before = pre + (at >= 0 ? from_lane(upto, at) - from_lane(v, at) : 0.0);
+    if (lane == 0) {
+        of_wave[1][wave] = first >= 0 ? 2 * 64 + first : end >= 0 ? 64 + end : 0;
+        of_wave[2][wave] = before;
+    }
+    __syncthreads();
+    Spot r{-1, 0, mark};
+    bool done = false;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        const int code = (int)of_wave[1][w];
+        if (!done && code >= 64) {                           // (a later wave's last one counts only where nobody has passed)
+            r.thread = w * 64 + (code & 63);
+            r.before = of_wave[2][w];
+        }
+        done = done || code >= 128;
+    }
+    return r;
 }
 
 template <bool BF16> __global__ __launch_bounds__(kThreads) void draft_pick_kernel(DraftKernelArgs a)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     constexpr int E = BF16 ? 8 : 4;
-    const int tid = threadIdx.x, lane = tid & 63, b = blockIdx.x;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, b = blockIdx.x, pieces = a.parts * kWaves, per_piece = a.per_part / kWaves;
+    __shared__ double of_wave[5][kWaves];
     const Verdict verdict = a.verdicts[b];
+    Sums s{0, 0, 0, 0};
     if (verdict.kind == kDone) return;
-    const int at = verdict.at, pieces = a.parts * kWaves, per_piece = a.per_part / kWaves;
-    __shared__ double of_wave[kWaves], start;
-    __shared__ int found, last, token;
-    const int drafts = drafts_of(a, b);
-    const bool down = at < drafts, minus = down && a.ld != nullptr;
-    const int without = down && a.ld == nullptr ? a.tokens[(size_t)b * a.n + at] : -1;
+    if (tid < pieces) s = a.sums[(size_t)b * pieces + tid];
+    const double u = __builtin_fmax((double)a.uniforms[(size_t)b * (a.n + 1) + a.n], 0.0);
+    const int at = verdict.at;
+    const bool minus = verdict.minus != 0;
     const size_t row_bytes = (size_t)a.vecs * 16;
     const uint8_t *const row_v = a.lv + ((size_t)b * a.nv + at) * row_bytes, *const row_d = minus ? a.ld + ((size_t)b * a.n + at) * row_bytes : row_v;
     const double c = verdict.c, at_p = -(double)verdict.ref_p * c, at_q = -(double)verdict.ref_q * c;
-    const double u = __builtin_fmax((double)a.uniforms[(size_t)b * (a.n + 1) + a.n], 0.0);
-    Sums s{0, 0, 0, 0};
-    if (tid < pieces) s = a.sums[(size_t)b * pieces + tid];
-    double all_p, all_q = 0;
-    (void)before(s.p, of_wave, all_p);
-    if (minus) (void)before(s.q, of_wave, all_q);
+    const double wave_p = wave_sum(s.p), wave_q = wave_sum(s.q);
+    if (lane == 0) {
+        of_wave[3][wave] = wave_p;
+        of_wave[4][wave] = wave_q;
+    }
+    __syncthreads();
+    double all_p = 0, all_q = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        all_p += of_wave[3][w];
+        all_q += of_wave[4][w];
+    }
     const double inv_p = all_p > 0 ? 1.0 / all_p : 0.0, inv_q = all_q > 0 ? 1.0 / all_q : 0.0;
+    int token = -1;
     // what is left of p without q; where p is nowhere above q, p itself
-    for (int left = 1; left >= 0; --left) {
-        const double mine = left ? s.above_p * inv_p - s.above_q * inv_q : s.p * inv_p;
-        double all;
-        const double pre = before(mine, of_wave, all), mark = u * all;
-        if (tid == 0) { found = pieces; last = -1; token = -1; }
-        __syncthreads();
-        if (mine > 0) {
-            if (pre + mine > mark) atomicMin(&found, tid);
-            atomicMax(&last, tid);
-        }
-        __syncthreads();
-        const int piece = found < pieces ? found : last;
-        if (tid == piece) start = pre;
-        __syncthreads();
-        if (piece < 0) continue;
+    for (int left = 1; left >= 0 && token < 0; --left) {
+        const Spot piece = spot_of(left ? s.above_p * inv_p - s.above_q * inv_q : s.p * inv_p, 0, false, 0, u, of_wave);
+        if (piece.thread < 0) continue;
         // ---- within the piece, neighbouring vectors per thread
-        const int begin = piece * per_piece, end = min(begin + per_piece, a.vecs), each = (end - begin + kThreads - 1) / kThreads;
+        const int begin = piece.thread * per_piece, end = min(begin + per_piece, a.vecs), each = (end - begin + kThreads - 1) / kThreads;
         auto weight = [&](float x, float y, int e) __attribute__((always_inline)) {
             double w = weight_of(x, c, at_p) * inv_p;
             if (left && minus) w = __builtin_fmax(w - weight_of(y, c, at_q) * inv_q, 0.0);
-            return left && e == without ? 0.0 : w;
+            return left && e == verdict.without ? 0.0 : w;
         };
         double sum = 0;
-        const int mine_from = begin + tid * each;
-        for (int v = mine_from; v < min(mine_from + each, end); ++v) {
+        const int mine = begin + tid * each;
+        for (int v = mine; v < min(mine + each, end); ++v) {
             float x[E], y[E];
             unpack<BF16>(reinterpret_cast<const u32x4 *>(row_v)[v], x);
             unpack<BF16>(reinterpret_cast<const u32x4 *>(row_d)[v], y);
 #pragma unroll
             for (int e = 0; e < E; ++e) sum += weight(x[e], y[e], v * E + e);
         }
-        double whole;
-        const double so_far = start + before(sum, of_wave, whole);
-        if (tid == 0) { found = kThreads; last = -1; }
-        __syncthreads();
-        if (sum > 0) {
-            if (so_far + sum > mark) atomicMin(&found, tid);
-            atomicMax(&last, tid);
-        }
-        __syncthreads();
-        const int who = found < kThreads ? found : last;
-        if (tid == who) start = so_far;
-        __syncthreads();
-        // ---- within that thread's vectors, an element per lane (of every wave the same)
-        if (who >= 0) {
-            const int from = (begin + who * each) * E, to = min(begin + (who + 1) * each, end) * E;
-            double done = start;
-            int hit = -1, fallback = -1;
-            for (int e0 = from; e0 < to && hit < 0; e0 += 64) {
-                const int e = e0 + lane;
-                const double w = e < to ? weight(logit<BF16>(row_v, e), logit<BF16>(row_d, e), e) : 0.0, upto = up_to(w);
-                const unsigned long long passed = __ballot(w > 0 && done + upto > mark), any = __ballot(w > 0);
-                if (passed) hit = e0 + __builtin_ctzll(passed);
-                if (any) fallback = e0 + 63 - __builtin_clzll(any);
-                done += __shfl(upto, 63);
+        __syncthreads();                                     // (`of_wave` has been read)
+        const Spot who = spot_of(sum, piece.before, true, piece.mark, 0, of_wave);
+        if (who.thread >= 0) {
+            // ---- within that thread's vectors, an element per lane, of every wave the same
+            const int from = (begin + who.thread * each) * E, to = min(begin + (who.thread + 1) * each, end) * E;
+            double done = who.before;
+            int last = -1;
+            for (int e0 = from; e0 < to && token < 0; e0 += 64) {
+                const int e = min(e0 + lane, to - 1);
+                const double w = e0 + lane < to ? weight(logit<BF16>(row_v, e), logit<BF16>(row_d, e), e) : 0.0, upto = up_to(w);
+                const unsigned long long passed = __ballot(w > 0 && done + upto > who.mark), some = __ballot(w > 0);
+                if (passed) token = e0 + __builtin_ctzll(passed);
+                if (some) last = e0 + 63 - __builtin_clzll(some);
+                done += from_lane(upto, 63);
             }
-            if (tid == 0) token = hit >= 0 ? hit : fallback;
+            if (token < 0) token = last;
         }
         __syncthreads();
-        if (token >= 0) break;
     }
     if (tid == 0) a.out_tokens[(size_t)b * (a.n + 1) + at] = token;      // (-1: no probability anywhere)
 #endif
