@@ -79,12 +79,14 @@ struct PagedTail {
     float scale_log2;                    // log2(e) / sqrt(d)
 };
 // The same of a call whose sequences share prefixes: a launch's first workgroups, `prefix_wgs`, have row tiles of whole groups and the
-// keys of their prefixes, the others those of a sequence and its own keys.  Every state goes to the workspace.
+// keys of their prefixes, the others those of a sequence and its own keys; every state goes to the workspace.  Or (`whole`, with no
+// workgroups of the first kind and no splits) a sequence's prefix and its own keys one after the other, and O is written.
 struct SharedTail : PagedTail {
     const int32_t *prefix_table, *prefix_lens, *group_starts;
     int groups, max_prefix_pages, B;
     unsigned prefix_wgs, own_wgs, prefix_tiles;              // row tiles of all groups at most
     int prefix_splits, slots, least;                         // splits of a prefix, of a row all together; least tiles of 64 keys of a split
+    bool whole;
 };
 #define DD_PAGED_HEAD const int32_t *table, const int32_t *kv_lens, const uint8_t *Kc, const uint8_t *Vc, int Hkv, int rows_total, int num_pages, \
                       int max_pages, unsigned launched, unsigned shape // launched: workgroups, kLongSplits; shape: row tiles, splits - 1 (6
@@ -96,6 +98,10 @@ struct Group { int index, first, members, tile; };
 __device__ __forceinline__ Group group_of(const int32_t *starts, int groups, int B, int rows, int tile_rows, int tile)
 {
     const int lane = threadIdx.x & 63;
+    if (groups == 1) {                               // (by scalar loads, beside others: a microsecond less)
+        const int lo = min(max(uniform_load(starts), 0), B), hi = min(max(uniform_load(starts + 1), lo), B);
+        return Group{0, lo, tile < ((hi - lo) * rows + tile_rows - 1) / tile_rows ? hi - lo : 0, tile};
+    }
     for (int g0 = 0; g0 < groups; g0 += 64) {
         const int g = g0 + lane;
         int lo = 0, hi = 0;
@@ -121,6 +127,18 @@ __device__ __forceinline__ Group group_of(const int32_t *starts, int groups, int
     }
     return Group{0, 0, 0, 0};
 }
+// the group that sequence b is in, -1: none
+__device__ __forceinline__ int group_with(const int32_t *starts, int groups, int b)
+{
+    const int lane = threadIdx.x & 63;
+    for (int g0 = 0; g0 < groups; g0 += 64) {
+        const int g = g0 + lane;
+        const unsigned long long in = __ballot(g < groups && starts[g < groups ? g : 0] <= b && b < starts[g < groups ? g + 1 : 0]);
+        if (in) return g0 + __builtin_ctzll(in);
+    }
+    return -1;
+}
+
 // How a sequence's tiles are shared out over the splits of a call: tiles per split and splits that have any.  The call's splits go by what
 // its table can hold, a sequence's by what it holds: with many rows and more workgroups than compute units (kLongSplits) only long ones
 // pay.  Workgroups that have none may not sit between the others (26.0 us where the first figure below is 20.8), so this is for calls whose
@@ -198,6 +216,9 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(DD_PAGED_HEAD, Tail 
     int rt, sp, first_seq = 0, row_count = rows_total;       // (SHARED) of the rows, the first sequence; rows of all of them
     unsigned b = 0, g;
     const int32_t *row_of_table, *held_at;
+    // (SHARED, whole) the prefix before a sequence's own keys: its tiles, positions and pages
+    int before = 0, prefix_len = 0;
+    const int32_t *prefix_row = nullptr;
     if constexpr (SHARED) {
         const unsigned xcd = bid & 7;                        // workgroups that share keys: on one XCD, of either kind
         const bool prefix = bid < a.prefix_wgs;
@@ -225,6 +246,14 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(DD_PAGED_HEAD, Tail 
             g = bid - (unsigned)first_seq * (unsigned)Hkv;
             row_of_table = table + (size_t)first_seq * max_pages;
             held_at = kv_lens + first_seq;
+            if (a.whole) {
+                const int group = group_with(a.group_starts, a.groups, first_seq);
+                if (group >= 0) {
+                    prefix_row = a.prefix_table + (size_t)group * a.max_prefix_pages;
+                    prefix_len = min(max(uniform_load(a.prefix_lens + group), 0), a.max_prefix_pages << P_log2);
+                    before = (int)(((unsigned)prefix_len + 63u) >> 6) * (2 / NT);
+                }
+            }
         }
     } else {
         {                                                    // workgroups that share keys: on one XCD
@@ -247,10 +276,17 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(DD_PAGED_HEAD, Tail 
     const unsigned in_page = (1u << P_log2) - 1;
     constexpr int IDS = ONE ? 1 : UNITS;             // pages: of the tile, or of each unit of 16 keys
     struct Pages { int id[IDS]; };
+    auto own_tile = [&](int tile) __attribute__((always_inline)) { return SHARED && tile >= before ? tile - before : tile; };   // of its part of the keys
     auto pages_of = [&](int tile) __attribute__((always_inline)) {
         Pages p;
+        const int32_t *row = row_of_table;
+        int last = max_pages - 1;
+        if constexpr (SHARED) {
+            if (tile < before) { row = prefix_row; last = a.max_prefix_pages - 1; }
+            tile = own_tile(tile);
+        }
 #pragma unroll
-        for (int u = 0; u < IDS; ++u) p.id[u] = uniform_load(row_of_table + min((tile * TILE + 16 * u) >> P_log2, max_pages - 1));
+        for (int u = 0; u < IDS; ++u) p.id[u] = uniform_load(row + min((tile * TILE + 16 * u) >> P_log2, last));
         return p;
     };
     const int held = uniform_load(held_at);
@@ -263,7 +299,8 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(DD_PAGED_HEAD, Tail 
     Share sh;
     if constexpr (SHARED) {
         sh = shared_share_of(held, max_pages, P_log2, splits, a.least);
-        if (sp >= sh.used) return;
+        if (a.whole) sh.per_split = before / (2 / NT) + sh.tiles;
+        else if (sp >= sh.used) return;
     } else {
         sh = share_of(held, max_pages, P_log2, splits, rows_total, launched);
         if (sp >= sh.used && sp > 0) return;
@@ -279,7 +316,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(DD_PAGED_HEAD, Tail 
             return row_base + r;
         }
     };
-    const int t_begin = sp * sh.per_split * (2 / NT), t_end = min(t_begin + sh.per_split * (2 / NT), (sh.len + TILE - 1) / TILE);
+    const int t_begin = sp * sh.per_split * (2 / NT), t_end = min(t_begin + sh.per_split * (2 / NT), before + (sh.len + TILE - 1) / TILE);
     const int mine = t_begin + stream;
     if (splits > 1) {
         now = pages_of(mine);
@@ -297,7 +334,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(DD_PAGED_HEAD, Tail 
     }
 
     // every stream takes as many tiles; those behind the split's last key are masked whole
-    const int rounds = (t_end - t_begin + STREAMS - 1) / STREAMS, key_end = min(sh.len, t_end * TILE);
+    const int rounds = (t_end - t_begin + STREAMS - 1) / STREAMS, last_key = min(sh.len, t_end * TILE);
     auto valid = [&](int id) __attribute__((always_inline)) { return (unsigned)id < (unsigned)num_pages; };
     auto place = [&](int id) __attribute__((always_inline)) { return (size_t)((valid(id) ? id : 0) * (long)Hkv + g); };      // page and head
 
@@ -314,7 +351,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(DD_PAGED_HEAD, Tail 
     auto k_from = [&](const Pages &p, int tile) __attribute__((always_inline)) {
         KFrom f;
 #pragma unroll
-        for (int u = 0; u < IDS; ++u) f.base[u] = Kc + ((place(p.id[u]) << P_log2) + ((unsigned)(tile * TILE + 16 * u) & in_page)) * ROWB;
+        for (int u = 0; u < IDS; ++u) f.base[u] = Kc + ((place(p.id[u]) << P_log2) + ((unsigned)(own_tile(tile) * TILE + 16 * u) & in_page)) * ROWB;
         return f;
     };
     auto put_k = [&](const KFrom &f, unsigned buf, int i) __attribute__((always_inline)) {
@@ -331,13 +368,13 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(DD_PAGED_HEAD, Tail 
     const int v_begin = RG == 1 ? 0 : block * (NV / RG);
     auto v_from = [&](const Pages &p, int tile) __attribute__((always_inline)) {         // the tile's, or the lane's, first address
         if constexpr (ONE) {
-            return Vc + (((place(p.id[0]) * D) << P_log2) + ((unsigned)(tile * TILE) & in_page)) * EB + v_begin * v_step;
+            return Vc + (((place(p.id[0]) * D) << P_log2) + ((unsigned)(own_tile(tile) * TILE) & in_page)) * EB + v_begin * v_step;
         } else {
             // the page of the lane's piece, by the bits of its unit (not by an index, which would put the pages into memory)
             const unsigned u = EB == 1 ? v_piece : v_piece >> 1, m0 = 0u - (u & 1), m1 = 0u - (u >> 1);
             unsigned id = ((unsigned)p.id[0] & ~m0) | ((unsigned)p.id[1] & m0);
             if constexpr (IDS == 4) id = (id & ~m1) | ((((unsigned)p.id[2] & ~m0) | ((unsigned)p.id[3] & m0)) & m1);
-            return Vc + (((place((int)id) * D) << P_log2) + ((unsigned)(tile * TILE + 16 * u) & in_page)) * EB + (v_off - 16 * u * EB) + v_begin * v_step;
+            return Vc + (((place((int)id) * D) << P_log2) + ((unsigned)(own_tile(tile) * TILE + 16 * u) & in_page)) * EB + (v_off - 16 * u * EB) + v_begin * v_step;
         }
     };
     auto put_v = [&](const uint8_t *from, unsigned buf, int i) __attribute__((always_inline)) {
@@ -411,6 +448,11 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(DD_PAGED_HEAD, Tail 
     };
     auto factors_of = [&](const Pages &p, const Scales &x, int t) __attribute__((always_inline)) {
         Factors f;
+        int key_end = last_key;
+        if constexpr (SHARED) {                      // (a tile behind the split's last has no key)
+            key_end = t >= t_end ? 0 : t < before ? prefix_len : sh.len;
+            t = own_tile(t);
+        }
         f.whole = t * TILE + TILE <= key_end;
 #pragma unroll
         for (int u = 0; u < IDS; ++u) f.whole = f.whole && valid(p.id[u]);
@@ -701,19 +743,23 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(DD_PAGED_HEAD, Tail 
         if (rounds > 0) round(std::integral_constant<int, 0>{}, rounds - 1, false);
     }
     l += halves_other(l);
+    bool whole_rows = false;                         // (SHARED) O is written
+    if constexpr (SHARED) whole_rows = a.whole;
 
     if constexpr (STREAMS == 1) {                    // a row is in one wave, four head dims of it at a time (and its keys are not split)
         if (v_first + l32 >= row_count) return;
         const size_t row = row_at(v_first + l32);
-        if constexpr (SHARED) {
-            const size_t state = row * a.slots + (blockIdx.x < a.prefix_wgs ? 0 : a.prefix_splits) + sp;
+        if (SHARED && !whole_rows) {
+            if constexpr (SHARED) {
+                const size_t state = row * a.slots + (blockIdx.x < a.prefix_wgs ? 0 : a.prefix_splits) + sp;
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt)
+                for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    *reinterpret_cast<float4 *>(a.part_o + state * D + dt * 32 + 8 * i + 4 * hh) =
-                        make_float4(o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]);
-            if (hh == 0) *reinterpret_cast<float2 *>(a.part_ml + state * 2) = make_float2(m, l);
+                    for (int i = 0; i < 4; ++i)
+                        *reinterpret_cast<float4 *>(a.part_o + state * D + dt * 32 + 8 * i + 4 * hh) =
+                            make_float4(o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]);
+                if (hh == 0) *reinterpret_cast<float2 *>(a.part_ml + state * 2) = make_float2(m, l);
+            }
             return;
         }
         const float inv = l > 0 ? 1.0f / l : 0.0f;   // no key at all: zeros
@@ -760,23 +806,19 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(DD_PAGED_HEAD, Tail 
                 x[4] += f * hi.x; x[5] += f * hi.y; x[6] += f * hi.z; x[7] += f * hi.w;
             }
             const size_t row = row_at(v);
-            if constexpr (SHARED) {
-                const size_t state = row * a.slots + (blockIdx.x < a.prefix_wgs ? 0 : a.prefix_splits) + sp;
-                float *to = a.part_o + state * D + d0;
-                *reinterpret_cast<float4 *>(to) = make_float4(x[0], x[1], x[2], x[3]);
-                *reinterpret_cast<float4 *>(to + 4) = make_float4(x[4], x[5], x[6], x[7]);
-                if (d0 == 0) *reinterpret_cast<float2 *>(a.part_ml + state * 2) = make_float2(M, L);
-            } else if (sh.used <= 1) {
+            if (SHARED ? whole_rows : sh.used <= 1) {
                 const float inv = L > 0 ? 1.0f / L : 0.0f;
                 *reinterpret_cast<uint4 *>(a.O + (row * D + d0) * 2) = make_uint4(pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv),
                                                                                  pack_bf16(x[4] * inv, x[5] * inv), pack_bf16(x[6] * inv, x[7] * inv));
             } else {
-                float *to = a.part_o + (row * splits + sp) * D + d0;
+                size_t state = row * splits + sp;
+                if constexpr (SHARED) state = row * a.slots + (blockIdx.x < a.prefix_wgs ? 0 : a.prefix_splits) + sp;
+                float *to = a.part_o + state * D + d0;
                 *reinterpret_cast<float4 *>(to) = make_float4(x[0], x[1], x[2], x[3]);
                 *reinterpret_cast<float4 *>(to + 4) = make_float4(x[4], x[5], x[6], x[7]);
                 if (d0 == 0) {
-                    a.part_ml[(row * splits + sp) * 2] = M;
-                    a.part_ml[(row * splits + sp) * 2 + 1] = L;
+                    a.part_ml[state * 2] = M;
+                    a.part_ml[state * 2 + 1] = L;
                 }
             }
         }

@@ -9,16 +9,30 @@
 namespace dd {
 namespace {
 
-// Every state of a row, merged by D / 4 lanes: the prefix's splits, then those of the own keys.
-template <int D>
+// Every state of a row, merged by D / 4 lanes: the prefix's splits, then those of the own keys.  PARTS such lots of lanes have a quarter of
+// the states each where there are many.  All that a row can have are asked for before it is known how many it has.
+template <int D, int PARTS>
 __global__ __launch_bounds__(256) void shared_merge_kernel(const float *part_ml, const float *part_o, const int32_t *kv_lens, uint8_t *O, int Hkv, int rows_total, int rows,
-                                                           int max_pages, int page_log2, int own_splits, int own_least, int prefix_least, SharedTail a)
+                                                           int max_pages, int page_log2, int own_splits, SharedTail a)
 {
-    constexpr int LANES = D / 4;
-    const int row = blockIdx.x * (256 / LANES) + threadIdx.x / LANES, d0 = (threadIdx.x % LANES) * 4;
-    if (row >= rows) return;
+    constexpr int LANES = D / 4, U = 8, ROWS = 256 / LANES / PARTS;
+    const int lot = threadIdx.x / LANES, part = lot % PARTS, mine = lot / PARTS, d0 = (threadIdx.x % LANES) * 4;
+    const int row = min((int)blockIdx.x * ROWS + mine, rows - 1);
+    const float2 *ml = reinterpret_cast<const float2 *>(part_ml) + (size_t)row * a.slots;
+    const floatx4 *po = reinterpret_cast<const floatx4 *>(part_o + (size_t)row * a.slots * D + d0);
+    float2 st[U];
+    floatx4 v[U];
+    auto fetch = [&](int s0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int s = min(s0 + u * PARTS, a.slots - 1);
+            st[u] = ml[s];
+            v[u] = po[(size_t)s * (D / 4)];
+        }
+    };
+    fetch(part);
     const int b = (int)((unsigned)row / (unsigned)rows_total / (unsigned)Hkv);
-    const int own = shared_share_of(kv_lens[b], max_pages, page_log2, own_splits, own_least).used;
+    const int own = shared_share_of(kv_lens[b], max_pages, page_log2, own_splits, a.least).used;
     int lo = 0, hi = a.groups;                       // the last group that begins at b or before
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
@@ -26,45 +40,61 @@ __global__ __launch_bounds__(256) void shared_merge_kernel(const float *part_ml,
         else hi = mid;
     }
     const bool member = a.group_starts[lo] <= b && b < a.group_starts[lo + 1];
-    const int shared = member ? shared_share_of(a.prefix_lens[lo], a.max_prefix_pages, page_log2, a.prefix_splits, prefix_least).used : 0;
-    const float2 *ml = reinterpret_cast<const float2 *>(part_ml) + (size_t)row * a.slots;
-    const floatx4 *po = reinterpret_cast<const floatx4 *>(part_o + (size_t)row * a.slots * D + d0);
-    const int count = shared + own;
-    constexpr int U = 8;                             // states on their way
+    const int shared = shared_share_of(member ? a.prefix_lens[lo] : 0, a.max_prefix_pages, page_log2, a.prefix_splits, a.least).used;
+    auto counts = [&](int s) __attribute__((always_inline)) { return s < shared || (s >= a.prefix_splits && s < a.prefix_splits + own); };
     float M = kNone, L = 0;
     floatx4 x = {0, 0, 0, 0};
-    for (int s0 = 0; s0 < count; s0 += U) {
-        float2 st[U];
-        floatx4 v[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int k = min(s0 + u, count - 1), s = k < shared ? k : a.prefix_splits + k - shared;
-            st[u] = ml[s];
-            v[u] = po[(size_t)s * (D / 4)];
-        }
+    for (int s0 = part;;) {
         float top = M;
 #pragma unroll
-        for (int u = 0; u < U; ++u) top = fmaxf(top, s0 + u < count ? st[u].x : M);
+        for (int u = 0; u < U; ++u) top = fmaxf(top, counts(s0 + u * PARTS) ? st[u].x : M);
         const float by = __builtin_amdgcn_exp2f(M - top);
         M = top;
         L *= by;
         x *= by;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (s0 + u < count) {
+            if (counts(s0 + u * PARTS)) {
                 const float f = __builtin_amdgcn_exp2f(st[u].x - M);
                 L += f * st[u].y;
                 x += f * v[u];
             }
         }
+        s0 += U * PARTS;
+        if (s0 >= a.slots) break;
+        fetch(s0);
     }
+    if constexpr (PARTS > 1) {
+        __shared__ float2 ml_of[256 / LANES];
+        __shared__ floatx4 x_of[256];
+        if (threadIdx.x % LANES == 0) ml_of[lot] = make_float2(M, L);
+        x_of[threadIdx.x] = x;
+        __syncthreads();
+        if (part != 0) return;
+        float2 all[PARTS];
+        float top = kNone;
+#pragma unroll
+        for (int k = 0; k < PARTS; ++k) {
+            all[k] = ml_of[lot + k];
+            top = fmaxf(top, all[k].x);
+        }
+        L = 0;
+        x = floatx4{0, 0, 0, 0};
+#pragma unroll
+        for (int k = 0; k < PARTS; ++k) {
+            const float f = __builtin_amdgcn_exp2f(all[k].x - top);
+            L += f * all[k].y;
+            x += f * x_of[threadIdx.x + k * LANES];
+        }
+    }
+    if ((int)blockIdx.x * ROWS + mine >= rows) return;
     const float inv = L > 0 ? 1.0f / L : 0.0f;       // no key at all: zeros
     *reinterpret_cast<uint2 *>(O + ((size_t)row * D + d0) * 2) = make_uint2(pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv));
 }
 
-// One kind of workgroup: 32-row blocks each takes, splits of the keys, least tiles of 64 keys of a split, row tiles, workgroups.
-struct Kind { int rg, splits, least; long row_tiles, wgs; };
-struct Plan { Kind prefix, own; int slots; };
+// One kind of workgroup: 32-row blocks each takes, splits of the keys, row tiles, workgroups.
+struct Kind { int rg, splits; long row_tiles, wgs; };
+struct Plan { Kind prefix, own; int slots; bool whole; };
 Plan plan_of(const SharedAttnShape &s)
 {
     const long rows = (long)(s.H / s.Hkv) * s.n, all = rows * s.B;
@@ -79,16 +109,23 @@ Plan plan_of(const SharedAttnShape &s)
     p.own.rg = group_rows(s.B * (long)s.Hkv * blocks_of(rows), rows <= kFewRows, is_full(rows));
     p.own.row_tiles = (rows + 32 * p.own.rg - 1) / (32 * p.own.rg);
     const long own_base = (long)s.B * s.Hkv * p.own.row_tiles;
-    p.own.least = kSplitTiles;
-    p.own.splits = splits_of(kUnits, own_base, ((long)s.max_pages << s.page_log2) / 64, p.own.least);
+    p.own.splits = splits_of(kUnits, own_base, ((long)s.max_pages << s.page_log2) / 64, kSplitTiles);
     p.own.wgs = own_base * p.own.splits;
     p.prefix.rg = group_rows((long)s.Hkv * blocks_of(all), all <= kFewRows, is_full(all));
     p.prefix.row_tiles = all / (32 * p.prefix.rg) + s.G;      // (every group may end within a tile)
     if (s.G == 1) p.prefix.row_tiles = (all + 32 * p.prefix.rg - 1) / (32 * p.prefix.rg);
     const long base = (long)s.Hkv * p.prefix.row_tiles;
-    p.prefix.least = kSplitTiles;
-    p.prefix.splits = splits_of(2 * kUnits, base, ((long)s.max_prefix_pages << s.page_log2) / 64, p.prefix.least);
+    p.prefix.splits = splits_of(2 * kUnits, base, ((long)s.max_prefix_pages << s.page_log2) / 64, kSplitTiles);
     p.prefix.wgs = base * p.prefix.splits;
+    // Where a sequence's own rows fill row blocks and there are enough of those for the card, nothing is gained by meeting the prefix
+    // together: arithmetic bounds the call either way, and without states there is nothing to merge.
+    p.whole = (rows + 31) / 32 * 32 * 4 <= rows * 5 && own_base >= kUnits;
+    if (p.whole) {
+        p.own.splits = 1;
+        p.own.wgs = own_base;
+        p.prefix.splits = 0;
+        p.prefix.wgs = 0;
+    }
     p.slots = p.prefix.splits + p.own.splits;
     return p;
 }
@@ -122,7 +159,8 @@ bool shared_attention_fits(const SharedAttnShape &s)
 
 size_t shared_attention_workspace_bytes(const SharedAttnShape &s)
 {
-    return (size_t)s.B * s.H * s.n * (size_t)plan_of(s).slots * (size_t)(s.d + 2) * sizeof(float);
+    const Plan p = plan_of(s);
+    return p.whole ? 0 : (size_t)s.B * s.H * s.n * (size_t)p.slots * (size_t)(s.d + 2) * sizeof(float);
 }
 
 hipError_t launch_attention_shared(const SharedAttnArgs &a, hipStream_t stream)
@@ -136,28 +174,31 @@ hipError_t launch_attention_shared(const SharedAttnArgs &a, hipStream_t stream)
     tail.prefix_table = a.prefix_table; tail.prefix_lens = a.prefix_lens; tail.group_starts = a.group_starts;
     tail.groups = s.G; tail.max_prefix_pages = s.max_prefix_pages; tail.B = s.B;
     tail.prefix_tiles = (unsigned)p.prefix.row_tiles; tail.prefix_splits = p.prefix.splits; tail.slots = p.slots;
+    tail.least = kSplitTiles; tail.whole = p.whole;
     const unsigned shape = (unsigned)p.own.row_tiles << 8 | (unsigned)(p.own.splits - 1) << 2 | (unsigned)(s.page_log2 - 4);
-    auto part = [&](int rg, long prefix_wgs, long own_wgs, int least) {
-        tail.prefix_wgs = eights(prefix_wgs); tail.own_wgs = (unsigned)own_wgs; tail.least = least;
+    auto part = [&](int rg, long prefix_wgs, long own_wgs) {
+        tail.prefix_wgs = eights(prefix_wgs); tail.own_wgs = (unsigned)own_wgs;
         const unsigned grid = tail.prefix_wgs + eights(own_wgs);
         return s.d == 128 ? (s.fp8 ? attend<128, true>(a, tail, rg, grid, (unsigned)prefix_wgs, shape, stream) : attend<128, false>(a, tail, rg, grid, (unsigned)prefix_wgs, shape, stream))
                           : (s.fp8 ? attend<64, true>(a, tail, rg, grid, (unsigned)prefix_wgs, shape, stream) : attend<64, false>(a, tail, rg, grid, (unsigned)prefix_wgs, shape, stream));
     };
     hipError_t e;
-    if (p.prefix.rg == p.own.rg && p.prefix.least == p.own.least) {
-        e = part(p.own.rg, p.prefix.wgs, p.own.wgs, p.own.least);
+    if (p.whole || p.prefix.rg == p.own.rg) {
+        e = part(p.own.rg, p.prefix.wgs, p.own.wgs);
     } else {
-        e = part(p.prefix.rg, p.prefix.wgs, 0, p.prefix.least);
-        if (e == hipSuccess) e = part(p.own.rg, 0, p.own.wgs, p.own.least);
+        e = part(p.prefix.rg, p.prefix.wgs, 0);
+        if (e == hipSuccess) e = part(p.own.rg, 0, p.own.wgs);
     }
-    if (e != hipSuccess) return e;
-    const unsigned per_wg = 256 / (s.d / 4);
+    if (e != hipSuccess || p.whole) return e;
+    const int parts = p.slots > 12 ? 4 : 1;
+    const unsigned per_wg = 256 / (s.d / 4) / parts;
     const dim3 grid((unsigned)((rows + per_wg - 1) / per_wg));
     auto merge = [&](auto kernel) {
         return launch(kernel, grid, dim3(256), stream, tail.part_ml, tail.part_o, a.kv_lens, tail.O, s.Hkv, (s.H / s.Hkv) * s.n, (int)rows, s.max_pages, s.page_log2,
-                      p.own.splits, p.own.least, p.prefix.least, tail);
+                      p.own.splits, tail);
     };
-    return s.d == 128 ? merge(shared_merge_kernel<128>) : merge(shared_merge_kernel<64>);
+    return s.d == 128 ? (parts == 4 ? merge(shared_merge_kernel<128, 4>) : merge(shared_merge_kernel<128, 1>))
+                      : (parts == 4 ? merge(shared_merge_kernel<64, 4>) : merge(shared_merge_kernel<64, 1>));
 }
 
 }  // namespace dd

@@ -538,7 +538,7 @@ Plan plan_of(int B, int n, int nv, int V, bool bf16, bool drafter)
         per = (int)(v < 0x7fffff00 ? v : 0x7fffff00);
         count = (int)(((long)p.vecs + per - 1) / per);
     };
-    divide(rows, 8192, kMostSplits, p.per_split, p.splits);
+    divide(rows, 2048, kMostSplits, p.per_split, p.splits);
     divide(B, 1024, kMostParts, p.per_part, p.parts);
     p.states = ((size_t)rows * p.splits * sizeof(State) + 255) / 256 * 256;
     p.sums = ((size_t)B * p.parts * kWaves * sizeof(Sums) + 255) / 256 * 256;
