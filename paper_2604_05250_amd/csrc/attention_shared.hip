@@ -92,6 +92,7 @@ __global__ __launch_bounds__(256) void shared_merge_kernel(const float *part_ml,
     *reinterpret_cast<uint2 *>(O + ((size_t)row * D + d0) * 2) = make_uint2(pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv));
 }
 
+constexpr int kLongSplitTiles = 32;          // tiles of 64 keys of a long split
 // One kind of workgroup: 32-row blocks each takes, splits of the keys, row tiles, workgroups.
 struct Kind { int rg, splits; long row_tiles, wgs; };
 struct Plan { Kind prefix, own; int slots; bool whole; };
@@ -102,7 +103,8 @@ Plan plan_of(const SharedAttnShape &s)
     auto group_rows = [&](long blocks, bool few, bool full) { return few || blocks <= (s.fp8 ? 512 : 256) ? 1 : full && blocks > (s.fp8 ? 1792 : 1024) ? 4 : 2; };
     auto is_full = [](long r) { return (r + 127) / 128 * 128 * 8 <= r * 9; };
     auto splits_of = [](long room, long base, long tiles, int least) {
-        long n = room / base < tiles / least ? room / base : tiles / least;
+        const long most = (tiles + least - 1) / least;       // (a tile for each wave; the last split may have less)
+        const long n = room / base < most ? room / base : most;
         return (int)(n < 1 ? 1 : n > kMaxSplits ? kMaxSplits : n);
     };
     Plan p;
@@ -115,11 +117,33 @@ Plan plan_of(const SharedAttnShape &s)
     p.prefix.row_tiles = all / (32 * p.prefix.rg) + s.G;      // (every group may end within a tile)
     if (s.G == 1) p.prefix.row_tiles = (all + 32 * p.prefix.rg - 1) / (32 * p.prefix.rg);
     const long base = (long)s.Hkv * p.prefix.row_tiles;
-    p.prefix.splits = splits_of(2 * kUnits, base, ((long)s.max_prefix_pages << s.page_log2) / 64, kSplitTiles);
+    // Splits of the prefix: as many workgroups as run at once, but for the room that the own keys' ones take where splits are short and a
+    // second round of workgroups costs (one token of 32 sequences over 4000 e4m3 keys and 64 of their own 23.4 -> 16.6 us, of 64 over 8192
+    // and 256 30.2 -> 25.3; of 64 over 32768 61.4 without, 62.8 with).
+    const long prefix_tiles = ((long)s.max_prefix_pages << s.page_log2) / 64;
+    long room = 2 * kUnits;
+    if (prefix_tiles < room / base * kLongSplitTiles) room = room - p.own.wgs > kUnits ? room - p.own.wgs : kUnits;
+    p.prefix.splits = splits_of(room, base, prefix_tiles, kSplitTiles);
     p.prefix.wgs = base * p.prefix.splits;
-    // Where a sequence's own rows fill row blocks and there are enough of those for the card, nothing is gained by meeting the prefix
-    // together: arithmetic bounds the call either way, and without states there is nothing to merge.
-    p.whole = (rows + 31) / 32 * 32 * 4 <= rows * 5 && own_base >= kUnits;
+    // Sequence by sequence, prefix and own keys in one go and nothing to merge, or the prefix together?  What either has to do is row blocks
+    // times keys; the first has more blocks where a sequence's rows fill less than one, and they are as long as all keys.  us, sequence by
+    // sequence / together, 32/8 heads, by sequences x rows and keys (64 of them a sequence's own):
+    //     e4m3    4 x 1     512   7.2 / 10.7    1024   9.8 / 10.3    2048  16.3 / 12.3       16 x 8   1280  13.6 / 19.5    2964  23.4 / 23.5
+    //            16 x 1     512   7.4 / 11.3    1024  11.0 / 11.7    1280  12.6 / 11.6        4 x 64  1024  12.0 / 26.1    4064  29.6 / 37.8
+    //            64 x 1    1024  15.0 / 18.4    1280  16.8 / 21.2    2048  23.3 / 21.0        4 x 64 16064  97.0 / 90.3
+    //             8 x 8    1280  13.3 / 15.6    2048  17.6 / 19.5    2964  23.3 / 19.7       16 x 64  1024  26.4 / 49.5    4064  78.4 / 96.8
+    //     bf16    4 x 1     512   8.3 / 11.2     768  11.0 / 11.3    1024  12.8 / 11.2       16 x 8   1280  16.1 / 19.7    2964  29.0 / 25.3
+    //            64 x 1     768  16.0 / 18.4    1024  19.1 / 19.6    1280  22.4 / 19.4        4 x 64  4064  36.5 / 42.9   16064 125.8 / 120
+    //             8 x 8     768  12.3 / 13.2    1280  16.0 / 16.7    2048  21.3 / 19.4       16 x 64  1024  29.6 / 49.8    4064  90.0 / 106
+    // So up to a length that grows with the row blocks that there are in all; where compute units have two workgroups or more, less of
+    // it, unless the blocks are full.
+    const long together = s.Hkv * blocks_of(all), apart = s.B * (long)s.Hkv * blocks_of(rows), keys = ((long)s.max_prefix_pages + s.max_pages) << s.page_log2;
+    const long least = s.fp8 ? 1024 : 768, grown = (s.fp8 ? 28 : 20) * together, most = least > grown ? least : grown;
+    const bool full = apart * 4 <= together * 5;
+    p.whole = full && together >= 2 * kUnits ? true
+            : keys <= (full || apart <= kUnits ? most : apart <= 2 * kUnits ? most * 3 / 4 : most * 3 * kUnits / (2 * apart));
+    const int hook = tune("DD_TUNE_SHARED_WHOLE", -1);
+    if (hook >= 0) p.whole = hook != 0;
     if (p.whole) {
         p.own.splits = 1;
         p.own.wgs = own_base;

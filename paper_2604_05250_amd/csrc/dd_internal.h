@@ -46,6 +46,7 @@ inline hipError_t launch(void (*kernel)(Params...), dim3 grid, dim3 block, hipSt
 //   DD_TUNE_BLOCK_SPLITS=n     key splits of a drafter call on the streaming / MFMA kernels (still at least 128 keys each)
 //   DD_TUNE_BLOCK_WIDE_ROWS=128/256   query rows per workgroup of such a call
 //   DD_TUNE_BLOCK_WIDE_MIN_ROWS=n     query rows per kv head from which it takes that kernel
+//   DD_TUNE_SHARED_WHOLE=0/1   attention over shared prefixes: the prefix together / sequence by sequence
 // Returns the variable's integer value, or `dflt` when hooks are off or the variable is unset.
 int tune(const char *name, int dflt);
 
