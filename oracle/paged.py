@@ -182,6 +182,6 @@ def paged_resize(table, free_pages, num_free, lens, new_lens, page_size, n):
         out.append(w)
         positions.append([a + r for r in range(n)])
         at = [row[p // page_size] if p < w else -1 for p in positions[-1]]
-        slots.append([page * page_size + p % page_size if page >= 0 else -1 for page, p in zip(at, positions[-1])])
+        slots.append([page * page_size + p % page_size if 0 <= page < len(stack) else -1 for page, p in zip(at, positions[-1])])
     as_ints = lambda x: np.array(x, np.int64)
     return as_ints(table), as_ints(stack), len(free), as_ints(out), as_ints(positions).reshape(len(lens), n), as_ints(slots).reshape(len(lens), n)

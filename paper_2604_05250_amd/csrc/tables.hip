@@ -65,7 +65,7 @@ __device__ __forceinline__ void place_row(const TableKernelArgs &a, int b, int r
     int slot = -1;
     if (p < out) {
         const int j = p >> a.page_log2, page = j < have ? a.table[(size_t)b * a.max_pages + j] : a.stack[top - 1 - (first + j - have)];
-        slot = page < 0 || page >= (0x7fffffff >> a.page_log2) ? -1 : (page << a.page_log2) + (p & ((1 << a.page_log2) - 1));
+        slot = (unsigned)page < (unsigned)a.capacity ? (page << a.page_log2) + (p & ((1 << a.page_log2) - 1)) : -1;
     }
     a.slots[at] = slot;
 }

@@ -151,3 +151,11 @@ def test_graph_replays_match_eager_calls():
             graph.replay()
             torch.cuda.synchronize()
             assert all(torch.equal(x, y) for x, y in zip(want, (*state, positions, slots))), f"B {B} replay {rep}"
+
+
+def test_pages_that_are_none_have_no_slots():
+    table, stack = np.array([[3, 50, -7, -1]], np.int32), np.array([49, 2 ** 31 - 1] + [-9] * 48, np.int32)
+    _, _, _, got = _check(table, stack, 2, [40], [64], 16, 24)          # (page 50 of 50, -7, and one taken that is none)
+    assert (got[2].cpu().numpy()[0] == -1).all()
+    _, _, _, got = _check(table, stack, 1, [40], [64], 16, 24)
+    assert (got[2].cpu().numpy()[0, 8:24] == 49 * 16 + np.arange(16)).all()

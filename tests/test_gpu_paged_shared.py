@@ -263,3 +263,26 @@ def test_two_kinds_of_workgroups_in_two_launches(cache, way):
     rng = np.random.default_rng(2)
     for B, H in ((180, 96), (100, 256)):
         _check([0, B // 3, B], H, H // 2, 1, 64, 32, cache, [70, 33], rng.integers(0, 40, B).tolist(), poison=True)
+
+
+@pytest.mark.parametrize("cache", ["fp8", "bf16"])
+def test_offsets_past_32_bits(cache, way):
+    # the pages of a small cache, scattered over one of more than 4 GB
+    import torch
+    args, _ = _case([0, 3, 5], 8, 8, 2, 128, 128, cache, [700, 150], [20, 130, 3, 90, 1])
+    pages = args["Kc"].shape[0]
+    many = 5 * (1 << 30) // (8 * 128 * 128 * args["Kc"].element_size())
+    to = torch.linspace(0, many - 1, pages, device="cuda").long().flip(0)
+    big = dict(args)
+    for name in ("Kc", "Vc"):
+        small = args[name].view(torch.uint8)
+        wide = torch.empty((many,) + tuple(small.shape[1:]), dtype=torch.uint8, device="cuda")
+        wide[to] = small
+        big[name] = wide.view(args[name].dtype)
+    for name in ("k_scale", "v_scale"):
+        if args[name] is not None:
+            big[name] = torch.full((many, 8), float("nan"), device="cuda")
+            big[name][to] = args[name]
+    for name in ("prefix_table", "block_table"):
+        big[name] = to[args[name].long()].int()
+    assert torch.equal(dd.dd_paged_attention_shared(**args), dd.dd_paged_attention_shared(**big))

@@ -232,3 +232,19 @@ def test_streams_side_by_side():
                 to.append(dd.dd_verify_draft(**c))
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for w, gs in zip(want, got) for g in gs for a, b in zip(w, g))
+
+
+def test_offsets_past_32_bits():
+    # rows of 2^27 fp32 logits, nine of them: a spike that stands, one that falls, and flat rows, where token floor(u V) is drawn
+    import torch
+    V, B, n = 1 << 27, 3, 2
+    lv, ld = torch.zeros((B, n + 1, V), device="cuda"), torch.zeros((B, n, V), device="cuda")
+    x = np.array([[V - 1, 5], [V - 2, 7], [V - 3, 9]], np.int32)
+    for b in range(B):
+        ld[b, 0, int(x[b, 0])] = lv[b, 0, int(x[b, 0])] = 60.0           # as likely with either: stands
+    lv[1, 1, V - 9], ld[1, 1, 7] = 60.0, 60.0                            # the drafter's favourite has no chance
+    k = [(1 << 24) - 1, 77, (1 << 24) - 5]
+    u = np.array([[0.5, 0.5, k[0] / 2 ** 24], [0.5, 0.5, k[1] / 2 ** 24], [0.5, 0.5, k[2] / 2 ** 24]], np.float32)
+    out, accepted, _ = dd.dd_verify_draft(lv, ld, ints(x), dev(u))
+    assert accepted.tolist() == [2, 1, 2]
+    assert out.tolist() == [[V - 1, 5, 8 * k[0]], [V - 2, V - 9, -1], [V - 3, 9, 8 * k[2]]]
