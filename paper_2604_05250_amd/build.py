@@ -4,6 +4,8 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
@@ -27,19 +29,26 @@ def stale() -> bool:
 
 
 def build_library(force: bool = True, verbose: bool = False, extra_flags=()) -> str:
-    """Compile every kernel source into one shared library.  Returns its path."""
+    """Compile every kernel source, a few at a time, and link them into one shared library.  Returns its path."""
     if not force and not stale():
         return LIB
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc] + FLAGS + list(extra_flags) + ["-o", LIB] + [os.path.join(CSRC, f) for f in SOURCES]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
-    out = "\n".join(l for l in res.stdout.splitlines() if "packed-fp32-ops" not in l)
-    if res.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + out)
-    if verbose and out.strip():
-        print(out)
+
+    def run(cmd):
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+        out = "\n".join(l for l in res.stdout.splitlines() if "packed-fp32-ops" not in l)
+        if res.returncode != 0:
+            raise RuntimeError("hipcc failed:\n" + out)
+        if verbose and out.strip():
+            print(out)
+
+    with tempfile.TemporaryDirectory() as tmp, ThreadPoolExecutor(min(4, os.cpu_count() or 1)) as pool:
+        objects = [os.path.join(tmp, os.path.splitext(f)[0] + ".o") for f in SOURCES]
+        compile_flags = [f for f in FLAGS if f != "-shared"] + list(extra_flags) + ["-c"]
+        list(pool.map(lambda s, o: run([hipcc] + compile_flags + ["-o", o, os.path.join(CSRC, s)]), SOURCES, objects))
+        run([hipcc] + FLAGS + list(extra_flags) + ["-o", LIB] + objects)
     return LIB
 
 
