@@ -27,7 +27,7 @@ typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
-[[maybe_unused]] constexpr int kLoads = 4;                    // vectors of 16 bytes of a lane on their way
+constexpr int kLoads = 4;                    // vectors of 16 bytes of a lane on their way
 constexpr int kMostSplits = 64;              // of a row: a lane of a wave for each
 constexpr int kMostParts = 64;               // workgroups of the row that is drawn from: a thread of a workgroup for each of their waves
 [[maybe_unused]] constexpr float kCold = 1.0e-6f;             // temperatures up to here: all of the probability on the largest logit
@@ -530,16 +530,19 @@ Plan plan_of(int B, int n, int nv, int V, bool bf16, bool drafter)
     Plan p;
     p.vecs = (int)((long)V * (bf16 ? 2 : 4) / 16);
     const long rows = (long)B * nv + (drafter ? (long)B * n : 0);
-    auto divide = [&](long rows, long want, int most, int &per, int &count) {
+    // about `want` workgroups, each of whole rounds of `unit` vectors once it has as many (a round that is short takes as long: 32 x 4 rows of
+    // 152064 logits in lots of 1536 vectors 30.1 us, of 2048 27.4), at most `most` of a row
+    auto divide = [&](long rows, long want, int most, long unit, int &per, int &count) {
         long v = (long)p.vecs * rows / want;                 // vectors per workgroup
         const long least = ((long)p.vecs + most - 1) / most;
         v = v > least ? v : least;
-        v = (v + kThreads - 1) / kThreads * kThreads;        // (a quarter of it per wave: whole waves too)
-        per = (int)(v < 0x7fffff00 ? v : 0x7fffff00);
+        const long whole = v > unit / 2 ? unit : kThreads;   // (256 at least: of a part a quarter per wave)
+        v = (v + whole - 1) / whole * whole;
+        per = (int)(v < 0x7ffff000 ? v : 0x7ffff000);
         count = (int)(((long)p.vecs + per - 1) / per);
     };
-    divide(rows, 2048, kMostSplits, p.per_split, p.splits);
-    divide(B, 1024, kMostParts, p.per_part, p.parts);
+    divide(rows, 2048, kMostSplits, kThreads * kLoads, p.per_split, p.splits);
+    divide(B, 1024, kMostParts, kThreads, p.per_part, p.parts);
     p.states = ((size_t)rows * p.splits * sizeof(State) + 255) / 256 * 256;
     p.sums = ((size_t)B * p.parts * kWaves * sizeof(Sums) + 255) / 256 * 256;
     p.bytes = p.states + p.sums + (size_t)B * sizeof(Verdict);
