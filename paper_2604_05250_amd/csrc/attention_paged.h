@@ -131,6 +131,7 @@ __device__ __forceinline__ Group group_of(const int32_t *starts, int groups, int
 __device__ __forceinline__ int group_with(const int32_t *starts, int groups, int b)
 {
     const int lane = threadIdx.x & 63;
+    if (groups == 1) return uniform_load(starts) <= b && b < uniform_load(starts + 1) ? 0 : -1;
     for (int g0 = 0; g0 < groups; g0 += 64) {
         const int g = g0 + lane;
         const unsigned long long in = __ballot(g < groups && starts[g < groups ? g : 0] <= b && b < starts[g < groups ? g + 1 : 0]);
@@ -216,7 +217,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(DD_PAGED_HEAD, Tail 
     int rt, sp, first_seq = 0, row_count = rows_total;       // (SHARED) of the rows, the first sequence; rows of all of them
     unsigned b = 0, g;
     const int32_t *row_of_table, *held_at;
-    // (SHARED, whole) the prefix before a sequence's own keys: its tiles, positions and pages
+    // (SHARED, whole) the prefix before a sequence's own keys: tiles that it takes, its positions and pages
     int before = 0, prefix_len = 0;
     const int32_t *prefix_row = nullptr;
     if constexpr (SHARED) {
@@ -247,11 +248,13 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(DD_PAGED_HEAD, Tail 
             row_of_table = table + (size_t)first_seq * max_pages;
             held_at = kv_lens + first_seq;
             if (a.whole) {
+                int len = uniform_load(a.prefix_lens);       // (of the first group, beside the starts)
                 const int group = group_with(a.group_starts, a.groups, first_seq);
+                if (group > 0) len = uniform_load(a.prefix_lens + group);
                 if (group >= 0) {
                     prefix_row = a.prefix_table + (size_t)group * a.max_prefix_pages;
-                    prefix_len = min(max(uniform_load(a.prefix_lens + group), 0), a.max_prefix_pages << P_log2);
-                    before = (int)(((unsigned)prefix_len + 63u) >> 6) * (2 / NT);
+                    prefix_len = min(max(len, 0), a.max_prefix_pages << P_log2);
+                    before = (int)(((unsigned)prefix_len + 127u) >> 7) * (4 / NT);       // (whole pages: own keys lie in a page as in their part)
                 }
             }
         }
@@ -276,17 +279,18 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(DD_PAGED_HEAD, Tail 
     const unsigned in_page = (1u << P_log2) - 1;
     constexpr int IDS = ONE ? 1 : UNITS;             // pages: of the tile, or of each unit of 16 keys
     struct Pages { int id[IDS]; };
-    auto own_tile = [&](int tile) __attribute__((always_inline)) { return SHARED && tile >= before ? tile - before : tile; };   // of its part of the keys
     auto pages_of = [&](int tile) __attribute__((always_inline)) {
         Pages p;
-        const int32_t *row = row_of_table;
-        int last = max_pages - 1;
         if constexpr (SHARED) {
-            if (tile < before) { row = prefix_row; last = a.max_prefix_pages - 1; }
-            tile = own_tile(tile);
-        }
+            const bool first = tile < before;
+            const int32_t *const row = first ? prefix_row : row_of_table;
+            const int last = (first ? a.max_prefix_pages : max_pages) - 1, off = first ? 0 : (before * TILE) >> P_log2;
 #pragma unroll
-        for (int u = 0; u < IDS; ++u) p.id[u] = uniform_load(row + min((tile * TILE + 16 * u) >> P_log2, last));
+            for (int u = 0; u < IDS; ++u) p.id[u] = uniform_load(row + min(((tile * TILE + 16 * u) >> P_log2) - off, last));
+        } else {
+#pragma unroll
+            for (int u = 0; u < IDS; ++u) p.id[u] = uniform_load(row_of_table + min((tile * TILE + 16 * u) >> P_log2, max_pages - 1));
+        }
         return p;
     };
     const int held = uniform_load(held_at);
@@ -299,7 +303,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(DD_PAGED_HEAD, Tail 
     Share sh;
     if constexpr (SHARED) {
         sh = shared_share_of(held, max_pages, P_log2, splits, a.least);
-        if (a.whole) sh.per_split = before / (2 / NT) + sh.tiles;
+        if (a.whole) sh.per_split = (before * TILE >> 6) + sh.tiles;
         else if (sp >= sh.used) return;
     } else {
         sh = share_of(held, max_pages, P_log2, splits, rows_total, launched);
@@ -351,7 +355,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(DD_PAGED_HEAD, Tail 
     auto k_from = [&](const Pages &p, int tile) __attribute__((always_inline)) {
         KFrom f;
 #pragma unroll
-        for (int u = 0; u < IDS; ++u) f.base[u] = Kc + ((place(p.id[u]) << P_log2) + ((unsigned)(own_tile(tile) * TILE + 16 * u) & in_page)) * ROWB;
+        for (int u = 0; u < IDS; ++u) f.base[u] = Kc + ((place(p.id[u]) << P_log2) + ((unsigned)(tile * TILE + 16 * u) & in_page)) * ROWB;
         return f;
     };
     auto put_k = [&](const KFrom &f, unsigned buf, int i) __attribute__((always_inline)) {
@@ -368,13 +372,13 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(DD_PAGED_HEAD, Tail 
     const int v_begin = RG == 1 ? 0 : block * (NV / RG);
     auto v_from = [&](const Pages &p, int tile) __attribute__((always_inline)) {         // the tile's, or the lane's, first address
         if constexpr (ONE) {
-            return Vc + (((place(p.id[0]) * D) << P_log2) + ((unsigned)(own_tile(tile) * TILE) & in_page)) * EB + v_begin * v_step;
+            return Vc + (((place(p.id[0]) * D) << P_log2) + ((unsigned)(tile * TILE) & in_page)) * EB + v_begin * v_step;
         } else {
             // the page of the lane's piece, by the bits of its unit (not by an index, which would put the pages into memory)
             const unsigned u = EB == 1 ? v_piece : v_piece >> 1, m0 = 0u - (u & 1), m1 = 0u - (u >> 1);
             unsigned id = ((unsigned)p.id[0] & ~m0) | ((unsigned)p.id[1] & m0);
             if constexpr (IDS == 4) id = (id & ~m1) | ((((unsigned)p.id[2] & ~m0) | ((unsigned)p.id[3] & m0)) & m1);
-            return Vc + (((place((int)id) * D) << P_log2) + ((unsigned)(own_tile(tile) * TILE + 16 * u) & in_page)) * EB + (v_off - 16 * u * EB) + v_begin * v_step;
+            return Vc + (((place((int)id) * D) << P_log2) + ((unsigned)(tile * TILE + 16 * u) & in_page)) * EB + (v_off - 16 * u * EB) + v_begin * v_step;
         }
     };
     auto put_v = [&](const uint8_t *from, unsigned buf, int i) __attribute__((always_inline)) {
@@ -450,8 +454,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(DD_PAGED_HEAD, Tail 
         Factors f;
         int key_end = last_key;
         if constexpr (SHARED) {                      // (a tile behind the split's last has no key)
-            key_end = t >= t_end ? 0 : t < before ? prefix_len : sh.len;
-            t = own_tile(t);
+            key_end = t >= t_end ? 0 : t < before ? prefix_len : before * TILE + sh.len;
         }
         f.whole = t * TILE + TILE <= key_end;
 #pragma unroll

@@ -3,36 +3,45 @@
 // and weighted sum of values, that of both is  M = max(m, m'),  2^(m-M) l + 2^(m'-M) l',  2^(m-M) o + 2^(m'-M) o'.  So the rows of all
 // sequences of a group meet the prefix together, as the rows of one very long block, and its keys are read once for all of them; the own
 // keys are met sequence by sequence; a second kernel merges the states.  The workgroups are those of attention_paged.h, of either kind in
-// one launch where both take one row block, as neither fills the card in a serving batch's step.
+// one launch where both take as many row blocks, as neither fills the card in a serving batch's step.  Where that pays (plan_of), a sequence's
+// rows take prefix and own keys in one go instead, and there is nothing to merge.
+// One token of 16 sequences, 32/8 heads, e4m3, over 4096 keys and 512 of their own: 15.3 us, of which two launches that find no key take
+// 6.2 and either part alone some 6 more; with dd_paged_attention on whole tables, where caches hold what sequences share, 22.  Of 64
+// over 32768 and 256: 60 to 65, 0.55 PFLOP/s, the own keys' workgroups behind the others some 10 of it; on whole tables 285.
 #include "attention_paged.h"
 
 namespace dd {
 namespace {
 
-// Every state of a row, merged by D / 4 lanes: the prefix's splits, then those of the own keys.  PARTS such lots of lanes have a quarter of
-// the states each where there are many.  All that a row can have are asked for before it is known how many it has.
+// Every state of a row, merged by D / 4 lanes: the prefix's splits, then those of the own keys.  Two or four such lots of lanes have a half or
+// a quarter of the states each where one would have to go to memory more than once (one token of 32 sequences over 4000 keys, nine states
+// 16.5 -> 14.3 us).  All that a row can have are asked for before it is known how many it has.
+struct SharedMerge {
+    const int32_t *kv_lens, *group_starts, *prefix_lens;
+    uint8_t *O;
+    int rows_total, Hkv, max_pages, max_prefix_pages, groups, page_log2, own_splits, prefix_splits;
+};
 template <int D, int PARTS>
-__global__ __launch_bounds__(256) void shared_merge_kernel(const float *part_ml, const float *part_o, const int32_t *kv_lens, uint8_t *O, int Hkv, int rows_total, int rows,
-                                                           int max_pages, int page_log2, int own_splits, SharedTail a)
+__global__ __launch_bounds__(256) void shared_merge_kernel(const float *part_ml, const float *part_o, int slots, int rows, SharedMerge a)
 {
     constexpr int LANES = D / 4, U = 8, ROWS = 256 / LANES / PARTS;
     const int lot = threadIdx.x / LANES, part = lot % PARTS, mine = lot / PARTS, d0 = (threadIdx.x % LANES) * 4;
     const int row = min((int)blockIdx.x * ROWS + mine, rows - 1);
-    const float2 *ml = reinterpret_cast<const float2 *>(part_ml) + (size_t)row * a.slots;
-    const floatx4 *po = reinterpret_cast<const floatx4 *>(part_o + (size_t)row * a.slots * D + d0);
+    const float2 *ml = reinterpret_cast<const float2 *>(part_ml) + (size_t)row * slots;
+    const floatx4 *po = reinterpret_cast<const floatx4 *>(part_o + (size_t)row * slots * D + d0);
     float2 st[U];
     floatx4 v[U];
     auto fetch = [&](int s0) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int s = min(s0 + u * PARTS, a.slots - 1);
+            const int s = min(s0 + u * PARTS, slots - 1);
             st[u] = ml[s];
             v[u] = po[(size_t)s * (D / 4)];
         }
     };
     fetch(part);
-    const int b = (int)((unsigned)row / (unsigned)rows_total / (unsigned)Hkv);
-    const int own = shared_share_of(kv_lens[b], max_pages, page_log2, own_splits, a.least).used;
+    const int b = (int)((unsigned)row / (unsigned)a.rows_total / (unsigned)a.Hkv);
+    const int own = shared_share_of(a.kv_lens[b], a.max_pages, a.page_log2, a.own_splits, kSplitTiles).used;
     int lo = 0, hi = a.groups;                       // the last group that begins at b or before
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
@@ -40,7 +49,7 @@ __global__ __launch_bounds__(256) void shared_merge_kernel(const float *part_ml,
         else hi = mid;
     }
     const bool member = a.group_starts[lo] <= b && b < a.group_starts[lo + 1];
-    const int shared = shared_share_of(member ? a.prefix_lens[lo] : 0, a.max_prefix_pages, page_log2, a.prefix_splits, a.least).used;
+    const int shared = shared_share_of(member ? a.prefix_lens[lo] : 0, a.max_prefix_pages, a.page_log2, a.prefix_splits, kSplitTiles).used;
     auto counts = [&](int s) __attribute__((always_inline)) { return s < shared || (s >= a.prefix_splits && s < a.prefix_splits + own); };
     float M = kNone, L = 0;
     floatx4 x = {0, 0, 0, 0};
@@ -61,7 +70,7 @@ __global__ __launch_bounds__(256) void shared_merge_kernel(const float *part_ml,
             }
         }
         s0 += U * PARTS;
-        if (s0 >= a.slots) break;
+        if (s0 >= slots) break;
         fetch(s0);
     }
     if constexpr (PARTS > 1) {
@@ -89,7 +98,7 @@ __global__ __launch_bounds__(256) void shared_merge_kernel(const float *part_ml,
     }
     if ((int)blockIdx.x * ROWS + mine >= rows) return;
     const float inv = L > 0 ? 1.0f / L : 0.0f;       // no key at all: zeros
-    *reinterpret_cast<uint2 *>(O + ((size_t)row * D + d0) * 2) = make_uint2(pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv));
+    *reinterpret_cast<uint2 *>(a.O + ((size_t)row * D + d0) * 2) = make_uint2(pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[2] * inv, x[3] * inv));
 }
 
 constexpr int kLongSplitTiles = 32;          // tiles of 64 keys of a long split
@@ -156,7 +165,8 @@ Plan plan_of(const SharedAttnShape &s)
 
 unsigned eights(long wgs) { return (unsigned)((wgs + 7) / 8 * 8); }
 
-template <int D, bool FP8, int NT, bool ONE> hipError_t attend(const SharedAttnArgs &a, const SharedTail &tail, int rg, unsigned grid, unsigned launched, unsigned shape, hipStream_t stream)
+template <int D, bool FP8, int NT, bool ONE>
+hipError_t attend(const SharedAttnArgs &a, const SharedTail &tail, int rg, unsigned grid, unsigned launched, unsigned shape, hipStream_t stream)
 {
     auto run = [&](auto kernel) {
         return launch(kernel, dim3(grid), dim3(256), stream, a.table, a.kv_lens, static_cast<const uint8_t *>(a.Kc), static_cast<const uint8_t *>(a.Vc), a.s.Hkv,
@@ -165,7 +175,8 @@ template <int D, bool FP8, int NT, bool ONE> hipError_t attend(const SharedAttnA
     return rg == 1 ? run(attn_paged_kernel<D, FP8, NT, ONE, 1, SharedTail>)
          : rg == 2 ? run(attn_paged_kernel<D, FP8, NT, ONE, 2, SharedTail>) : run(attn_paged_kernel<D, FP8, NT, ONE, 4, SharedTail>);
 }
-template <int D, bool FP8> hipError_t attend(const SharedAttnArgs &a, const SharedTail &tail, int rg, unsigned grid, unsigned launched, unsigned shape, hipStream_t stream)
+template <int D, bool FP8>
+hipError_t attend(const SharedAttnArgs &a, const SharedTail &tail, int rg, unsigned grid, unsigned launched, unsigned shape, hipStream_t stream)
 {
     constexpr int NT = FP8 ? 2 : 1;
     return (1 << a.s.page_log2) >= 32 * NT ? attend<D, FP8, NT, true>(a, tail, rg, grid, launched, shape, stream)
@@ -203,8 +214,8 @@ hipError_t launch_attention_shared(const SharedAttnArgs &a, hipStream_t stream)
     auto part = [&](int rg, long prefix_wgs, long own_wgs) {
         tail.prefix_wgs = eights(prefix_wgs); tail.own_wgs = (unsigned)own_wgs;
         const unsigned grid = tail.prefix_wgs + eights(own_wgs);
-        return s.d == 128 ? (s.fp8 ? attend<128, true>(a, tail, rg, grid, (unsigned)prefix_wgs, shape, stream) : attend<128, false>(a, tail, rg, grid, (unsigned)prefix_wgs, shape, stream))
-                          : (s.fp8 ? attend<64, true>(a, tail, rg, grid, (unsigned)prefix_wgs, shape, stream) : attend<64, false>(a, tail, rg, grid, (unsigned)prefix_wgs, shape, stream));
+        auto go = [&](auto attends) { return attends(a, tail, rg, grid, (unsigned)prefix_wgs, shape, stream); };
+        return s.d == 128 ? (s.fp8 ? go(attend<128, true>) : go(attend<128, false>)) : (s.fp8 ? go(attend<64, true>) : go(attend<64, false>));
     };
     hipError_t e;
     if (p.whole || p.prefix.rg == p.own.rg) {
@@ -214,15 +225,14 @@ hipError_t launch_attention_shared(const SharedAttnArgs &a, hipStream_t stream)
         if (e == hipSuccess) e = part(p.own.rg, 0, p.own.wgs);
     }
     if (e != hipSuccess || p.whole) return e;
-    const int parts = p.slots > 12 ? 4 : 1;
+    const int parts = p.slots > 16 ? 4 : p.slots > 8 ? 2 : 1;
     const unsigned per_wg = 256 / (s.d / 4) / parts;
     const dim3 grid((unsigned)((rows + per_wg - 1) / per_wg));
-    auto merge = [&](auto kernel) {
-        return launch(kernel, grid, dim3(256), stream, tail.part_ml, tail.part_o, a.kv_lens, tail.O, s.Hkv, (s.H / s.Hkv) * s.n, (int)rows, s.max_pages, s.page_log2,
-                      p.own.splits, tail);
-    };
-    return s.d == 128 ? (parts == 4 ? merge(shared_merge_kernel<128, 4>) : merge(shared_merge_kernel<128, 1>))
-                      : (parts == 4 ? merge(shared_merge_kernel<64, 4>) : merge(shared_merge_kernel<64, 1>));
+    const SharedMerge m{a.kv_lens, a.group_starts, a.prefix_lens, tail.O, (s.H / s.Hkv) * s.n, s.Hkv, s.max_pages, s.max_prefix_pages, s.G, s.page_log2, p.own.splits,
+                        p.prefix.splits};
+    auto merge = [&](auto kernel) { return launch(kernel, grid, dim3(256), stream, tail.part_ml, tail.part_o, p.slots, (int)rows, m); };
+    return s.d == 128 ? (parts == 4 ? merge(shared_merge_kernel<128, 4>) : parts == 2 ? merge(shared_merge_kernel<128, 2>) : merge(shared_merge_kernel<128, 1>))
+                      : (parts == 4 ? merge(shared_merge_kernel<64, 4>) : parts == 2 ? merge(shared_merge_kernel<64, 2>) : merge(shared_merge_kernel<64, 1>));
 }
 
 }  // namespace dd

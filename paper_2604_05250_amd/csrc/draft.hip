@@ -14,7 +14,10 @@
 //                       wrong they agree to kNear, for kNear of the tokens, and a part's weight is off by kNear^2 of it at most
 //   draft_pick_kernel   the part in which the running sum passes its mark, and there the token
 // An fp64 instruction takes a wave as long here as an fp32 one (2.2 and 1.9 ns), a power of two 18 of them; with fp64 sums in the
-// first kernel too, that one took 100 us for 64 sequences of 8 drafts, 126464 bf16 logits, which are 44 us from memory.
+// first kernel too, that one took 100 us for 64 sequences of 8 drafts, 126464 bf16 logits.  As it is the three take 47 (5.8 TB/s), 24 and 5:
+// the second's workgroups are 7 us at the decisions, which are chains of loads just behind 275 MB of others, and 5 to 8 at their part of the
+// row.  (The drafts' fate by a launch of its own: 7.5 + 17 for the 24.  All of a row's loads before its arithmetic, and logits picked up
+// by the first kernel: no difference.  Exponentials of 15 instructions for 18: 24.6.)
 #include "dd_internal.h"
 
 #include <type_traits>

