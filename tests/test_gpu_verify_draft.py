@@ -248,3 +248,56 @@ def test_offsets_past_32_bits():
     out, accepted, _ = dd.dd_verify_draft(lv, ld, ints(x), dev(u))
     assert accepted.tolist() == [2, 1, 2]
     assert out.tolist() == [[V - 1, 5, 8 * k[0]], [V - 2, V - 9, -1], [V - 3, 9, 8 * k[2]]]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("u", [0.0, 1 - 2.0 ** -24])
+def test_random_numbers_at_their_ends(dtype, u):
+    # 0 keeps every draft that is possible and draws the first token that is, the largest number the last one
+    args, want = _case(16, 3, 320, dtype=dtype, holes=0.5, seed=21)
+    want["uniforms"] = np.full((16, 4), u)
+    args["uniforms"] = dev(want["uniforms"].astype(np.float32))
+    args["tokens"][::2] = ints(np.random.default_rng(0).integers(0, 320, (8, 3)))
+    want["tokens"] = args["tokens"].cpu().numpy()
+    tokens, accepted, _, margin = draft.verify_draft(**want)
+    got = dd.dd_verify_draft(**args)
+    sure = (margin > NEAR) | (u == 0)                        # (0 is no further from the first border than that token's own weight)
+    assert sure.any() and np.array_equal(got[1].cpu().numpy()[sure], accepted[sure]) and np.array_equal(got[0].cpu().numpy()[sure], tokens[sure])
+
+
+def test_temperatures_far_out():
+    # very hot: all tokens that are possible alike; very cold: the largest logit, from 1e-6 down by rule
+    temps = [1e30, 3e38, 1e6, 2e-6, 1e-4, 1e-6, 1e-38, 0.0]
+    args, want = _case(8, 3, 512, temperature=[1.0] * 8, holes=0.3, seed=13)
+    args["temperature"], want["temperature"] = dev(np.array(temps, np.float32)), np.array(temps, np.float32).astype(np.float64)
+    _compare(dd.dd_verify_draft(**args), want)
+
+
+def test_many_sequences_and_the_same_memory_on_both_sides():
+    import torch
+    B, V = 5000, 64
+    g = torch.Generator(device="cuda").manual_seed(3)
+    lv = torch.randn((B, 1, V), generator=g, device="cuda")
+    tokens = torch.randint(0, V, (B, 1), generator=g, device="cuda").int()
+    u = torch.rand((B, 2), generator=g, device="cuda")
+    out, accepted, chances = dd.dd_verify_draft(lv, lv, tokens, u)
+    assert bool((accepted == 1).all()) and torch.equal(out[:, :1], tokens) and bool((out[:, 1] == -1).all()) and bool((chances == 1).all())
+    ld = torch.randn((B, 1, V), generator=g, device="cuda")
+    _compare(dd.dd_verify_draft(lv, ld, tokens, u), dict(logits_v=host(lv), logits_d=host(ld), tokens=tokens.cpu().numpy(), uniforms=host(u), bonus=False))
+
+
+def test_tokens_come_out_with_the_verifiers_probabilities():
+    # drafts drawn from q, three hundred thousand of them: counts of the first token against p, chi squared with 15 degrees of freedom
+    import torch
+    B, V = 300000, 16
+    g = torch.Generator(device="cuda").manual_seed(7)
+    l = torch.randn((2, V), generator=g, device="cuda") * 1.5
+    tokens = torch.multinomial(torch.softmax(l[1], 0), B, replacement=True, generator=g).int()[:, None]
+    lv, ld = l[0].expand(B, 1, V).contiguous(), l[1].expand(B, 1, V).contiguous()
+    for d in (ld, None):
+        x = tokens if d is not None else torch.full_like(tokens, 3)
+        out, accepted, _ = dd.dd_verify_draft(lv, d, x, torch.rand((B, 2), generator=g, device="cuda"))
+        counts = torch.bincount(out[:, 0].long(), minlength=V).double()
+        p = torch.softmax(l[0].double(), 0)
+        chi2 = float(((counts - B * p) ** 2 / (B * p)).sum())
+        assert chi2 < 60, chi2                               # (a chance of 2e-7)
