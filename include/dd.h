@@ -551,8 +551,8 @@ size_t dd_verify_scores_workspace_bytes(int P, int V, dd_dtype logit_dtype);
  * Arithmetic: draws in fp64 with exponentials to 1.1e-12, and so is a draft's decision wherever fp32 exponentials leave it open:
  * which drafts stand and which token is drawn does not hang on roundings.  Chances are good to 2e-5 of each, 1e-7 as a rule.
  * V * sizeof(element) a multiple of 16; logits 16-byte aligned; no output overlaps an input or another output (DD_ERR_SHAPE); B >= 0
- * (0: a no-op), n >= 0, n >= 1 without bonus; workspace from the query; workgroups of one launch (rows, and parts of long rows)
- * fewer than 2^24, else DD_ERR_SHAPE.
+ * (0: a no-op), n >= 0, n >= 1 without bonus, B*(n+1) < 2^30; workspace from the query; workgroups of one launch (rows, and parts of long
+ * rows) fewer than 2^24, else DD_ERR_SHAPE.
  */
 int dd_verify_draft(const void *logits_v, const void *logits_d, const int32_t *tokens, const int32_t *n_draft,
                     const float *uniforms, const float *temperature,

@@ -17,7 +17,8 @@
 // first kernel too, that one took 100 us for 64 sequences of 8 drafts, 126464 bf16 logits.  As it is the three take 47 (5.8 TB/s), 24 and 5:
 // the second's workgroups are 7 us at the decisions, which are chains of loads just behind 275 MB of others, and 5 to 8 at their part of the
 // row.  (The drafts' fate by a launch of its own: 7.5 + 17 for the 24.  All of a row's loads before its arithmetic, and logits picked up
-// by the first kernel: no difference.  Exponentials of 15 instructions for 18: 24.6.)
+// by the first kernel: no difference.  Exponentials of 15 instructions for 18: 24.6.  The last of a sequence's workgroups as the third launch: 194
+// for 24 and 5, as every workgroup's fence writes its cache back.)
 #include "dd_internal.h"
 
 #include <type_traits>
