@@ -395,7 +395,7 @@ size_t dd_paged_attention_workspace_bytes(int n, int B, int H, int Hkv, int d, i
  *   everything else (lengths, pages that are none, empty rows, dtypes, ranges, arithmetic) as for dd_paged_attention
  * For starts that descend, the outputs of the sequences concerned are unspecified; no access leaves the tensors.  The states of a row's
  * parts live in `workspace`; how many there are goes by sizes and capacities alone.
- * G, max_prefix_pages >= 1, max_prefix_pages*page_size < 2^30, (B*(ceil(n*H/Hkv / 32) + 1) + G)*Hkv < 2^24; O overlaps none of its inputs.
+ * G, max_prefix_pages >= 1, max_prefix_pages*page_size < 2^30, (B*(ceil(n*H/Hkv / 32) + 1) + G)*Hkv < 2^22; O overlaps none of its inputs.
  */
 int dd_paged_attention_shared(const void *Q, const void *Kc, const void *Vc, const float *k_scale, const float *v_scale,
                               const int32_t *prefix_table, const int32_t *prefix_lens, const int32_t *group_starts,

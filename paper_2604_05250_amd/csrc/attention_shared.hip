@@ -188,8 +188,9 @@ hipError_t attend(const SharedAttnArgs &a, const SharedTail &tail, int rg, unsig
 bool shared_attention_fits(const SharedAttnShape &s)
 {
     const double rows = (double)(s.H / s.Hkv) * s.n;
-    // (splits are for calls of few workgroups: with or without them a launch of either kind has fewer than 2^24, and all of them 2^25)
-    return rows * s.B * s.Hkv < 1073741824.0 && ((__builtin_ceil(rows / 32) + 1) * s.B + s.G) * s.Hkv < 16777216.0;
+    // (fewer than 2^22 workgroups of either kind, of 256 threads, and fewer than 2^27 rows, for which the merge has a workgroup per eight or more,
+    // less only where rows are few: launches of fewer than 2^32 threads)
+    return rows * s.B * s.Hkv < 1073741824.0 && ((__builtin_ceil(rows / 32) + 1) * s.B + s.G) * s.Hkv < 4194304.0;
 }
 
 size_t shared_attention_workspace_bytes(const SharedAttnShape &s)

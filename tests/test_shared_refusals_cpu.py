@@ -33,6 +33,13 @@ def test_refused(want, kw):
     assert attend(**kw) == want
 
 
+def test_launches_have_fewer_than_2_32_threads():
+    # (a workspace that would do: what is refused is the size)
+    big = dict(H=2, Hkv=2, pages=99, wsn=1 << 62)
+    assert attend(B=1 << 20, **big) == SHAPE and attend(B=(1 << 20) - 4, G=4, **dict(big, ws=None)) == WORKSPACE
+    assert attend(B=1, n=1 << 26, **big) == SHAPE and attend(B=1, G=1 << 21, **big) == SHAPE
+
+
 def test_without_queries_does_nothing():
     assert attend(n=0) == 0 and attend(n=0, Q=None, O=None) == 0
 
