@@ -153,6 +153,9 @@ Plan plan_of(const SharedAttnShape &s)
             : keys <= (full || apart <= kUnits ? most : apart <= 2 * kUnits ? most * 3 / 4 : most * 3 * kUnits / (2 * apart));
     const int hook = tune("DD_TUNE_SHARED_WHOLE", -1);
     if (hook >= 0) p.whole = hook != 0;
+    // In one go a sequence's positions are those of both tables, counted in 32 bits, with up to 127 between them and a thousand asked for behind
+    // the last.  Tables that may hold more together than one may are taken by two kinds of workgroups.
+    if (keys >= 1l << 30) p.whole = false;
     if (p.whole) {
         p.own.splits = 1;
         p.own.wgs = own_base;
