@@ -548,8 +548,10 @@ size_t dd_verify_scores_workspace_bytes(int P, int V, dd_dtype logit_dtype);
  * Logits are finite or -inf (probability 0), below 2^30 T in magnitude; a row has a finite one.  For any other values, of
  * uniforms, tokens and temperatures too, no access leaves the tensors and tokens are in [-1, V) or drafts.  Rows behind the last that
  * a sequence needs are not read.
- * Arithmetic: draws in fp64 with exponentials to 1.1e-12, and so is a draft's decision wherever fp32 exponentials leave it open:
- * which drafts stand and which token is drawn does not hang on roundings.  Chances are good to 2e-5 of each, 1e-7 as a rule.
+ * Arithmetic: draws in fp64 with exponentials to 1.1e-12, and so is a draft's decision wherever fp32 exponentials leave it open.  Drafts
+ * and tokens are those of exact arithmetic wherever p_i(x_i) and u_i q_i(x_i) are more than 1e-11 of the larger apart, and u sum w more than
+ * 1e-11 from the borders (p summing to 1): also of a w that is next to nothing, as from a drafter that nearly agrees.  Chances are good
+ * to 2e-5 of each, 1e-7 as a rule.
  * V * sizeof(element) a multiple of 16; logits 16-byte aligned; no output overlaps an input or another output (DD_ERR_SHAPE); B >= 0
  * (0: a no-op), n >= 0, n >= 1 without bonus, B*(n+1) < 2^30; workspace from the query; workgroups of one launch (rows, and parts of long
  * rows) fewer than 2^24, else DD_ERR_SHAPE.

@@ -10,11 +10,16 @@
 //                       exponentials, whose sums are good to kNear: memory bounds it
 //   draft_decide_kernel the drafts' fate; a draft nearer to its border than kNear is decided again on fp64 sums of its rows (one in some
 //                       ten thousand).  Then, of the one row that a token is drawn from, in fp64 by parts: sums of p's and q's
-//                       exponentials, all and where p is the larger.  Which of the two is the larger goes by the fp32 sums: where that is
-//                       wrong they agree to kNear, for kNear of the tokens, and a part's weight is off by kNear^2 of it at most
-//   draft_pick_kernel   the part in which the running sum passes its mark, and there the token
+//                       exponentials, all and where p is the larger.  Which of the two is the larger goes by the fp32 sums, and may be
+//                       wrong for tokens where they agree to kNear: of those there is a sum too
+//   draft_pick_kernel   the part in which the running sum passes its mark, and there the token.  Now S_p and S_q are known in fp64, and with
+//                       them by how much the quotient that decided was off, e: no border is off by more than e times the probability of
+//                       the tokens that were near.  A mark closer than that to its token's borders is taken again, with the parts that
+//                       have such tokens summed by the true quotient: fewer than one row in ten thousand where drafter and
+//                       verifier differ; every row where they agree to 10^-5, or on a token that outweighs all others.  (One
+//                       sequence, 126464 fp32 logits: 14.5 us, 22 with such a token, 88 where all tokens are near; 64 of them 36, 51, 105.)
 // An fp64 instruction takes a wave as long here as an fp32 one (2.2 and 1.9 ns), a power of two 18 of them; with fp64 sums in the
-// first kernel too, that one took 100 us for 64 sequences of 8 drafts, 126464 bf16 logits.  As it is the three take 47 (5.8 TB/s), 24 and 5:
+// first kernel too, that one took 100 us for 64 sequences of 8 drafts, 126464 bf16 logits.  As it is the three take 47.5 (5.8 TB/s), 24.4 and 5.6:
 // the second's workgroups are 7 us at the decisions, which are chains of loads just behind 275 MB of others, and 5 to 8 at their part of the
 // row.  (The drafts' fate by a launch of its own: 7.5 + 17 for the 24.  All of a row's loads before its arithmetic, and logits picked up
 // by the first kernel: no difference.  Exponentials of 15 instructions for 18: 24.6.  The last of a sequence's workgroups as the third launch: 194
@@ -44,9 +49,9 @@ constexpr int kMostParts = 64;               // workgroups of the row that is dr
 [[maybe_unused]] constexpr double kNear = 2.0e-5;
 
 struct State { float ref; int first; double sum; };      // reference, its first index (temperature 0), sum
-struct Sums { double p, q, above_p, above_q; };          // of exponentials, of a part of the row that is drawn from: all, and where p > q
+struct Sums { double p, q, above_p, above_q, near_p; };  // of exponentials, of a part of the row that is drawn from: all, where p > q, of vectors where that is open
 enum { kDone = 0, kDraw = 1 };
-struct Verdict { int kind, at, minus, without; float ref_p, ref_q; double c; };      // how the token at `at` is drawn
+struct Verdict { int kind, at, minus, without; float ref_p, ref_q; double c, even; };        // how the token at `at` is drawn; S_p / S_q of the fp32 sums
 
 struct DraftKernelArgs {
     const uint8_t *lv, *ld;
@@ -330,7 +335,7 @@ template <bool BF16> __global__ __launch_bounds__(kThreads) void draft_decide_ke
             if (j != at || !draws) a.out_tokens[(size_t)b * (a.n + 1) + j] = j < at ? a.tokens[(size_t)b * a.n + j] : -1;
         if (tid == 0) a.out_accepted[b] = at;
     }
-    Verdict verdict{kDone, at, 0, -1, 0, 0, c};
+    Verdict verdict{kDone, at, 0, -1, 0, 0, c, 0};
     State p{}, q{};
     const bool minus = down && a.ld != nullptr;
     const int without = down && a.ld == nullptr ? a.tokens[(size_t)b * a.n + at] : -1;       // a drafter without probabilities was sure of this one
@@ -342,7 +347,8 @@ template <bool BF16> __global__ __launch_bounds__(kThreads) void draft_decide_ke
             if (part == 0 && tid == 0) a.out_tokens[(size_t)b * (a.n + 1) + at] = p.first < V ? p.first : -1;
         } else {
             if (minus) q = row_state(a, d_row + at, c);
-            verdict = Verdict{kDraw, at, minus, without, p.ref, q.ref, c};
+            // p > q as e_p > e_q S_p / S_q; a row without any probability is below whatever there is
+            verdict = Verdict{kDraw, at, minus, without, p.ref, q.ref, c, minus && q.sum > 0 ? p.sum / q.sum : 0};
         }
     }
     if (part == 0 && tid == 0) a.verdicts[b] = verdict;
@@ -351,9 +357,7 @@ template <bool BF16> __global__ __launch_bounds__(kThreads) void draft_decide_ke
     const int per_wave = a.per_part / kWaves, begin = part * a.per_part + wave * per_wave, end = min(begin + per_wave, a.vecs);
     const u32x4 *const pv = reinterpret_cast<const u32x4 *>(row_v(at)), *const pd = minus ? reinterpret_cast<const u32x4 *>(row_d(at)) : pv;
     const double at_p = -(double)p.ref * c, at_q = -(double)q.ref * c;
-    // p > q as e_p > e_q S_p / S_q; a row without any probability is below whatever there is
-    const double even = minus && q.sum > 0 ? p.sum / q.sum : 0;
-    Sums s{0, 0, 0, 0};
+    Sums s{0, 0, 0, 0, 0};
     if (begin < end) {
         u32x4 wv = pv[min(begin + lane, end - 1)], wd = pd[min(begin + lane, end - 1)];
         for (int v = begin + lane; v < end; v += 64) {
@@ -363,15 +367,21 @@ template <bool BF16> __global__ __launch_bounds__(kThreads) void draft_decide_ke
             wv = pv[min(v + 64, end - 1)];                   // (the next ones, on their way meanwhile)
             wd = pd[min(v + 64, end - 1)];
             if (minus) {
+                double of_vector = 0;
+                bool open = false;
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
                     const double ep = weight_of(x[e], c, at_p), eq = weight_of(y[e], c, at_q);
-                    const bool above = ep > eq * even;
-                    s.p += ep;
+                    const double more = __builtin_fma(-eq, verdict.even, ep);
+                    const bool above = more > 0;
+                    of_vector += ep;
                     s.q += eq;
                     s.above_p += above ? ep : 0;
                     s.above_q += above ? eq : 0;
+                    open = open || __builtin_fabs(more) <= kNear * ep;
                 }
+                s.p += of_vector;
+                s.near_p += open ? of_vector : 0;
             } else {
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
@@ -384,6 +394,7 @@ template <bool BF16> __global__ __launch_bounds__(kThreads) void draft_decide_ke
     }
     s.q = wave_sum(s.q);
     s.above_q = wave_sum(s.above_q);
+    s.near_p = wave_sum(s.near_p);
     s.p = wave_sum(s.p);
     s.above_p = wave_sum(s.above_p);
     if (lane == 0) a.sums[((size_t)b * a.parts + part) * kWaves + wave] = s;
@@ -460,9 +471,9 @@ template <bool BF16> __global__ __launch_bounds__(kThreads) void draft_pick_kern
 #if defined(__HIP_DEVICE_COMPILE__)
     constexpr int E = BF16 ? 8 : 4;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, b = blockIdx.x, pieces = a.parts * kWaves, per_piece = a.per_part / kWaves;
-    __shared__ double of_wave[5][kWaves];
+    __shared__ double of_wave[6][kWaves], again[kThreads];
     const Verdict verdict = a.verdicts[b];
-    Sums s{0, 0, 0, 0};
+    Sums s{0, 0, 0, 0, 0};
     if (verdict.kind == kDone) return;
     if (tid < pieces) s = a.sums[(size_t)b * pieces + tid];
     const double u = __builtin_fmax((double)a.uniforms[(size_t)b * (a.n + 1) + a.n], 0.0);
@@ -470,41 +481,74 @@ template <bool BF16> __global__ __launch_bounds__(kThreads) void draft_pick_kern
     const bool minus = verdict.minus != 0;
     const size_t row_bytes = (size_t)a.vecs * 16;
     const uint8_t *const row_v = a.lv + ((size_t)b * a.nv + at) * row_bytes, *const row_d = minus ? a.ld + ((size_t)b * a.n + at) * row_bytes : row_v;
+    const u32x4 *const pv = reinterpret_cast<const u32x4 *>(row_v), *const pd = reinterpret_cast<const u32x4 *>(row_d);
     const double c = verdict.c, at_p = -(double)verdict.ref_p * c, at_q = -(double)verdict.ref_q * c;
-    const double wave_p = wave_sum(s.p), wave_q = wave_sum(s.q);
+    const double wave_p = wave_sum(s.p), wave_q = wave_sum(s.q), wave_near = wave_sum(s.near_p);
     if (lane == 0) {
         of_wave[3][wave] = wave_p;
         of_wave[4][wave] = wave_q;
+        of_wave[5][wave] = wave_near;
     }
     __syncthreads();
-    double all_p = 0, all_q = 0;
+    double all_p = 0, all_q = 0, near_p = 0;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
         all_p += of_wave[3][w];
         all_q += of_wave[4][w];
+        near_p += of_wave[5][w];
     }
     const double inv_p = all_p > 0 ? 1.0 / all_p : 0.0, inv_q = all_q > 0 ? 1.0 / all_q : 0.0;
+    // How far borders may be off as tokens stand on the wrong side of S_p / S_q:  such a token's p and q differ by no more than that quotient is
+    // off, relative, and all of them go the same way.  Twice that.  (Values that are none: everything is taken again.)
+    const double off = minus && near_p > 0 ? 2 * __builtin_fabs(verdict.even * (all_q * inv_p) - 1) * (near_p * inv_p) : 0.0;
     int token = -1;
-    // what is left of p without q; where p is nowhere above q, p itself
-    for (int left = 1; left >= 0 && token < 0; --left) {
-        const Spot piece = spot_of(left ? s.above_p * inv_p - s.above_q * inv_q : s.p * inv_p, 0, false, 0, u, of_wave);
-        if (piece.thread < 0) continue;
-        // ---- within the piece, neighbouring vectors per thread
-        const int begin = piece.thread * per_piece, end = min(begin + per_piece, a.vecs), each = (end - begin + kThreads - 1) / kThreads;
+    // what is left of p without q, on the sums at hand, then, where that leaves it open, on true ones; where p is nowhere above q, p itself
+    enum { kLeft = 2, kAgain = 1, kAll = 0 };
+    for (int how = kLeft; how >= kAll && token < 0; --how) {
+        const bool left = how != kAll;
         auto weight = [&](float x, float y, int e) __attribute__((always_inline)) {
             double w = weight_of(x, c, at_p) * inv_p;
             if (left && minus) w = __builtin_fmax(w - weight_of(y, c, at_q) * inv_q, 0.0);
             return left && e == verdict.without ? 0.0 : w;
         };
-        double sum = 0;
-        const int mine = begin + tid * each;
-        for (int v = mine; v < min(mine + each, end); ++v) {
+        auto weights = [&](const u32x4 &wv, const u32x4 &wd, int v) __attribute__((always_inline)) {       // of a vector of the row
             float x[E], y[E];
-            unpack<BF16>(reinterpret_cast<const u32x4 *>(row_v)[v], x);
-            unpack<BF16>(reinterpret_cast<const u32x4 *>(row_d)[v], y);
+            unpack<BF16>(wv, x);
+            unpack<BF16>(wd, y);
+            double sum = 0;
 #pragma unroll
             for (int e = 0; e < E; ++e) sum += weight(x[e], y[e], v * E + e);
+            return sum;
+        };
+        double mine = left ? s.above_p * inv_p - s.above_q * inv_q : s.p * inv_p;
+        if (how == kAgain) {
+            if (off == 0) continue;
+            again[tid] = s.near_p != 0 ? -1 : mine;          // (parts without such tokens stay as they are)
+            __syncthreads();
+            for (int k = wave; k < pieces; k += kWaves) {
+                if (again[k] > -0.5) continue;
+                const int begin = k * per_piece, end = min(begin + per_piece, a.vecs);
+                u32x4 wv = pv[min(begin + lane, end - 1)], wd = pd[min(begin + lane, end - 1)];
+                double sum = 0;
+                for (int v = begin + lane; v < end; v += 64) {
+                    const u32x4 now_v = wv, now_d = wd;
+                    wv = pv[min(v + 64, end - 1)];
+                    wd = pd[min(v + 64, end - 1)];
+                    sum += weights(now_v, now_d, v);
+                }
+                sum = wave_sum(sum);
+                if (lane == 0) again[k] = sum;
+            }
+            __syncthreads();
+            mine = again[tid];
         }
+        const Spot piece = spot_of(mine, 0, false, 0, u, of_wave);
+        if (piece.thread < 0) continue;
+        // ---- within the piece, neighbouring vectors per thread
+        const int begin = piece.thread * per_piece, end = min(begin + per_piece, a.vecs), each = (end - begin + kThreads - 1) / kThreads;
+        double sum = 0;
+        const int first = begin + tid * each;
+        for (int v = first; v < min(first + each, end); ++v) sum += weights(pv[v], pd[v], v);
         __syncthreads();                                     // (`of_wave` has been read)
         const Spot who = spot_of(sum, piece.before, true, piece.mark, 0, of_wave);
         if (who.thread >= 0) {
@@ -512,15 +556,22 @@ template <bool BF16> __global__ __launch_bounds__(kThreads) void draft_pick_kern
             const int from = (begin + who.thread * each) * E, to = min(begin + (who.thread + 1) * each, end) * E;
             double done = who.before;
             int last = -1;
+            bool clear = false;
             for (int e0 = from; e0 < to && token < 0; e0 += 64) {
                 const int e = min(e0 + lane, to - 1);
                 const double w = e0 + lane < to ? weight(logit<BF16>(row_v, e), logit<BF16>(row_d, e), e) : 0.0, upto = up_to(w);
                 const unsigned long long passed = __ballot(w > 0 && done + upto > who.mark), some = __ballot(w > 0);
-                if (passed) token = e0 + __builtin_ctzll(passed);
+                if (passed) {
+                    const int l = __builtin_ctzll(passed);
+                    const double behind = done + from_lane(upto, l);
+                    token = e0 + l;
+                    clear = behind - who.mark > off && who.mark - (behind - from_lane(w, l)) > off;
+                }
                 if (some) last = e0 + 63 - __builtin_clzll(some);
                 done += from_lane(upto, 63);
             }
             if (token < 0) token = last;
+            if (how == kLeft && off != 0 && !clear) token = -1;
         }
         __syncthreads();
     }
