@@ -335,7 +335,8 @@ int dd_paged_cache_append(void *Kc, void *Vc, float *k_scale, float *v_scale,
  * have = ceil(lens[b] / page_size) pages of block_table[b,:], shall have new_lens[b] on need = ceil(new_lens[b] / page_size).
  *     need < have: entries need .. have - 1 go back to the pool and become -1
  *     need > have: entries have .. need - 1 are set to free pages.  In the order of b, a sequence gets them if the pages that it and the
- *         sequences before it ask for (those that get none included) are no more than are free once all pages have come back
+ *         sequences before it ask for (those that get none included) are no more than are free once all pages have come back: behind one
+ *         that asks for more than there is, nobody gets any in this call, so a caller puts first what has to go on
  * free_pages [capacity] i32 is the pool's stack, its first *num_free entries are free.  With F entries and R pages given back, the i-th of
  * them (in the order of sequences, then entries) goes to place F + R - 1 - i, the t-th page taken comes from place F + R - 1 - t, and
  * *num_free becomes F + R less the pages taken: a call and its opposite leave the tables and the stack as they were.
@@ -388,13 +389,16 @@ size_t dd_paged_attention_workspace_bytes(int n, int B, int H, int Hkv, int d, i
  * group_starts[g+1] have the positions of prefix g before their own,
  *     O[b,h,i,:] = sum_j softmax_j( Q[b,h,i,:] . K_j / sqrt(d) ) V_j   over the prefix's positions j < prefix_lens[g], on the pages of
  *     prefix_table[g,:], and the sequence's own positions j < kv_lens[b], on those of block_table[b,:]
- * as dd_paged_attention computes it on a table that has both, but with a prefix's keys and values read once for all of its sequences
- * and not once for each.  A prefix may end within a page: the sequence's own positions begin on a page of their own.
+ * as dd_paged_attention computes it on a table that has both.  A prefix is taken for all of its sequences together, its keys and values read
+ * once for them, where its table and theirs are long next to the rows; where that would cost more than it saves (short tables; rows that fill
+ * row blocks by the hundred, as blocks and prompts of a batch do) each sequence takes prefix and own keys in one go, and reads what
+ * dd_paged_attention would.  Which of the two goes by sizes and capacities alone; the first needs a workspace.  A prefix may end within a
+ * page: the sequence's own positions begin on a page of their own.
  *   prefix_table [G,max_prefix_pages] i32, prefix_lens [G] i32;  group_starts [G+1] i32, not descending, in [0, B]: sequences below
  *   group_starts[0] and from group_starts[G] on have no prefix, and a group may have no sequence
  *   everything else (lengths, pages that are none, empty rows, dtypes, ranges, arithmetic) as for dd_paged_attention
  * For starts that descend, the outputs of the sequences concerned are unspecified; no access leaves the tensors.  The states of a row's
- * parts live in `workspace`; how many there are goes by sizes and capacities alone.
+ * parts live in `workspace`.
  * G, max_prefix_pages >= 1, max_prefix_pages*page_size < 2^30, (B*(ceil(n*H/Hkv / 32) + 1) + G)*Hkv < 2^22; O overlaps none of its inputs.
  */
 int dd_paged_attention_shared(const void *Q, const void *Kc, const void *Vc, const float *k_scale, const float *v_scale,

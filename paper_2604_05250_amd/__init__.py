@@ -283,7 +283,7 @@ def dd_paged_resize_workspace_bytes(n, B, page_size, max_pages) -> int:
 def dd_paged_resize(block_table, free_pages, num_free, lens, new_lens, page_size: int, n: int = 0, out_lens=None, positions=None, slots=None):
     """Sequences of lens [B] positions grow or shrink to new_lens [B]: pages that are over go back from block_table [B,max_pages] to
     the stack free_pages [pages] (its first num_free [1] entries are free), what is missing is taken from there, in place; a
-    sequence whose pages are not there stays as it is.  All int32 on the device.  Returns (out_lens [B]: the lengths now; positions
+    sequence whose pages are not there stays as it is, and so do those behind it that ask for any.  All int32 on the device.  Returns (out_lens [B]: the lengths now; positions
     [B,n] and slots [B,n] of the n rows behind lens: page * page_size + offset, -1 where the sequence has none; None each for n == 0)."""
     return native().paged_resize(block_table, free_pages, num_free, lens, new_lens, page_size, n, out_lens, positions, slots)
 
@@ -306,7 +306,7 @@ def dd_paged_attention_shared(Q, Kc, Vc, prefix_table, prefix_lens, group_starts
                               cache_dtype: Optional[int] = None):
     """dd_paged_attention for sequences that share prefixes: sequences group_starts[g] .. group_starts[g+1] - 1 attend the
     prefix_lens[g] positions on the pages prefix_table[g] and then their own kv_lens[b] on block_table[b]; a prefix is read once for all
-    of them.  prefix_table [G,max_prefix_pages], prefix_lens [G], group_starts [G+1], not descending: i32, on the device."""
+    of them where that pays by sizes and capacities, else by each sequence in one go with its own.  prefix_table [G,max_prefix_pages], prefix_lens [G], group_starts [G+1], not descending: i32, on the device."""
     return native().paged_attention_shared(Q, Kc, Vc, prefix_table, prefix_lens, group_starts, block_table, kv_lens, k_scale, v_scale, O, cache_dtype)
 
 
