@@ -172,7 +172,14 @@ __global__ __launch_bounds__(256) void places_kernel(TableKernelArgs a, int piec
 }
 
 int pieces_of(int n, int max_pages) { return ((n > max_pages ? n : max_pages) + kPiece - 1) / kPiece; }
-// one workgroup for everything, or a second launch
+// One workgroup for everything, or a second launch for entries and rows.  us for a call and its opposite, one / two launches, pages of 16:
+//     16 sequences, a token, tables of 64 entries         7.9 / 11.4       8192 rows: 16 x 512      11.6 / 12.4     128 x 64    17.5 / 17.1
+//     the same, tables of 4096                            7.7 / 12.0       16384: 16 x 1024         14.4 / 12.7
+//     all 65536 entries there and back: 16 x 4096        30.0 / 33.9       32768: 32 x 1024         21.0 / 13.8     1 x 32768   25.4 / 17.9
+//     64 x 1024  32.1 / 37.8      256 x 256  35.9 / 38.2
+// So two from 8192 rows on; entries that move cost as much either way, as what comes back is one workgroup's in both (a wave per sequence),
+// and those that do not move cost nothing, so 65536 of them is as far as this was timed.  Many sequences are slower in one launch
+// than they need be, a token of 1000 on 16 entries 20.0 / 12.1, of 4000 76.4 / 33.0: the rule does not go by that.
 bool small(int n, int B, int max_pages) { return (double)B * n <= 8192 && (double)B * max_pages <= 65536; }
 
 }  // namespace
