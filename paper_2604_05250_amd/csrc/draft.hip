@@ -378,7 +378,7 @@ template <bool BF16> __global__ __launch_bounds__(kThreads) void draft_decide_ke
                     s.q += eq;
                     s.above_p += above ? ep : 0;
                     s.above_q += above ? eq : 0;
-                    open = open || __builtin_fabs(more) <= kNear * ep;
+                    open = open || __builtin_fabs(more) < kNear * ep;      // (not where both are 0)
                 }
                 s.p += of_vector;
                 s.near_p += open ? of_vector : 0;
